@@ -215,6 +215,82 @@ size_t fwa_backward_workspace_bytes(int64_t N, int L, int C, int heads, int dtyp
 int fwa_bias_gather(const float* table, float* bias, int heads, int k, void* stream);
 int fwa_bias_scatter(const float* dbias, float* dtable, int heads, int k, void* stream);
 
+/*
+ * Relative-position bias by buckets for 1-D sequences.  The distance key - query of a pair, cut off at -far and
+ * far, names a column of the table:
+ *   bias[h][i][j] = table[h][ buckets[far + clamp(j - (q_start + i), -far, far)] ],   i < Lq, j < Lk
+ *   table   : [heads, columns] fp32
+ *   buckets : [2 far + 1] int32; an entry outside [0, columns) adds nothing and gets no gradient
+ *   q_start : position of query 0 on the axis of the keys
+ * fwa_bucket_gather  : table -> bias [heads, Lq, Lk], fp32 or (bias_dtype FWA_BF16, rounded once) bf16: the bias of
+ *                      fwa_forward and fwa_backward where Lq == Lk <= 256, or a dense one for other code
+ * fwa_bucket_scatter : dbias [heads, Lq, Lk] fp32 -> dtable [heads, columns], its adjoint: overwritten, fixed summation
+ *                      order, bit-reproducible.  `workspace` is device scratch of at least
+ *                      fwa_bucket_scatter_workspace_bytes(...) bytes, 16-byte aligned.
+ * heads <= 2^15, columns <= 2^16, far <= FWA_BUCKET_MAX_FAR, Lq and Lk from 0 to 2^24, heads * Lq <= 2^28.  table and buckets
+ * need 4-byte alignment only.  No dimension of zero launches anything but the zeros of dtable.
+ */
+#define FWA_BUCKET_MAX_FAR 8192
+int fwa_bucket_gather(const float* table, const int32_t* buckets, void* bias, int heads, int columns, int far,
+                      int Lq, int Lk, int64_t q_start, int bias_dtype, void* stream);
+int fwa_bucket_scatter(const float* dbias, const int32_t* buckets, float* dtable, int heads, int columns, int far,
+                       int Lq, int Lk, int64_t q_start, void* workspace, size_t workspace_bytes, void* stream);
+size_t fwa_bucket_scatter_workspace_bytes(int heads, int columns, int far, int Lq, int Lk);
+
+/*
+ * Attention of whole sequences: any number of queries and keys, scores never in memory.
+ *   O[n, i, head h] = sum_j P[i][j] V[n, j, head g],  P = softmax_j(scale * Q_ih . K_jg + B[h][i][j]),  g = h / (heads / kv_heads)
+ * over the keys j that query i sees.
+ *   q, o      : [N, Lq, heads * d], rows ld_q resp. ld_o elements apart (sequence n begins at row n * Lq)
+ *   k, v      : [N, Lk, kv_heads * d], rows ld_kv elements apart; kv_heads divides heads
+ *   d         : 32, 64 or 128; dtype FWA_F32, FWA_BF16 or FWA_F16.  Lq and Lk from 0 to 2^24.
+ *   table, buckets, columns, far : the bias B by buckets, formed inside the kernels, as in fwa_bucket_gather (with the
+ *               q_start below for each sequence); table NULL: none, the other three are ignored
+ *   q_lengths : NULL, or [N] int32: queries from q_lengths[n] on are padding; their rows of o are zero
+ *   k_lengths : NULL, or [N] int32: keys from k_lengths[n] on are not seen, whatever memory holds there.  Both lengths are cut
+ *               off at 0 and at Lq resp. Lk.
+ *   q_start   : NULL (0), or [N] int32: position of query 0 of sequence n on the axis of its keys
+ *   causal    : nonzero: query i sees the keys j <= q_start[n] + i only
+ *   stats     : NULL, or out [N, heads, Lq, 2] fp32: for each row a reference r and log2 of sum_j 2^(s_j - r), s the scores
+ *               in base-2 units (times log2 e); their sum times ln 2 is the logarithm of the row's sum.  (-inf, 0) for a row
+ *               without a key.
+ *   workspace : device scratch of at least fwa_sequence_forward_workspace_bytes(...) bytes (0 for most calls; few rows against
+ *               many keys are shared out over the keys and joined), 16-byte aligned
+ * A row that sees no key, or whose scores are all -inf, gives zeros.  Table values of -inf shut pairs out; the lowest finite value
+ * counts as such (a row of nothing else is uniform).  Inside the lengths q, k, v and d_o are expected to be finite: an
+ * infinity or NaN in a key's row may reach queries that causality keeps from seeing it.
+ * Arithmetic: fp32 data in fp32 throughout; 16-bit data are multiplied as they are, sums, softmax and statistics are fp32, P and
+ * (backward) dS are rounded once to the data's type in front of the product they enter.
+ * Lengths, starts, table and buckets need 4-byte alignment only.
+ */
+int fwa_sequence_forward(const void* q, const void* k, const void* v, void* o, float* stats,
+                         int64_t N, int Lq, int Lk, int heads, int kv_heads, int d, float scale,
+                         int64_t ld_q, int64_t ld_kv, int64_t ld_o,
+                         const float* table, const int32_t* buckets, int columns, int far,
+                         const int32_t* q_lengths, const int32_t* k_lengths, const int32_t* q_start, int causal,
+                         int dtype, void* workspace, size_t workspace_bytes, void* stream);
+size_t fwa_sequence_forward_workspace_bytes(int64_t N, int Lq, int Lk, int heads, int kv_heads, int d, int dtype);
+
+/*
+ * Its gradients, with the probabilities formed again from stats.
+ *   o, stats   : what the forward of the same arguments wrote
+ *   d_o        : in, like o, rows ld_do apart
+ *   dq, dk, dv : out, like q, k, v, rows ld_dq resp. ld_dkv apart, fully overwritten (padding with zeros)
+ *   dtable     : NULL, or out [heads, columns] fp32: the gradient of the table, overwritten; its terms are not rounded to the
+ *                data's type
+ *   workspace  : at least fwa_sequence_backward_workspace_bytes(...) bytes, 16-byte aligned
+ * Bit-reproducible from run to run.  With half data dS beyond 1023 overflows.
+ */
+int fwa_sequence_backward(const void* q, const void* k, const void* v, const void* o, const void* d_o, const float* stats,
+                          void* dq, void* dk, void* dv, float* dtable,
+                          int64_t N, int Lq, int Lk, int heads, int kv_heads, int d, float scale,
+                          int64_t ld_q, int64_t ld_kv, int64_t ld_o, int64_t ld_do, int64_t ld_dq, int64_t ld_dkv,
+                          const float* table, const int32_t* buckets, int columns, int far,
+                          const int32_t* q_lengths, const int32_t* k_lengths, const int32_t* q_start, int causal,
+                          int dtype, void* workspace, size_t workspace_bytes, void* stream);
+size_t fwa_sequence_backward_workspace_bytes(int64_t N, int Lq, int Lk, int heads, int kv_heads, int d, int far, int dtype,
+                                             int want_dtable);
+
 /* Static, NUL-terminated description of an error code. */
 const char* fwa_status_string(int code);
 

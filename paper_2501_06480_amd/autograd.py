@@ -7,6 +7,10 @@ its backward writes dq, dk, dv straight into one [N, L, 3, heads, d] gradient te
 The backward kernels need nothing from the forward but its inputs (paper Algorithm 2).
 Both take the mask either as a dense fp32 ``mask`` [nW, L, L] or as int32 region ``labels``
 [nW, L] with a ``mask_value`` (the kernels then form the mask themselves).
+
+``bucket_bias(table, buckets, Lq, Lk)`` is the dense bias of 1-D distances by buckets, differentiable in the table: the
+``bias`` of a window attention of such a sequence.  ``sequence_attention(q, k, v, heads, scale, table, buckets, ...)`` is
+attention of whole sequences, which forms that bias inside its kernels.
 """
 from __future__ import annotations
 
@@ -94,3 +98,51 @@ def window_attention_qkv(qkv, scale: float, bias=None, mask=None, labels=None, m
     N, L, _, heads, d = qkv.shape
     _check_dbias_supported(qkv, N, L, heads * d, heads, bias)
     return _WindowAttentionQKV.apply(qkv, bias, mask, scale, labels, float(mask_value))
+
+
+class _BucketBias(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, buckets, Lq, Lk, q_start, dtype):
+        ctx.save_for_backward(buckets)
+        ctx.columns, ctx.q_start = table.shape[1], q_start
+        return binding.fwa_bucket_gather(table, buckets, Lq, Lk, q_start, dtype)
+
+    @staticmethod
+    def backward(ctx, dbias):
+        buckets, = ctx.saved_tensors
+        return (binding.fwa_bucket_scatter(dbias.float().contiguous(), buckets.contiguous(), ctx.columns, ctx.q_start),) + (None,) * 5
+
+
+class _SequenceAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, table, buckets, q_lengths, k_lengths, q_start, heads, scale, causal):
+        o, stats = binding.fwa_sequence_forward(q, k, v, heads, scale, table, buckets, q_lengths, k_lengths, q_start, causal, want_stats=True)
+        ctx.save_for_backward(q, k, v, o, stats, table, buckets, q_lengths, k_lengths, q_start)
+        ctx.heads, ctx.scale, ctx.causal = heads, scale, causal
+        return o
+
+    @staticmethod
+    def backward(ctx, d_o):
+        q, k, v, o, stats, table, buckets, q_lengths, k_lengths, q_start = ctx.saved_tensors
+        dq, dk, dv, dtable = binding.fwa_sequence_backward(q, k, v, o, stats, d_o.contiguous(), ctx.heads, ctx.scale, table, buckets, q_lengths,
+                                                           k_lengths, q_start, ctx.causal, want_dtable=table is not None and ctx.needs_input_grad[3])
+        return (dq, dk, dv, dtable) + (None,) * 7
+
+
+def bucket_bias(table, buckets, Lq: int, Lk=None, q_start: int = 0, dtype=None):
+    """[heads, Lq, Lk] bias of a [heads, columns] table by buckets of the distance (``binding.fwa_bucket_gather``), fp32 or bf16,
+    differentiable in the table."""
+    if dtype not in (None, torch.float32, torch.bfloat16):
+        raise TypeError("the bias is float32 or bfloat16")
+    Lk = Lq if Lk is None else Lk
+    if _native_node(table, buckets):
+        return binding._native().bucket_bias(table, buckets, int(Lq), int(Lk), int(q_start), dtype == torch.bfloat16)
+    return _BucketBias.apply(table, buckets, int(Lq), int(Lk), int(q_start), dtype)
+
+
+def sequence_attention(q, k, v, heads: int, scale: float, table=None, buckets=None, q_lengths=None, k_lengths=None, q_start=None,
+                       causal: bool = False):
+    """Attention of whole sequences (``binding.fwa_sequence_forward``), differentiable in q, k, v and the table."""
+    if _native_node(q, k, v, table, buckets, q_lengths, k_lengths, q_start):
+        return binding._native().sequence_attention(q, k, v, int(heads), float(scale), table, buckets, q_lengths, k_lengths, q_start, bool(causal))
+    return _SequenceAttention.apply(q, k, v, table, buckets, q_lengths, k_lengths, q_start, int(heads), float(scale), bool(causal))

@@ -26,6 +26,7 @@ FWA_ERR_WORKSPACE = 5
 FWA_ERR_LAUNCH = 6
 FWA_ERR_ALIAS = 7
 FWA_NOALLOC_SCRATCH_BYTES = 16 * 1024 * 1024
+FWA_BUCKET_MAX_FAR = 8192
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libfwa.so")
@@ -33,7 +34,9 @@ _lib = None
 
 EXPORTS = ("fwa_forward", "fwa_forward_strided", "fwa_forward_labels", "fwa_backward", "fwa_backward_strided",
            "fwa_backward_labels", "fwa_backward_noalloc",
-           "fwa_backward_workspace_bytes", "fwa_bias_gather", "fwa_bias_scatter", "fwa_status_string")
+           "fwa_backward_workspace_bytes", "fwa_bias_gather", "fwa_bias_scatter", "fwa_status_string",
+           "fwa_bucket_gather", "fwa_bucket_scatter", "fwa_bucket_scatter_workspace_bytes", "fwa_sequence_forward",
+           "fwa_sequence_forward_workspace_bytes", "fwa_sequence_backward", "fwa_sequence_backward_workspace_bytes")
 
 
 class FwaError(RuntimeError):
@@ -85,6 +88,22 @@ def load_library():
     lib.fwa_bias_gather.argtypes = [vp, vp, ci, ci, vp]
     lib.fwa_bias_scatter.restype = ci
     lib.fwa_bias_scatter.argtypes = [vp, vp, ci, ci, vp]
+    lib.fwa_bucket_gather.restype = ci
+    lib.fwa_bucket_gather.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, i64, ci, vp]
+    lib.fwa_bucket_scatter.restype = ci
+    lib.fwa_bucket_scatter.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, i64, vp, sz, vp]
+    lib.fwa_bucket_scatter_workspace_bytes.restype = sz
+    lib.fwa_bucket_scatter_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
+    lib.fwa_sequence_forward.restype = ci
+    lib.fwa_sequence_forward.argtypes = [vp, vp, vp, vp, vp, i64, ci, ci, ci, ci, ci, cf, i64, i64, i64, vp, vp, ci, ci, vp, vp, vp, ci,
+                                         ci, vp, sz, vp]
+    lib.fwa_sequence_forward_workspace_bytes.restype = sz
+    lib.fwa_sequence_forward_workspace_bytes.argtypes = [i64, ci, ci, ci, ci, ci, ci]
+    lib.fwa_sequence_backward.restype = ci
+    lib.fwa_sequence_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, ci, ci, ci, ci, ci, cf, i64, i64, i64, i64, i64, i64,
+                                          vp, vp, ci, ci, vp, vp, vp, ci, ci, vp, sz, vp]
+    lib.fwa_sequence_backward_workspace_bytes.restype = sz
+    lib.fwa_sequence_backward_workspace_bytes.argtypes = [i64, ci, ci, ci, ci, ci, ci, ci, ci]
     lib.fwa_status_string.restype = ctypes.c_char_p
     lib.fwa_status_string.argtypes = [ci]
     _lib = lib
@@ -310,3 +329,114 @@ def fwa_bias_gather(table, k: int, stream=None):
 def fwa_bias_scatter(dbias, k: int, stream=None):
     """[heads, k*k, k*k] fp32 bias gradient -> [heads, (2k-1)^2] table gradient."""
     return _bias_call("bias_scatter", dbias, k, stream, "fwa_bias_scatter")
+
+
+def log_buckets(columns: int, far: int, bidirectional: bool = True, device=None):
+    """The usual map from distances -far .. far (key - query) to the columns of a bias table, as int32 [2 far + 1]: half of the
+    columns for keys at or behind the query and half for keys in front of it (all for the former where not `bidirectional`);
+    of each half the first half one distance each, the rest logarithmic up to `far`, whose column takes what lies beyond.
+    The borders are formed in whole numbers."""
+    if columns < (2 if bidirectional else 1) or far < 1:
+        raise ValueError("log_buckets needs columns for each direction and far >= 1")
+    if far > FWA_BUCKET_MAX_FAR:
+        raise ValueError(f"far must be at most {FWA_BUCKET_MAX_FAR}")
+    each = columns // 2 if bidirectional else columns
+    exact = each // 2
+    steps = each - exact
+    if exact > far:
+        raise ValueError("far must not be smaller than the distances with a column of their own")
+    half = []
+    t = 0
+    for n in range(far + 1):
+        if exact == 0 or n < exact:
+            half.append(min(n, each - 1))
+            continue
+        while t + 1 < steps and exact ** (steps - t - 1) * far ** (t + 1) <= n ** steps:
+            t += 1
+        half.append(exact + t)
+    front = [each + c for c in half] if bidirectional else [0] * (far + 1)
+    return _torch().tensor(half[:0:-1] + [half[0]] + front[1:], dtype=_torch().int32, device=device)
+
+
+def fwa_bucket_gather(table, buckets, Lq: int, Lk: Optional[int] = None, q_start: int = 0, dtype=None, out=None, stream=None):
+    """[heads, columns] fp32 table -> [heads, Lq, Lk] bias, bias[h, i, j] = table[h, buckets[far + clamp(j - q_start - i, -far, far)]],
+    fp32 or (`dtype`) bf16.  `buckets` is int32 [2 far + 1] (``log_buckets``)."""
+    torch = _torch()
+    if dtype not in (None, torch.float32, torch.bfloat16):
+        raise TypeError("the bias is float32 or bfloat16")
+    args = (table, buckets, int(Lq), int(Lq if Lk is None else Lk), int(q_start), dtype == torch.bfloat16, out)
+    call = (_native_mod or _native()).bucket_gather
+    if stream is None:
+        r = call(*args, None)
+    else:
+        with _alloc_on(stream, table.device):
+            r = call(*args, _stream_handle(stream, table.device))
+    if type(r) is int:
+        raise FwaError(r, "fwa_bucket_gather")
+    return r
+
+
+def fwa_bucket_scatter(dbias, buckets, columns: int, q_start: int = 0, workspace=None, stream=None):
+    """[heads, Lq, Lk] fp32 bias gradient -> [heads, columns] table gradient, the adjoint of ``fwa_bucket_gather``."""
+    call = (_native_mod or _native()).bucket_scatter
+    args = (dbias, buckets, int(columns), int(q_start), workspace)
+    if stream is None:
+        r = call(*args, None)
+    else:
+        with _alloc_on(stream, dbias.device):
+            r = call(*args, _stream_handle(stream, dbias.device))
+    if type(r) is int:
+        raise FwaError(r, "fwa_bucket_scatter")
+    return r
+
+
+def fwa_bucket_scatter_workspace_bytes(heads: int, columns: int, far: int, Lq: int, Lk: int) -> int:
+    return int(load_library().fwa_bucket_scatter_workspace_bytes(heads, columns, far, Lq, Lk))
+
+
+def fwa_sequence_forward(q, k, v, heads: int, scale: float, table=None, buckets=None, q_lengths=None, k_lengths=None, q_start=None,
+                         causal: bool = False, want_stats: bool = False, out=None, workspace=None, stream=None):
+    """softmax(scale Q K^T + B) V of whole sequences: q [N, Lq, heads * d], k and v [N, Lk, kv_heads * d] on the GPU (row-strided views
+    of fused projections or caches as well), d 32, 64 or 128, kv_heads a divisor of heads.  B is the bias by buckets of the
+    distance (``fwa_bucket_gather``), formed inside the kernels.  int32 [N] tensors: `q_lengths` (rows behind them give zeros),
+    `k_lengths` (keys behind them are not seen), `q_start` (position of query 0 among the keys: 0 for a sequence that attends to
+    itself, the number of earlier tokens for new ones against a cache).  `causal`: query i sees keys up to q_start + i.
+    Returns o, or (o, stats) with the row statistics that the backward reads: stats.sum(-1) * ln 2 is the logarithm of each
+    row's sum of exponentials."""
+    args = (q, k, v, int(heads), float(scale), table, buckets, q_lengths, k_lengths, q_start, bool(causal), bool(want_stats), out, workspace)
+    call = (_native_mod or _native()).sequence_forward
+    if stream is None:
+        r = call(*args, None)
+    else:
+        with _alloc_on(stream, q.device):
+            r = call(*args, _stream_handle(stream, q.device))
+    if type(r) is int:
+        raise FwaError(r, "fwa_sequence_forward")
+    return r
+
+
+def fwa_sequence_forward_workspace_bytes(N: int, Lq: int, Lk: int, heads: int, kv_heads: int, d: int, dtype: int) -> int:
+    return int(load_library().fwa_sequence_forward_workspace_bytes(N, Lq, Lk, heads, kv_heads, d, dtype))
+
+
+def fwa_sequence_backward(q, k, v, o, stats, d_o, heads: int, scale: float, table=None, buckets=None, q_lengths=None, k_lengths=None,
+                          q_start=None, causal: bool = False, want_dtable: bool = False, out=None, workspace=None, stream=None):
+    """(dQ, dK, dV, dTable) of ``fwa_sequence_forward`` with the same arguments, whose results `o` and `stats` are given.  dTable is
+    None unless asked for.  `out` = (dq, dk, dv) writes into given tensors."""
+    dq, dk, dv = out if out is not None else (None, None, None)
+    args = (q, k, v, o, stats, d_o, int(heads), float(scale), table, buckets, q_lengths, k_lengths, q_start, bool(causal), bool(want_dtable),
+            dq, dk, dv, workspace)
+    call = (_native_mod or _native()).sequence_backward
+    if stream is None:
+        r = call(*args, None)
+    else:
+        with _alloc_on(stream, q.device):
+            r = call(*args, _stream_handle(stream, q.device))
+    if type(r) is int:
+        raise FwaError(r, "fwa_sequence_backward")
+    return r
+
+
+def fwa_sequence_backward_workspace_bytes(N: int, Lq: int, Lk: int, heads: int, kv_heads: int, d: int, far: int, dtype: int,
+                                          want_dtable: bool) -> int:
+    return int(load_library().fwa_sequence_backward_workspace_bytes(N, Lq, Lk, heads, kv_heads, d, far, dtype, int(bool(want_dtable))))

@@ -1,6 +1,7 @@
 // extern "C" entry points of libfwa: argument validation and dispatch.
 // Every check happens before any HIP call, so an error never launches work.
 #include "../../include/fwa.h"
+#include "fwa_check.h"
 #include "fwa_internal.h"
 
 namespace fwa {
@@ -61,7 +62,7 @@ hipError_t allow_lds(const void* fn, size_t lds_bytes) {
 
 namespace {
 
-inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+using namespace fwa::check;
 
 // Shape checks shared by forward, backward and the workspace query.
 // Head width 32 everywhere; 64, 128 and 256 for L <= 64 (`wide_ok`: every forward and backward call).
@@ -94,37 +95,6 @@ int check_backward_support(int L, int dtype, bool want_dbias) {
 // floats, rounded up to 256 bytes
 size_t large_bias_copy_bytes(int L, int heads) {
     return (((size_t)heads * L * L * sizeof(float)) + 255) & ~(size_t)255;
-}
-
-// Row stride of a strided tensor, in elements: at least C, rows 16-byte aligned, and small enough
-// that the byte offsets inside one window fit 32 bits with room to spare.
-int check_row_stride(int64_t ld, int C, int dtype) {
-    const int64_t per16 = dtype == FWA_F32 ? 4 : 8;
-    if (ld < C) return FWA_ERR_SHAPE;
-    if (ld % per16 != 0) return FWA_ERR_ALIGN;
-    if (ld > (int64_t)1 << 20) return FWA_ERR_UNSUPPORTED;
-    return FWA_OK;
-}
-
-// A row-strided [N, L, C] tensor as the bytes it touches: rows of `width` bytes every `ld` bytes.
-struct Span {
-    uintptr_t base;
-    uint64_t ld, width, rows;
-    uintptr_t end() const { return base + (rows - 1) * ld + width; }
-};
-Span span_of(const void* p, int64_t N, int L, int C, int64_t ld, int dtype) {
-    const uint64_t e = dtype == FWA_F32 ? 4 : 2;
-    return Span{reinterpret_cast<uintptr_t>(p), (uint64_t)ld * e, (uint64_t)C * e, (uint64_t)N * (uint64_t)L};
-}
-// Whether two such tensors share a byte.  Tensors whose extents are disjoint do not.  With equal row
-// strides (the views of one fused [N, L, 3, heads, d] buffer) the test is exact: rows interleave
-// without touching iff the bases differ, modulo the stride, by at least a row width either way.
-// Extents that intersect under different strides are reported as overlapping (conservative).
-bool overlaps(const Span& a, const Span& b) {
-    if (a.end() <= b.base || b.end() <= a.base) return false;
-    if (a.ld != b.ld) return true;
-    const uint64_t d = (a.base >= b.base ? a.base - b.base : b.base - a.base) % a.ld;
-    return d < a.width || a.ld - d < a.width;
 }
 
 // The mask comes as a dense tile per window position or as region labels, never both.

@@ -111,4 +111,46 @@ hipError_t launch_widen_bf16(const void* src, float* dst, size_t count, hipStrea
 hipError_t launch_bias_gather(const float* table, float* bias, int heads, int k, hipStream_t s);
 hipError_t launch_bias_scatter(const float* dbias, float* dtable, int heads, int k, hipStream_t s);
 
+// Attention of whole sequences (fwa_sequence_*.hip).
+struct SeqArgs {
+    const void* q;       // [N, Lq, H * D]
+    const void* k;       // [N, Lk, KV * D]
+    const void* v;
+    void* o;             // forward: out; backward: in
+    float* stats;        // [N, H, Lq, 2]: reference and base-2 logarithm of the sum of each row, or nullptr (forward only)
+    const void* d_o;
+    void* dq;
+    void* dk;
+    void* dv;
+    float* dtable;       // [H, nb] or nullptr
+    const float* table;  // [H, nb] or nullptr
+    const int32_t* buckets;  // [2 far + 1]
+    const int32_t* q_len;    // [N] or nullptr
+    const int32_t* k_len;
+    const int32_t* q_start;
+    long long N;
+    int Lq, Lk, H, KV, D;
+    int nb, far;
+    int causal;
+    int dtype;           // 0 fp32, 1 bf16, 2 half
+    float scale;
+    long long ldq, ldk, ldo, ldg, lddq, lddk;  // elements between rows of q; of k and v; of o; of d_o; of dq; of dk and dv
+};
+
+// Keys per tile of the forward: two tiles each of K and V take at most 64 KB of LDS, and 32 KB where a workgroup is one wave of
+// 16-bit data (five workgroups on a CU).
+constexpr int seq_forward_keys(int row_bytes, int waves) { return row_bytes >= 512 || (waves == 1 && row_bytes >= 256) ? 32 : 64; }
+
+hipError_t launch_sequence_forward(const SeqArgs& a, void* workspace, hipStream_t s);
+size_t seq_forward_workspace(const SeqArgs& a);
+hipError_t launch_sequence_backward(const SeqArgs& a, void* workspace, hipStream_t s);
+size_t seq_backward_workspace(const SeqArgs& a, bool want_dtable);
+hipError_t launch_bucket_gather(const float* table, const int32_t* buckets, void* bias, int heads, int nb, int far, int Lq, int Lk, int q_start, bool bf16,
+                                hipStream_t s);
+size_t bucket_lines_bytes(int heads, int far, long long count);
+hipError_t launch_bucket_sums(const float* parts, float* lines, const int32_t* buckets, float* dtable, int heads, int nb, int far, long long count, hipStream_t s);
+size_t bucket_scatter_workspace(int heads, int far, int Lq);
+hipError_t launch_bucket_scatter(const float* dbias, const int32_t* buckets, float* dtable, int heads, int nb, int far, int Lq, int Lk, int q_start,
+                                 float* workspace, hipStream_t s);
+
 }  // namespace fwa

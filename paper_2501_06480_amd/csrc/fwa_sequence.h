@@ -1,0 +1,220 @@
+// Shared parts of the kernels for attention over whole sequences (fwa_sequence_forward.hip, fwa_sequence_backward.hip).
+//
+// Products run on the 32 x 32 matrix instructions.  Lane (hi, c), hi = lane >> 5, c = lane & 31, supplies row resp. column c of an
+// operand and receives column c of the result, rows 8 (r / 4) + 4 hi + r % 4 of it in register r = 0..15.  A tile of scores is
+// always formed such that the index a later product sums over runs over the registers: its 16 values per lane are then an operand of
+// that product as they stand, k-slots in the order of the registers, and the probabilities never go through LDS.  The other operand
+// of the later product is read from LDS in the same order: 16-bit data by the transposing read, fp32 data a row at a time.
+#pragma once
+
+#include "fwa_device.h"
+#include "fwa_internal.h"
+
+namespace fwa {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+struct SeqBf16 {};
+struct SeqF16 {};
+struct SeqF32 {};
+template <class T>
+struct SeqSize { static constexpr int value = 2; };
+template <>
+struct SeqSize<SeqF32> { static constexpr int value = 4; };
+
+// One step of a product whose operands have their k-slots along a row of memory: 32 bytes of each row, lane (hi, c) holding
+// bytes 16 hi .. 16 hi + 15 of row c.
+template <class T>
+__device__ __forceinline__ f32x16 seq_dot(const u32x4& a, const u32x4& b, f32x16 c) {
+    if constexpr (__is_same(T, SeqBf16)) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+    } else if constexpr (__is_same(T, SeqF16)) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    } else {
+        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], c, 0, 0, 0);
+        return c;
+    }
+}
+
+// Tiles in LDS: rows of RB bytes, one behind the other; within a row the 16-byte chunk c stands at place c ^ seq_swizzle(row), so that
+// both the reads of one chunk of 16 rows and the transposing reads of 64 bytes of 8 rows meet every bank equally often.
+template <int RB>
+__device__ __forceinline__ constexpr uint32_t seq_swizzle(uint32_t row) {
+    if constexpr (RB == 64) return (row >> 2) & 3u;
+    else if constexpr (RB == 128) return ((row & 2u) << 1) | ((row >> 2) & 3u);
+    else return ((row & 3u) << 2) | ((row >> 2) & 3u);
+}
+
+// The loads of one tile of ROWS rows by WAVES waves: wave-uniform descriptor, 1024 bytes of LDS per load.
+template <int RB, int ROWS, int WAVES>
+struct SeqLoader {
+    static constexpr int kLoads = ROWS * RB / 1024 / WAVES;
+    static_assert(kLoads >= 1 && kLoads * 1024 * WAVES == ROWS * RB, "a tile is a whole number of loads per wave");
+    uint32_t off[kLoads];
+    uint32_t to;
+    __device__ __forceinline__ void init(uint32_t wave, uint32_t lane, uint32_t row_bytes) {
+        to = wave * 1024u;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const uint32_t at = ((uint32_t)i * WAVES + wave) * 1024u + lane * 16u;
+            const uint32_t row = at / RB, place = (at % RB) / 16u;
+            off[i] = row * row_bytes + ((place ^ seq_swizzle<RB>(row)) * 16u);
+        }
+    }
+    // rows from `first` on (64-bit), `rows` of which exist; `lds` = the tile's place
+    __device__ __forceinline__ void issue(const char* first, int rows, uint32_t row_bytes, uint32_t lds) const {
+        const uint32_t n = rows < ROWS ? (rows > 0 ? (uint32_t)rows : 0u) : (uint32_t)ROWS;
+        const u32x4 src = lds_source(first, n ? (n - 1u) * row_bytes + RB : 0u);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load_to_lds(src, off[i], lds + to + (uint32_t)i * (1024u * WAVES));
+    }
+};
+
+__device__ __forceinline__ u32x4 seq_lds_b128(uint32_t at) {
+    return *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)at;
+}
+__device__ __forceinline__ float seq_lds_f32(uint32_t at) {
+    return *(const __attribute__((address_space(3))) float*)(uintptr_t)at;
+}
+__device__ __forceinline__ f32x4 seq_lds_f32x4(uint32_t at) {
+    return *(const __attribute__((address_space(3))) f32x4*)(uintptr_t)at;
+}
+__device__ __forceinline__ void seq_lds_put(uint32_t at, float x) {
+    *(__attribute__((address_space(3))) float*)(uintptr_t)at = x;
+}
+__device__ __forceinline__ uint2 seq_lds_tr(uint32_t at) {
+    typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+    const v4i16 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(uintptr_t)at);
+    return __builtin_bit_cast(uint2, v);
+}
+
+// Where lane (hi, c) finds chunk 2 s + hi of row c of a tile: place() ^ 32 s, plus 32 RB for the next 32 rows.
+template <int RB>
+struct SeqRowReader {
+    uint32_t at;
+    __device__ __forceinline__ void init(uint32_t hi, uint32_t c) { at = c * RB + ((hi ^ seq_swizzle<RB>(c)) << 4); }
+    __device__ __forceinline__ u32x4 read(uint32_t tile, int s, int block) const {
+        return seq_lds_b128(tile + (at ^ (uint32_t)(32 * s)) + (uint32_t)(32 * RB * block));
+    }
+};
+
+// Sums over the rows of a tile in LDS: acc[b] += X[rows of the block][channels 32 b ..]^T  times the 32 x 32 tile in `w`, whose registers run
+// over the rows.
+template <class T, int D>
+struct SeqColumnReader {
+    static constexpr int RB = D * SeqSize<T>::value;
+    uint32_t at;
+    __device__ __forceinline__ void init(uint32_t hi, uint32_t c) {
+        if constexpr (__is_same(T, SeqF32)) {
+            // row 4 hi, channel c
+            at = 4u * hi * RB + (((c >> 2) ^ seq_swizzle<RB>(4u * hi)) << 4) + 4u * (c & 3u);
+        } else {
+            // lane r of 16 passes row 4 hi + (r >> 2), channels 16 (c >> 4) + 4 (r & 3) ..
+            const uint32_t r = c & 15u, row = 4u * hi + (r >> 2), chunk = 2u * (c >> 4) + ((r & 3u) >> 1);
+            at = row * RB + ((chunk ^ seq_swizzle<RB>(row)) << 4) + 8u * (r & 1u);
+        }
+    }
+    __device__ __forceinline__ void accumulate(f32x16 (&acc)[D / 32], uint32_t tile, int block, const f32x16& w) const {
+        tile += (uint32_t)(32 * RB * block);
+        if constexpr (__is_same(T, SeqF32)) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const uint32_t row = 8u * (r / 4) + r % 4;  // and 4 hi, in `at`
+                const float x = w[r];
+#pragma unroll
+                for (int b = 0; b < D / 32; ++b) {
+                    const uint32_t flip = (seq_swizzle<RB>(row) << 4) ^ (uint32_t)(128 * b);
+                    acc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(seq_lds_f32(tile + (at ^ flip) + row * RB), x, acc[b], 0, 0, 0);
+                }
+            }
+        } else {
+            constexpr bool F16 = __is_same(T, SeqF16);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const u32x4 x = {pack_e<F16>(w[8 * t], w[8 * t + 1]), pack_e<F16>(w[8 * t + 2], w[8 * t + 3]),
+                                 pack_e<F16>(w[8 * t + 4], w[8 * t + 5]), pack_e<F16>(w[8 * t + 6], w[8 * t + 7])};
+#pragma unroll
+                for (int b = 0; b < D / 32; ++b) {
+                    const uint32_t first = at ^ (uint32_t)(64 * b), second = first ^ (seq_swizzle<RB>(8u) << 4);
+                    const uint2 p = seq_lds_tr(tile + first + (uint32_t)(16 * t) * RB);
+                    const uint2 q = seq_lds_tr(tile + second + (uint32_t)(16 * t + 8) * RB);
+                    acc[b] = seq_dot<T>(u32x4{p.x, p.y, q.x, q.y}, x, acc[b]);
+                }
+            }
+        }
+    }
+};
+
+// max / sum of a value over the two lanes (0, c), (1, c)
+__device__ __forceinline__ float seq_max_halves(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t a = s[0], b = s[1];
+    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+__device__ __forceinline__ float seq_sum_halves(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t a = s[0], b = s[1];
+    return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+}
+
+__device__ __forceinline__ void seq_zero(f32x16& x) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = 0.f;
+}
+
+// One entry of the table in base-2 units.  Finite values keep finite in these units: the type's lowest value, which stands for a mask in
+// many programs, would otherwise turn into an infinity, and a row of nothing else would be empty instead of uniform.
+__device__ __forceinline__ float seq_bias_log2(float b) {
+    const float x = b * kLog2e;
+    return __builtin_isinf(b) ? b : fminf(fmaxf(x, -3.4e38f), 3.4e38f);
+}
+// The bias of distance key - query for a head's row of the table; entries of the map outside the table add nothing.
+__device__ __forceinline__ float seq_bias_at(const float* row, const int32_t* buckets, int nb, int far, int distance) {
+    const int at = distance < -far ? -far : (distance > far ? far : distance);
+    const uint32_t b = (uint32_t)buckets[far + at];
+    return b < (uint32_t)nb ? seq_bias_log2(row[b]) : 0.f;
+}
+
+// Positions are int32 of the caller's; beyond these bounds every distance is cut off at `far` and every comparison decided, so they are
+// cut there and sums of a position and a row cannot overflow.
+constexpr int kSeqFarthest = 1 << 29;
+__device__ __forceinline__ int seq_length(const int32_t* lengths, long long n, int most) {
+    if (lengths == nullptr) return most;
+    const int x = lengths[n];
+    return x < 0 ? 0 : (x > most ? most : x);
+}
+__device__ __forceinline__ int seq_start(const int32_t* starts, long long n) {
+    if (starts == nullptr) return 0;
+    const int x = starts[n];
+    return x < -kSeqFarthest ? -kSeqFarthest : (x > kSeqFarthest ? kSeqFarthest : x);
+}
+
+// Four neighbouring channels of a row, rounded to the type.
+template <class T>
+__device__ __forceinline__ void seq_store4(char* row, uint32_t channel, float a, float b, float c, float d) {
+    if constexpr (__is_same(T, SeqF32)) {
+        *reinterpret_cast<f32x4*>(row + channel * 4u) = f32x4{a, b, c, d};
+    } else {
+        constexpr bool F16 = __is_same(T, SeqF16);
+        *reinterpret_cast<uint2*>(row + channel * 2u) = uint2{pack_e<F16>(a, b), pack_e<F16>(c, d)};
+    }
+}
+
+// How a forward call is laid out on the device.
+struct SeqPlan {
+    int group;           // heads of queries per head of keys
+    int packed;          // one block has the rows of a whole group (few rows: group * Lq <= 32)
+    int waves, blocks, splits;
+    unsigned grid;
+    uint32_t xcd_q, xcd_r, bias_entries;
+    FastDiv by_splits, by_blocks, by_heads;
+    size_t rows;         // N * H * Lq
+    float* part_o;       // [splits][rows][D], not divided by the sum
+    float* part_ml;      // [splits][rows][2]
+};
+
+}  // namespace fwa

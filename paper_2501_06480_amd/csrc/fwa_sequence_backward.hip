@@ -1,0 +1,595 @@
+// Gradients of the attention of whole sequences, from q, k, v, o, d_o and the forward's row statistics; the probabilities are formed
+// again.  Two kernels, each with the sums of its outputs in registers, so that no gradient needs atomics and every result is the same
+// from run to run:
+//   rows   a wave has 32 queries and walks the keys: dQ, the row sums delta = sum_j P dP, the sums of dS by distance for the table
+//   keys   a wave has 32 keys and walks the queries (of all heads that share them): dK, dV
+// Scores and dP = dO V^T are formed in both (14 instead of 10 flops per channel of a pair); the alternative, dQ added up in memory over the
+// blocks of keys, has no fixed order.  Both products of a tile use its P and dS as they stand in registers (fwa_sequence.h).
+#include "fwa_sequence.h"
+
+namespace fwa {
+namespace {
+
+struct BackPlan {
+    int group, waves, row_blocks, key_blocks, splits;
+    unsigned row_grid, key_grid;
+    uint32_t row_q, row_r, key_q, key_r, bias_entries;
+    FastDiv by_row_blocks, by_heads, by_key_blocks, by_splits, by_kv;
+    int row_waves;       // waves with rows per head of a sequence: ceil(Lq / 32)
+    float* delta;        // [N, H, Lq]
+    float* parts;        // [H][N * row_waves][2 far + 1] sums of dS by distance
+    float* lines;
+    float* part_kv;      // [splits][2][N, Lk, KV, D]
+};
+
+constexpr float kDead = __builtin_inff();
+
+// the weight of a score in base-2 units, against the reference of its row
+__device__ __forceinline__ float weight(float s, float ref) { return __builtin_amdgcn_exp2f(s - ref); }
+
+template <class T, int D, int W, int KT, bool TABLE>
+__global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan plan) {
+    constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, KS = KT / 32;
+    constexpr uint32_t kTile = KT * RB, kLine = KT + 32;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const uint32_t base = lds_offset(lds), bias_at = base + 4u * kTile, bias_bytes = 4u * plan.bias_entries;
+    const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t hi = lane >> 5, c = lane & 31u;
+
+    uint32_t at = xcd_logical_block(blockIdx.x, plan.row_q, plan.row_r);
+    uint32_t rest = fastdiv(at, plan.by_row_blocks);
+    int block = (int)(at - rest * plan.by_row_blocks.d);
+    const long long n = fastdiv(rest, plan.by_heads);
+    const int head = (int)(rest - (uint32_t)n * plan.by_heads.d), kv = head / plan.group;
+    if (a.causal) block = plan.row_blocks - 1 - block;
+    const int i0 = block * 32 * W, i = i0 + (int)(32u * wave + c);
+    const int span_rows = a.Lq - i0 < 32 * W ? a.Lq - i0 : 32 * W;
+    const int qlen = seq_length(a.q_len, n, a.Lq), klen = seq_length(a.k_len, n, a.Lk), start = seq_start(a.q_start, n);
+    const int first = start + i0, last = first + span_rows - 1, pos = i < a.Lq ? start + i : last;
+
+    int kend = i0 < qlen ? klen : 0;
+    if (a.causal && kend > last + 1) kend = last + 1 > 0 ? last + 1 : 0;
+    const int tiles = (kend + KT - 1) / KT;
+
+    const char* const kp = static_cast<const char*>(a.k) + ((size_t)n * a.Lk * a.ldk + (size_t)kv * D) * E;
+    const char* const vp = static_cast<const char*>(a.v) + ((size_t)n * a.Lk * a.ldk + (size_t)kv * D) * E;
+    const uint32_t kld = (uint32_t)(a.ldk * E);
+    SeqLoader<RB, KT, W> load;
+    load.init(wave, lane, kld);
+    SeqRowReader<RB> row_reader;
+    row_reader.init(hi, c);
+    SeqColumnReader<T, D> column_reader;
+    column_reader.init(hi, c);
+    auto issue = [&](int t, uint32_t buf) {
+        const size_t row = (size_t)t * KT;
+        const uint32_t to = base + buf * 2u * kTile;
+        load.issue(kp + row * kld, klen - t * KT, kld, to);
+        load.issue(vp + row * kld, klen - t * KT, kld, to + kTile);
+    };
+
+    const size_t row = ((size_t)n * a.H + head) * a.Lq + i;
+    bool dead = true;
+    float ref = 0.f, rl = 0.f, delta = 0.f;
+    u32x4 qf[NC], gf[NC];
+#pragma unroll
+    for (int s = 0; s < NC; ++s) qf[s] = gf[s] = u32x4{0u, 0u, 0u, 0u};
+    if (i < qlen) {
+        const f32x2 stat = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
+        dead = stat[0] == -__builtin_inff();
+        ref = dead ? 0.f : stat[0];
+        rl = dead ? 0.f : __builtin_amdgcn_exp2f(-stat[1]);
+        const size_t at_row = (size_t)n * a.Lq + i, channel = (size_t)head * D;
+        const char* const qp = static_cast<const char*>(a.q) + (at_row * a.ldq + channel) * E + 16u * hi;
+        const char* const gp = static_cast<const char*>(a.d_o) + (at_row * a.ldg + channel) * E + 16u * hi;
+        const char* const op = static_cast<const char*>(a.o) + (at_row * a.ldo + channel) * E + 16u * hi;
+        // delta as the product of d_o and the rounded output; the rounding is taken out below
+#pragma unroll
+        for (int s = 0; s < NC; ++s) {
+            qf[s] = *reinterpret_cast<const u32x4*>(qp + 32 * s);
+            gf[s] = *reinterpret_cast<const u32x4*>(gp + 32 * s);
+            const u32x4 of = *reinterpret_cast<const u32x4*>(op + 32 * s);
+            if constexpr (__is_same(T, SeqF32)) {
+                const f32x4 x = __builtin_bit_cast(f32x4, of), y = __builtin_bit_cast(f32x4, gf[s]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) delta = fmaf(x[e], y[e], delta);
+            } else if constexpr (__is_same(T, SeqF16)) {
+                const f16x8 x = __builtin_bit_cast(f16x8, of), y = __builtin_bit_cast(f16x8, gf[s]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) delta = fmaf((float)x[e], (float)y[e], delta);
+            } else {
+                const bf16x8 x = as_bf16x8(of), y = as_bf16x8(gf[s]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) delta = fmaf((float)x[e], (float)y[e], delta);
+            }
+        }
+    }
+    delta = seq_sum_halves(delta);
+    const bool some_dead = __any(dead);
+    if (klen % KT != 0 && tiles > 0) {  // rows that no load fills: as in the forward
+        for (uint32_t o = threadIdx.x * 16u; o < 4u * kTile; o += 64u * W * 16u) *reinterpret_cast<u32x4*>(lds + o) = u32x4{0u, 0u, 0u, 0u};
+        __syncthreads();
+    }
+
+    const float* const table = a.table ? a.table + (size_t)head * a.nb : nullptr;
+    const int far = a.far;
+    const float below = table ? seq_bias_at(table, a.buckets, a.nb, far, -far) : 0.f, above = table ? seq_bias_at(table, a.buckets, a.nb, far, far) : 0.f;
+    const uint32_t entries = (uint32_t)(KT + span_rows - 1), my_bias = bias_at + 4u * ((uint32_t)(last - pos) + 4u * hi);
+    const int lim = dead ? 0 : (a.causal && pos + 1 < klen ? pos + 1 : klen);
+    const float scale = a.scale * kLog2e;
+    auto is_near = [&](int t) { return table && t * KT - last < far && t * KT + KT - 1 - first > -far; };
+
+    // before the barrier of tile t: its bias; behind it: the loads of the tile that follows
+    auto begin = [&](int t, uint32_t buf, bool more) {
+        if (is_near(t))
+            for (uint32_t e = threadIdx.x; e < entries; e += 64u * W)
+                seq_lds_put(bias_at + buf * bias_bytes + 4u * e, seq_bias_at(table, a.buckets, a.nb, far, t * KT - last + (int)e));
+        lds_loads_done();
+        __syncthreads();
+        if (more) issue(t + 1, buf ^ 1u);
+    };
+    // weights exp2(s - ref), the row's sum not divided out, and dP of a block of 32 keys
+    auto scores = [&](int t, uint32_t buf, int k, f32x16& p, f32x16& dp) {
+        const uint32_t kt = base + buf * 2u * kTile, vt = kt + kTile;
+        const int j0 = t * KT;
+        seq_zero(p);
+        seq_zero(dp);
+#pragma unroll
+        for (int x = 0; x < NC; ++x) p = seq_dot<T>(row_reader.read(kt, x, k), qf[x], p);
+#pragma unroll
+        for (int x = 0; x < NC; ++x) dp = seq_dot<T>(row_reader.read(vt, x, k), gf[x], dp);
+        if (is_near(t)) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) p[r] = fmaf(p[r], scale, seq_lds_f32(my_bias + buf * bias_bytes + 4u * (32 * k + 8 * (r / 4) + r % 4)));
+        } else {
+            const float b = j0 + KT - 1 - first <= -far ? below : above;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) p[r] = fmaf(p[r], scale, b);
+        }
+        if (some_dead || j0 + KT > klen || (a.causal && j0 + KT - 1 > first)) {
+            const int room = lim - j0 - 4 * (int)hi;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) p[r] = 32 * k + 8 * (r / 4) + r % 4 < room ? p[r] : -__builtin_inff();
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] = weight(p[r], ref);
+    };
+
+    f32x16 dq[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) seq_zero(dq[b]);
+    float ds_all = 0.f, ds_below = 0.f, ds_above = 0.f, p_below = 0.f, p_above = 0.f;
+    if (tiles > 0) issue(0, 0);
+    for (int t = 0; t < tiles; ++t) {
+        const uint32_t buf = (uint32_t)t & 1u;
+        begin(t, buf, t + 1 < tiles);
+        f32x16 p, dp;
+        if (tiles == 1) {
+            // few keys, of which one may have all the weight: delta from the same products as dP, so that what cancels does so exactly
+            float sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                scores(t, buf, k, p, dp);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum = fmaf(p[r], dp[r], sum);
+            }
+            delta = rl * seq_sum_halves(sum);
+        }
+        float ds_tile = 0.f, p_tile = 0.f;
+        const bool near = is_near(t);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            scores(t, buf, k, p, dp);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dp[r] = p[r] * (dp[r] - delta);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) ds_tile += dp[r];
+            if constexpr (TABLE) {
+                if (!near)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) p_tile += p[r];
+            }
+            column_reader.accumulate(dq, base + buf * 2u * kTile, k, dp);
+        }
+        ds_all += ds_tile;
+        if constexpr (TABLE) {
+            if (!near && t * KT + KT - 1 - first <= -far) { ds_below += ds_tile; p_below += p_tile; }
+            else if (!near) { ds_above += ds_tile; p_above += p_tile; }
+        }
+    }
+    // The dS of a row add up to zero; what they add up to is what delta is off by, times the row's weights.  dQ of 16-bit data keeps
+    // it (it is below the roundings of dS); dK and the sums by distance, which are not rounded, get the better delta.
+    const float off = rl * seq_sum_halves(ds_all);
+    delta += off;
+
+    if constexpr (TABLE) {
+        float sum_below = rl * (ds_below - off * p_below), sum_above = rl * (ds_above - off * p_above);
+        // sums by distance where the distances tell
+        int t0 = first - far - KT + 1, t1 = (far + last + KT - 1);
+        t0 = t0 < 0 ? 0 : t0 / KT + 1;
+        t1 = t1 < 0 ? 0 : t1 / KT;
+        if (t1 > tiles) t1 = tiles;
+        const uint32_t line_at = bias_at + 2u * bias_bytes + wave * (8u * kLine), mine = line_at + 4u * kLine * hi;
+        const int wave_last = first + 32 * (int)wave + 31;
+        const bool writes = i0 + 32 * (int)wave < a.Lq;
+        const size_t width = 2 * (size_t)far + 1;
+        float* const out = plan.parts + (((size_t)head * a.N + n) * plan.row_waves + (block * W + (int)wave)) * width;
+        // entry e of the two lines, one for each half of the wave: distance e + t KT - wave_last
+        for (uint32_t e = lane; e < 2u * kLine; e += 64u) seq_lds_put(line_at + 4u * e, 0.f);
+        auto flush = [&](int from, int count) {
+            if ((int)lane < count) {
+                const float x = seq_lds_f32(line_at + 4u * lane) + seq_lds_f32(line_at + 4u * (kLine + lane));
+                const int d = from + (int)lane;
+                if (d <= -far) sum_below += x;
+                else if (d >= far) sum_above += x;
+                else if (writes) out[far + d] = x;
+            }
+        };
+        __syncthreads();  // the tiles of the first walk have been read by all waves
+        if (t0 < t1) issue(t0, 0);
+        for (int t = t0; t < t1; ++t) {
+            const uint32_t buf = (uint32_t)(t - t0) & 1u;
+            begin(t, buf, t + 1 < t1);
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                f32x16 p, dp;
+                scores(t, buf, k, p, dp);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float x = rl * p[r] * (dp[r] - delta);
+                    // lanes of a half have places of their own, and a wave's additions are made in its order
+                    __hip_atomic_fetch_add((__attribute__((address_space(3))) float*)(uintptr_t)(mine + 4u * (31u - c + 4u * hi) + 4u * (32 * k + 8 * (r / 4) + r % 4)), x,
+                                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+            flush(t * KT - wave_last, KT);
+            const float x = seq_lds_f32(mine + 4u * (KT + c));
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+            seq_lds_put(mine + 4u * c, x);
+#pragma unroll
+            for (int k = 1; k <= KS; ++k) seq_lds_put(mine + 4u * (32 * k + c), 0.f);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+        }
+        int from = 1 << 30, to = 1 << 30;
+        if (t0 < t1) {
+            flush(t1 * KT - wave_last, 31);
+            from = t0 * KT - wave_last;
+            to = t1 * KT - wave_last + 31;
+        }
+        if (writes) {
+            for (int d = 1 - far + (int)lane; d < far; d += 64)
+                if (d < from || d >= to) out[far + d] = 0.f;
+        }
+#pragma unroll
+        for (int x = 32; x > 0; x /= 2) {
+            sum_below += __shfl_xor(sum_below, x, 64);
+            sum_above += __shfl_xor(sum_above, x, 64);
+        }
+        if (writes && lane == 0) {
+            if (far == 0) out[0] = sum_below + sum_above;
+            else {
+                out[0] = sum_below;
+                out[2 * (size_t)far] = sum_above;
+            }
+        }
+    }
+
+    if (i >= a.Lq) return;
+    if (hi == 0) plan.delta[row] = dead ? 0.f : delta;
+    const float f = rl * a.scale;
+    char* const to = static_cast<char*>(a.dq) + (((size_t)n * a.Lq + i) * a.lddq + (size_t)head * D) * E;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = dead ? 0.f : dq[b][4 * q + e] * f;
+            seq_store4<T>(to, 32 * b + 8 * q + 4 * hi, x[0], x[1], x[2], x[3]);
+        }
+}
+
+// Half data: P and dS are taken 2^6 times as large and the sums divided again, since a probability of 2^-14 and less (keys by the
+// thousand) has fewer bits in that type; dS beyond 1023 overflows.
+template <class T>
+constexpr float seq_lift() { return __is_same(T, SeqF16) ? 6.f : 0.f; }
+
+template <class T, int D, int W, int QT>
+__global__ void __launch_bounds__(64 * W) seq_keys_kernel(SeqArgs a, BackPlan plan) {
+    constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, QS = QT / 32;
+    constexpr uint32_t kTile = QT * RB;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const uint32_t base = lds_offset(lds), stat_at = base + 4u * kTile, bias_at = stat_at + 2u * 12u * QT, bias_bytes = 4u * plan.bias_entries;
+    const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t hi = lane >> 5, c = lane & 31u;
+
+    uint32_t at = xcd_logical_block(blockIdx.x, plan.key_q, plan.key_r);
+    uint32_t rest = fastdiv(at, plan.by_splits);
+    const int split = (int)(at - rest * plan.by_splits.d);
+    at = rest;
+    rest = fastdiv(at, plan.by_key_blocks);
+    const int block = (int)(at - rest * plan.by_key_blocks.d);
+    const long long n = fastdiv(rest, plan.by_kv);
+    const int kv = (int)(rest - (uint32_t)n * plan.by_kv.d);
+    const int j0 = block * 32 * W, j = j0 + (int)(32u * wave + c), j_last = j0 + 32 * W - 1;
+    const int qlen = seq_length(a.q_len, n, a.Lq), klen = seq_length(a.k_len, n, a.Lk), start = seq_start(a.q_start, n);
+
+    // tiles of queries with a key of this block, and the heads that share it, one after the other
+    int q0 = 0;
+    if (a.causal && j0 > start) q0 = (j0 - start) / QT;
+    const int q1 = j0 < klen ? (qlen + QT - 1) / QT : 0, each = q1 > q0 ? q1 - q0 : 0, all = each * plan.group;
+    const int per = (all + plan.splits - 1) / plan.splits, s0 = split * per, s1 = s0 + per < all ? s0 + per : all;
+
+    const uint32_t qld = (uint32_t)(a.ldq * E), gld = (uint32_t)(a.ldg * E);
+    SeqLoader<RB, QT, W> load_q, load_g;
+    load_q.init(wave, lane, qld);
+    load_g.init(wave, lane, gld);
+    SeqRowReader<RB> row_reader;
+    row_reader.init(hi, c);
+    SeqColumnReader<T, D> column_reader;
+    column_reader.init(hi, c);
+
+    int g = 0, t = q0;  // of the tile that is loaded next
+    if (each > 0) {
+        g = s0 / each;
+        t = q0 + s0 - g * each;
+    }
+    auto issue = [&](uint32_t buf) {
+        const int head = kv * plan.group + g;
+        const size_t row = (size_t)n * a.Lq + (size_t)t * QT;
+        const uint32_t to = base + buf * 2u * kTile;
+        load_q.issue(static_cast<const char*>(a.q) + (row * a.ldq + (size_t)head * D) * E, qlen - t * QT, qld, to);
+        load_g.issue(static_cast<const char*>(a.d_o) + (row * a.ldg + (size_t)head * D) * E, qlen - t * QT, gld, to + kTile);
+    };
+
+    u32x4 kf[NC], vf[NC];
+#pragma unroll
+    for (int s = 0; s < NC; ++s) kf[s] = vf[s] = u32x4{0u, 0u, 0u, 0u};
+    if (j < klen) {
+        const size_t from = (((size_t)n * a.Lk + j) * a.ldk + (size_t)kv * D) * E + 16u * hi;
+        const char* const kp = static_cast<const char*>(a.k) + from;
+        const char* const vp = static_cast<const char*>(a.v) + from;
+#pragma unroll
+        for (int s = 0; s < NC; ++s) {
+            kf[s] = *reinterpret_cast<const u32x4*>(kp + 32 * s);
+            vf[s] = *reinterpret_cast<const u32x4*>(vp + 32 * s);
+        }
+    }
+    if (qlen % QT != 0 && s0 < s1) {
+        for (uint32_t o = threadIdx.x * 16u; o < 4u * kTile; o += 64u * W * 16u) *reinterpret_cast<u32x4*>(lds + o) = u32x4{0u, 0u, 0u, 0u};
+        __syncthreads();
+    }
+
+    f32x16 dk[NB], dv[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        seq_zero(dk[b]);
+        seq_zero(dv[b]);
+    }
+    const int far = a.far;
+    const float scale = a.scale * kLog2e;
+    if (s0 < s1) issue(0);
+    for (int s = s0; s < s1; ++s) {
+        const uint32_t buf = (uint32_t)(s - s0) & 1u, qt = base + buf * 2u * kTile, gt = qt + kTile, stat = stat_at + buf * (12u * QT);
+        const int head = kv * plan.group + g, i0 = t * QT, first = start + i0;
+        const float* const table = a.table ? a.table + (size_t)head * a.nb : nullptr;
+        const bool near = table && j0 - (first + QT - 1) < far && j_last - first > -far;
+        if (near)
+            for (uint32_t e = threadIdx.x; e < (uint32_t)(QT + 32 * W - 1); e += 64u * W)
+                seq_lds_put(bias_at + buf * bias_bytes + 4u * e, seq_bias_at(table, a.buckets, a.nb, far, j_last - first - (int)e));
+        for (uint32_t e = threadIdx.x; e < (uint32_t)QT; e += 64u * W) {
+            float ref = 0.f, l = kDead, delta = 0.f;
+            if (i0 + (int)e < qlen) {
+                const size_t row = ((size_t)n * a.H + head) * a.Lq + i0 + e;
+                const f32x2 x = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
+                if (x[0] != -__builtin_inff()) {
+                    ref = x[0];
+                    l = x[1] - seq_lift<T>();
+                    delta = plan.delta[row];
+                }
+            }
+            seq_lds_put(stat + 4u * e, ref);
+            seq_lds_put(stat + 4u * (QT + e), l);
+            seq_lds_put(stat + 4u * (2 * QT + e), delta);
+        }
+        if (++t == q1) {
+            t = q0;
+            ++g;
+        }
+        lds_loads_done();
+        __syncthreads();
+        if (s + 1 < s1) issue(buf ^ 1u);
+
+        const float far_bias = table && !near ? seq_bias_at(table, a.buckets, a.nb, far, j_last - first <= -far ? -far : far) : 0.f;
+        const bool masked = j_last >= klen || (a.causal && j_last > first);
+        const int from_row = j < klen ? (a.causal ? j - first : -(1 << 30)) : 1 << 30;  // rows from which on the lane's key is seen
+#pragma unroll
+        for (int k = 0; k < QS; ++k) {
+            f32x16 p, dp;
+            seq_zero(p);
+            seq_zero(dp);
+#pragma unroll
+            for (int x = 0; x < NC; ++x) p = seq_dot<T>(row_reader.read(qt, x, k), kf[x], p);
+#pragma unroll
+            for (int x = 0; x < NC; ++x) dp = seq_dot<T>(row_reader.read(gt, x, k), vf[x], dp);
+            if (near) {
+                const uint32_t my_bias = bias_at + buf * bias_bytes + 4u * ((uint32_t)(j_last - j) + 4u * hi);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) p[r] = fmaf(p[r], scale, seq_lds_f32(my_bias + 4u * (32 * k + 8 * (r / 4) + r % 4)));
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) p[r] = fmaf(p[r], scale, far_bias);
+            }
+            if (masked) {
+                const int room = from_row - 4 * (int)hi;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) p[r] = 32 * k + 8 * (r / 4) + r % 4 >= room ? p[r] : -__builtin_inff();
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t rows = stat + 4u * (32 * k + 8 * q) + 16u * hi;
+                const f32x4 ref = seq_lds_f32x4(rows), l = seq_lds_f32x4(rows + 4u * QT), delta = seq_lds_f32x4(rows + 8u * QT);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 4 * q + e;
+                    // the reference first: it cancels against the score however large a bias made both
+                    p[r] = __builtin_amdgcn_exp2f((p[r] - ref[e]) - l[e]);
+                    dp[r] = p[r] * (dp[r] - delta[e]);
+                }
+            }
+            column_reader.accumulate(dv, gt, k, p);
+            column_reader.accumulate(dk, qt, k, dp);
+        }
+    }
+
+    if (j >= a.Lk) return;
+    const float down = __builtin_amdgcn_exp2f(-seq_lift<T>());
+    const size_t row = (size_t)n * a.Lk + j;
+    if (plan.splits > 1) {
+        const size_t values = (size_t)a.N * a.Lk * a.KV * D, to = (row * a.KV + kv) * D;
+        float* const part = plan.part_kv + (size_t)split * 2 * values + to;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t ch = 32 * b + 8 * q + 4 * hi;
+                *reinterpret_cast<f32x4*>(part + ch) = f32x4{dk[b][4 * q], dk[b][4 * q + 1], dk[b][4 * q + 2], dk[b][4 * q + 3]};
+                *reinterpret_cast<f32x4*>(part + values + ch) = f32x4{dv[b][4 * q], dv[b][4 * q + 1], dv[b][4 * q + 2], dv[b][4 * q + 3]};
+            }
+        return;
+    }
+    const size_t to = (row * a.lddk + (size_t)kv * D) * E;
+    char* const dkp = static_cast<char*>(a.dk) + to;
+    char* const dvp = static_cast<char*>(a.dv) + to;
+    const float fk = a.scale * down;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t ch = 32 * b + 8 * q + 4 * hi;
+            seq_store4<T>(dkp, ch, dk[b][4 * q] * fk, dk[b][4 * q + 1] * fk, dk[b][4 * q + 2] * fk, dk[b][4 * q + 3] * fk);
+            seq_store4<T>(dvp, ch, dv[b][4 * q] * down, dv[b][4 * q + 1] * down, dv[b][4 * q + 2] * down, dv[b][4 * q + 3] * down);
+        }
+}
+
+// Joins the parts of dK and dV: a thread has four channels of a key of one of the two.
+template <class T, int D>
+__global__ void __launch_bounds__(256) seq_join_keys_kernel(SeqArgs a, BackPlan plan) {
+    constexpr int E = SeqSize<T>::value;
+    const size_t values = (size_t)a.N * a.Lk * a.KV * D, at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (at >= 2 * values) return;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < plan.splits; ++s) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(plan.part_kv + (size_t)s * 2 * values + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += x[e];
+    }
+    const bool is_dv = at >= values;
+    const size_t in = is_dv ? at - values : at, row = in / ((size_t)a.KV * D), channel = in - row * ((size_t)a.KV * D);
+    const float f = __builtin_amdgcn_exp2f(-seq_lift<T>()) * (is_dv ? 1.f : a.scale);
+    char* const to = static_cast<char*>(is_dv ? a.dv : a.dk) + row * a.lddk * E;
+    seq_store4<T>(to, (uint32_t)channel, sum[0] * f, sum[1] * f, sum[2] * f, sum[3] * f);
+}
+
+template <class Kernel>
+hipError_t start(Kernel* kernel, unsigned grid, int block, size_t lds, hipStream_t s, const SeqArgs& a, const BackPlan& plan) {
+    if (grid == 0) return hipSuccess;  // no queries, or no keys
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(block), lds, s, a, plan);
+    return hipGetLastError();
+}
+
+template <class T, int D, int W>
+hipError_t launch(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
+    constexpr int KT = seq_forward_keys(D * SeqSize<T>::value, W);
+    const size_t tiles = 4 * (size_t)KT * D * SeqSize<T>::value, bias = 2 * sizeof(float) * plan.bias_entries;
+    hipError_t e = a.dtable ? start(&seq_rows_kernel<T, D, W, KT, true>, plan.row_grid, 64 * W, tiles + bias + W * 8 * (KT + 32), s, a, plan)
+                            : start(&seq_rows_kernel<T, D, W, KT, false>, plan.row_grid, 64 * W, tiles + bias, s, a, plan);
+    if (e != hipSuccess) return e;
+    if (a.dtable) {
+        e = launch_bucket_sums(plan.parts, plan.lines, a.buckets, a.dtable, a.H, a.nb, a.far, a.N * plan.row_waves, s);
+        if (e != hipSuccess) return e;
+    }
+    e = start(&seq_keys_kernel<T, D, W, KT>, plan.key_grid, 64 * W, tiles + 24 * KT + bias, s, a, plan);
+    if (e != hipSuccess || plan.splits == 1 || a.Lk == 0) return e;
+    const size_t threads = (size_t)a.N * a.Lk * a.KV * D / 2, blocks = (threads + 255) / 256;
+    hipLaunchKernelGGL((seq_join_keys_kernel<T, D>), dim3((unsigned)blocks), dim3(256), 0, s, a, plan);
+    return hipGetLastError();
+}
+template <class T>
+hipError_t launch(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
+    if (plan.waves == 1) {
+        if (a.D == 32) return launch<T, 32, 1>(a, plan, s);
+        if (a.D == 64) return launch<T, 64, 1>(a, plan, s);
+        return launch<T, 128, 1>(a, plan, s);
+    }
+    if (a.D == 32) return launch<T, 32, 4>(a, plan, s);
+    if (a.D == 64) return launch<T, 64, 4>(a, plan, s);
+    return launch<T, 128, 4>(a, plan, s);
+}
+
+bool back_plan(const SeqArgs& a, BackPlan& p) {
+    const int cus = cu_count();
+    p.group = a.H / a.KV;
+    p.waves = a.Lq <= 32 && a.Lk <= 32 ? 1 : 4;
+    const int KT = seq_forward_keys(a.D * (a.dtype == 0 ? 4 : 2), p.waves), block = 32 * p.waves;
+    p.row_blocks = (a.Lq + block - 1) / block;
+    p.key_blocks = (a.Lk + block - 1) / block;
+    p.row_waves = (a.Lq + 31) / 32;
+    const double rows = (double)a.N * a.H * p.row_blocks, keys = (double)a.N * a.KV * p.key_blocks;
+    // Too few blocks of keys for the device: their queries are shared out, no more than leaves each two tiles.
+    const long long all = (long long)((a.Lq + KT - 1) / KT) * p.group;
+    long long splits = (long long)(2.0 * cus / (keys > 1 ? keys : 1));
+    if (splits > all / 2) splits = all / 2;
+    if (splits > 16) splits = 16;
+    p.splits = splits < 1 ? 1 : (int)splits;
+    if (rows * 64 * p.waves > 4.0e9 || keys * p.splits * 64 * p.waves > 4.0e9) return false;
+    p.row_grid = (unsigned)rows;
+    p.key_grid = (unsigned)((long long)keys * p.splits);
+    p.row_q = p.row_grid / 8u;
+    p.row_r = p.row_grid % 8u;
+    p.key_q = p.key_grid / 8u;
+    p.key_r = p.key_grid % 8u;
+    p.by_row_blocks = make_fastdiv((uint32_t)(p.row_blocks > 0 ? p.row_blocks : 1));
+    p.by_heads = make_fastdiv((uint32_t)a.H);
+    p.by_key_blocks = make_fastdiv((uint32_t)(p.key_blocks > 0 ? p.key_blocks : 1));
+    p.by_splits = make_fastdiv((uint32_t)p.splits);
+    p.by_kv = make_fastdiv((uint32_t)a.KV);
+    p.bias_entries = a.table ? (uint32_t)(KT + block - 1) : 0u;
+    return true;
+}
+
+size_t padded(size_t floats) { return (floats * sizeof(float) + 255) & ~(size_t)255; }
+
+}  // namespace
+
+// workspace: delta, the parts of dK and dV, the sums of dS by distance
+size_t seq_backward_workspace(const SeqArgs& a, bool want_dtable) {
+    BackPlan p;
+    if (!back_plan(a, p)) return 0;
+    size_t bytes = padded((size_t)a.N * a.H * a.Lq);
+    if (p.splits > 1) bytes += padded((size_t)p.splits * 2 * a.N * a.Lk * a.KV * a.D);
+    if (want_dtable) {
+        const long long count = a.N * p.row_waves;
+        bytes += padded((size_t)a.H * count * (2 * (size_t)a.far + 1)) + bucket_lines_bytes(a.H, a.far, count);
+    }
+    return bytes;
+}
+
+hipError_t launch_sequence_backward(const SeqArgs& a, void* workspace, hipStream_t s) {
+    BackPlan p;
+    if (!back_plan(a, p)) return hipErrorInvalidValue;
+    char* ws = static_cast<char*>(workspace);
+    p.delta = reinterpret_cast<float*>(ws);
+    ws += padded((size_t)a.N * a.H * a.Lq);
+    p.part_kv = reinterpret_cast<float*>(ws);
+    if (p.splits > 1) ws += padded((size_t)p.splits * 2 * a.N * a.Lk * a.KV * a.D);
+    p.parts = reinterpret_cast<float*>(ws);
+    if (a.dtable) ws += padded((size_t)a.H * a.N * p.row_waves * (2 * (size_t)a.far + 1));
+    p.lines = reinterpret_cast<float*>(ws);
+    if (a.dtype == 0) return launch<SeqF32>(a, p, s);
+    return a.dtype == 1 ? launch<SeqBf16>(a, p, s) : launch<SeqF16>(a, p, s);
+}
+
+}  // namespace fwa

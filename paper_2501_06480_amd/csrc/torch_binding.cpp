@@ -290,6 +290,220 @@ py::object bias_scatter(const at::Tensor& dbias, int k, std::optional<uintptr_t>
     return rc == FWA_OK ? py::cast(dtable) : py::cast(rc);
 }
 
+// ------------------------------------------------------------------ bias by buckets, attention of whole sequences
+
+void need_same_device(const at::Tensor& t, const char* name, const at::Tensor& like) {
+    need_gpu(t, name);
+    if (t.device() != like.device()) value_error(std::string(name) + " must be on the device of the other tensors");
+}
+
+// The map from distances to columns: contiguous int32 [2 far + 1]
+struct Buckets {
+    const int32_t* p;
+    int far;
+};
+Buckets buckets_of(const at::Tensor& t, const at::Tensor& like) {
+    need_same_device(t, "buckets", like);
+    if (t.scalar_type() != at::kInt || t.dim() != 1 || t.size(0) % 2 != 1 || !t.is_contiguous())
+        value_error("buckets must be a contiguous int32 tensor [2 far + 1]");
+    if (t.size(0) > 0x7fffffff) value_error("buckets is too long");
+    return {t.data_ptr<int32_t>(), (int)(t.size(0) / 2)};
+}
+int to_int(int64_t x, const char* name) {
+    if (x < -0x7fffffff || x > 0x7fffffff) value_error(std::string(name) + " is out of range");
+    return (int)x;
+}
+
+int run_bucket_gather(at::Tensor& bias, const at::Tensor& table, const at::Tensor& buckets, int64_t Lq, int64_t Lk, int64_t q_start, bool bf16,
+                      const OptTensor& out, std::optional<uintptr_t> stream) {
+    if (table.dim() != 2) value_error("table must be [heads, columns]");
+    if (Lq < 0 || Lk < 0) value_error("Lq and Lk must not be negative");
+    const float* const src = static_cast<const float*>(dense_ptr(table, "table", true));
+    const Buckets b = buckets_of(buckets, table);
+    const at::ScalarType type = bf16 ? at::kBFloat16 : at::kFloat;
+    if (out) {
+        need_same_device(*out, "out", table);
+        if (out->dim() != 3 || out->size(0) != table.size(0) || out->size(1) != Lq || out->size(2) != Lk || out->scalar_type() != type || !out->is_contiguous())
+            value_error("out must be a contiguous [heads, Lq, Lk] tensor of the type asked for");
+    }
+    bias = out ? *out : at::empty({table.size(0), Lq, Lk}, table.options().dtype(type));
+    void* const dst = bias.data_ptr();
+    void* const st = stream_of(stream, table);
+    const c10::DeviceGuard guard(table.device());
+    const Nogil nogil;
+    return fwa_bucket_gather(src, b.p, dst, to_int(table.size(0), "heads"), to_int(table.size(1), "columns"), b.far, to_int(Lq, "Lq"), to_int(Lk, "Lk"), q_start,
+                             bf16 ? FWA_BF16 : FWA_F32, st);
+}
+py::object bucket_gather(const at::Tensor& table, const at::Tensor& buckets, int64_t Lq, int64_t Lk, int64_t q_start, bool bf16, const OptTensor& out,
+                         std::optional<uintptr_t> stream) {
+    at::Tensor bias;
+    const int rc = run_bucket_gather(bias, table, buckets, Lq, Lk, q_start, bf16, out, stream);
+    return rc == FWA_OK ? py::cast(bias) : py::cast(rc);
+}
+
+int run_bucket_scatter(at::Tensor& dtable, const at::Tensor& dbias, const at::Tensor& buckets, int64_t columns, int64_t q_start, const OptTensor& workspace,
+                       std::optional<uintptr_t> stream) {
+    if (dbias.dim() != 3) value_error("dbias must be [heads, Lq, Lk]");
+    if (columns < 1) value_error("columns must be positive");
+    const float* const src = static_cast<const float*>(dense_ptr(dbias, "dbias", true));
+    const Buckets b = buckets_of(buckets, dbias);
+    const int heads = to_int(dbias.size(0), "heads"), Lq = to_int(dbias.size(1), "Lq"), Lk = to_int(dbias.size(2), "Lk"), nb = to_int(columns, "columns");
+    dtable = at::empty({dbias.size(0), columns}, dbias.options());
+    const size_t need = fwa_bucket_scatter_workspace_bytes(heads, nb, b.far, Lq, Lk);
+    if (workspace) need_same_device(*workspace, "workspace", dbias);
+    const at::Tensor ws = workspace ? *workspace : need ? at::empty({(int64_t)need}, dbias.options().dtype(at::kByte)) : at::Tensor();
+    float* const dst = dtable.data_ptr<float>();
+    void* const wp = ws.defined() ? ws.data_ptr() : nullptr;
+    const size_t wb = ws.defined() ? (size_t)ws.nbytes() : 0;
+    void* const st = stream_of(stream, dbias);
+    const c10::DeviceGuard guard(dbias.device());
+    const Nogil nogil;
+    return fwa_bucket_scatter(src, b.p, dst, heads, nb, b.far, Lq, Lk, q_start, wp, wb, st);
+}
+py::object bucket_scatter(const at::Tensor& dbias, const at::Tensor& buckets, int64_t columns, int64_t q_start, const OptTensor& workspace,
+                          std::optional<uintptr_t> stream) {
+    at::Tensor dtable;
+    const int rc = run_bucket_scatter(dtable, dbias, buckets, columns, q_start, workspace, stream);
+    return rc == FWA_OK ? py::cast(dtable) : py::cast(rc);
+}
+
+// What the calls of a sequence attention have in common, besides the tensors of their directions.
+struct Sequence {
+    int64_t N, Lq, Lk;
+    int heads, kv_heads, d, dtype;
+    float scale;
+    const float* table = nullptr;
+    const int32_t* buckets = nullptr;
+    int columns = 0, far = 0;
+    const int32_t *q_lengths = nullptr, *k_lengths = nullptr, *q_start = nullptr;
+    int causal;
+};
+const int32_t* per_sequence(const OptTensor& t, const char* name, const at::Tensor& q) {
+    if (!t) return nullptr;
+    need_same_device(*t, name, q);
+    if (t->scalar_type() != at::kInt || t->dim() != 1 || t->size(0) != q.size(0) || !t->is_contiguous())
+        value_error(std::string(name) + " must be a contiguous int32 tensor [N]");
+    return t->data_ptr<int32_t>();
+}
+Sequence sequence_of(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, int64_t heads, double scale, const OptTensor& table, const OptTensor& buckets,
+                     const OptTensor& q_lengths, const OptTensor& k_lengths, const OptTensor& q_start, bool causal) {
+    need_gpu(q, "q");
+    if (q.dim() != 3) value_error("q must be [N, Lq, heads * d]");
+    if (heads < 1 || q.size(2) % heads != 0 || q.size(2) == 0) value_error("the channels of q must be a multiple of heads");
+    Sequence s;
+    s.N = q.size(0);
+    s.Lq = to_int(q.size(1), "Lq");
+    s.heads = to_int(heads, "heads");
+    s.d = to_int(q.size(2) / heads, "d");
+    for (const auto& t : {std::make_pair(&k, "k"), std::make_pair(&v, "v")}) {
+        need_same_device(*t.first, t.second, q);
+        if (t.first->dim() != 3 || t.first->size(0) != s.N || t.first->scalar_type() != q.scalar_type())
+            value_error(std::string(t.second) + " must be [N, Lk, kv_heads * d] of the type of q");
+    }
+    if (v.sizes() != k.sizes()) value_error("k and v must have one shape");
+    if (k.size(2) == 0 || k.size(2) % s.d != 0 || heads % (k.size(2) / s.d) != 0) value_error("the channels of k must be kv_heads * d, kv_heads a divisor of heads");
+    s.Lk = to_int(k.size(1), "Lk");
+    s.kv_heads = (int)(k.size(2) / s.d);
+    s.dtype = dtype_code(q);
+    s.scale = (float)scale;
+    s.causal = causal;
+    if (table.has_value() != buckets.has_value()) value_error("table and buckets go together");
+    if (table) {
+        if (table->dim() != 2 || table->size(0) != heads) value_error("table must be [heads, columns]");
+        s.table = static_cast<const float*>(dense_ptr(*table, "table", true));
+        need_same_device(*table, "table", q);
+        const Buckets b = buckets_of(*buckets, q);
+        s.buckets = b.p;
+        s.far = b.far;
+        s.columns = to_int(table->size(1), "columns");
+    }
+    s.q_lengths = per_sequence(q_lengths, "q_lengths", q);
+    s.k_lengths = per_sequence(k_lengths, "k_lengths", q);
+    s.q_start = per_sequence(q_start, "q_start", q);
+    return s;
+}
+at::Tensor scratch(size_t bytes, const at::Tensor& like) {
+    return bytes ? at::empty({(int64_t)bytes}, like.options().dtype(at::kByte)) : at::Tensor();
+}
+void need_one_stride(const Rows& k, const Rows& v, const char* names, int64_t N, int64_t L) {
+    if (k.ld != v.ld && N * L > 1) value_error(std::string(names) + " must share one row stride");
+}
+
+int run_sequence_forward(at::Tensor& o, at::Tensor& stats, bool want_stats, const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, int64_t heads, double scale,
+                         const OptTensor& table, const OptTensor& buckets, const OptTensor& q_lengths, const OptTensor& k_lengths, const OptTensor& q_start,
+                         bool causal, const OptTensor& out, const OptTensor& workspace, std::optional<uintptr_t> stream) {
+    const Sequence s = sequence_of(q, k, v, heads, scale, table, buckets, q_lengths, k_lengths, q_start, causal);
+    o = out ? *out : at::empty(q.sizes(), q.options());
+    if (want_stats) stats = at::empty({s.N, heads, s.Lq, 2}, q.options().dtype(at::kFloat));
+    const Rows rq = rows_of(q, "q", nullptr), rk = rows_of(k, "k", nullptr), rv = rows_of(v, "v", nullptr), ro = rows_of(o, "out", &q);
+    need_one_stride(rk, rv, "k and v", s.N, s.Lk);
+    if (workspace) need_same_device(*workspace, "workspace", q);
+    const at::Tensor ws = workspace ? *workspace
+                                    : scratch(fwa_sequence_forward_workspace_bytes(s.N, (int)s.Lq, (int)s.Lk, s.heads, s.kv_heads, s.d, s.dtype), q);
+    float* const sp = stats.defined() ? stats.data_ptr<float>() : nullptr;
+    void* const wp = ws.defined() ? ws.data_ptr() : nullptr;
+    const size_t wb = ws.defined() ? (size_t)ws.nbytes() : 0;
+    void* const st = stream_of(stream, q);
+    const c10::DeviceGuard guard(q.device());
+    const Nogil nogil;
+    return fwa_sequence_forward(rq.p, rk.p, rv.p, ro.p, sp, s.N, (int)s.Lq, (int)s.Lk, s.heads, s.kv_heads, s.d, s.scale, rq.ld, rk.ld, ro.ld, s.table, s.buckets,
+                                s.columns, s.far, s.q_lengths, s.k_lengths, s.q_start, s.causal, s.dtype, wp, wb, st);
+}
+py::object sequence_forward(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, int64_t heads, double scale, const OptTensor& table,
+                            const OptTensor& buckets, const OptTensor& q_lengths, const OptTensor& k_lengths, const OptTensor& q_start, bool causal,
+                            bool want_stats, const OptTensor& out, const OptTensor& workspace, std::optional<uintptr_t> stream) {
+    at::Tensor o, stats;
+    const int rc = run_sequence_forward(o, stats, want_stats, q, k, v, heads, scale, table, buckets, q_lengths, k_lengths, q_start, causal, out, workspace, stream);
+    if (rc != FWA_OK) return py::cast(rc);
+    if (want_stats) return py::make_tuple(o, stats);
+    return py::cast(o);
+}
+
+int run_sequence_backward(Grads& d, const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, const at::Tensor& o, const at::Tensor& stats, const at::Tensor& d_o,
+                          int64_t heads, double scale, const OptTensor& table, const OptTensor& buckets, const OptTensor& q_lengths, const OptTensor& k_lengths,
+                          const OptTensor& q_start, bool causal, bool want_dtable, const OptTensor& dq_out, const OptTensor& dk_out, const OptTensor& dv_out,
+                          const OptTensor& workspace, std::optional<uintptr_t> stream) {
+    const Sequence s = sequence_of(q, k, v, heads, scale, table, buckets, q_lengths, k_lengths, q_start, causal);
+    if (want_dtable && !table) value_error("the gradient of a table needs the table");
+    need_same_device(stats, "stats", q);
+    if (stats.scalar_type() != at::kFloat || stats.dim() != 4 || stats.size(0) != s.N || stats.size(1) != heads || stats.size(2) != s.Lq || stats.size(3) != 2 ||
+        !stats.is_contiguous())
+        value_error("stats must be the contiguous float32 tensor [N, heads, Lq, 2] of the forward");
+    d.q = dq_out ? *dq_out : at::empty(q.sizes(), q.options());
+    d.k = dk_out ? *dk_out : at::empty(k.sizes(), k.options());
+    d.v = dv_out ? *dv_out : at::empty(v.sizes(), v.options());
+    if (want_dtable) d.bias = at::empty({heads, (int64_t)s.columns}, q.options().dtype(at::kFloat));
+    const Rows rq = rows_of(q, "q", nullptr), rk = rows_of(k, "k", nullptr), rv = rows_of(v, "v", nullptr), ro = rows_of(o, "o", &q), rg = rows_of(d_o, "d_o", &q);
+    const Rows rdq = rows_of(d.q, "dq", &q), rdk = rows_of(d.k, "dk", nullptr), rdv = rows_of(d.v, "dv", nullptr);
+    for (const auto& t : {std::make_pair(&d.k, "dk"), std::make_pair(&d.v, "dv")})
+        if (t.first->sizes() != k.sizes() || t.first->scalar_type() != k.scalar_type() || t.first->device() != k.device())
+            value_error(std::string(t.second) + " must match k in shape, dtype and device");
+    need_one_stride(rk, rv, "k and v", s.N, s.Lk);
+    need_one_stride(rdk, rdv, "dk and dv", s.N, s.Lk);
+    if (workspace) need_same_device(*workspace, "workspace", q);
+    const at::Tensor ws = workspace ? *workspace
+                                    : scratch(fwa_sequence_backward_workspace_bytes(s.N, (int)s.Lq, (int)s.Lk, s.heads, s.kv_heads, s.d, s.far, s.dtype, want_dtable), q);
+    float* const dt = d.bias.defined() ? d.bias.data_ptr<float>() : nullptr;
+    const float* const sp = stats.data_ptr<float>();
+    void* const wp = ws.defined() ? ws.data_ptr() : nullptr;
+    const size_t wb = ws.defined() ? (size_t)ws.nbytes() : 0;
+    void* const st = stream_of(stream, q);
+    const c10::DeviceGuard guard(q.device());
+    const Nogil nogil;
+    return fwa_sequence_backward(rq.p, rk.p, rv.p, ro.p, rg.p, sp, rdq.p, rdk.p, rdv.p, dt, s.N, (int)s.Lq, (int)s.Lk, s.heads, s.kv_heads, s.d, s.scale, rq.ld, rk.ld,
+                                 ro.ld, rg.ld, rdq.ld, rdk.ld, s.table, s.buckets, s.columns, s.far, s.q_lengths, s.k_lengths, s.q_start, s.causal, s.dtype, wp, wb, st);
+}
+py::object sequence_backward(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, const at::Tensor& o, const at::Tensor& stats, const at::Tensor& d_o,
+                             int64_t heads, double scale, const OptTensor& table, const OptTensor& buckets, const OptTensor& q_lengths, const OptTensor& k_lengths,
+                             const OptTensor& q_start, bool causal, bool want_dtable, const OptTensor& dq_out, const OptTensor& dk_out, const OptTensor& dv_out,
+                             const OptTensor& workspace, std::optional<uintptr_t> stream) {
+    Grads d;
+    const int rc = run_sequence_backward(d, q, k, v, o, stats, d_o, heads, scale, table, buckets, q_lengths, k_lengths, q_start, causal, want_dtable, dq_out, dk_out,
+                                         dv_out, workspace, stream);
+    if (rc != FWA_OK) return py::cast(rc);
+    return py::make_tuple(d.q, d.k, d.v, or_none(d.bias));
+}
+
 // ------------------------------------------------------------------ autograd
 // The two differentiable calls as native nodes.  What they save goes through the engine's saved variables (version counters,
 // saved-tensor hooks); an error in the backward reaches Python as the exception that the direct call raises.
@@ -394,6 +608,61 @@ at::Tensor attention_qkv(const at::Tensor& qkv, double scale, const OptTensor& b
     return AttentionQKV::apply(qkv, bias, mask, labels, scale, mask_value);
 }
 
+struct BucketBias : torch::autograd::Function<BucketBias> {
+    static at::Tensor forward(AutogradContext* ctx, const at::Tensor& table, const at::Tensor& buckets, int64_t Lq, int64_t Lk, int64_t q_start, bool bf16) {
+        ctx->save_for_backward({buckets});
+        ctx->saved_data["columns"] = table.dim() == 2 ? table.size(1) : 0;
+        ctx->saved_data["q_start"] = q_start;
+        at::Tensor bias;
+        const int rc = run_bucket_gather(bias, table, buckets, Lq, Lk, q_start, bf16, std::nullopt, std::nullopt);
+        if (rc != FWA_OK) raise_status(rc, "fwa_bucket_gather");
+        return bias;
+    }
+    static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
+        return with_python_errors([&]() -> variable_list {
+            const variable_list s = ctx->get_saved_variables();
+            at::Tensor dtable;
+            const int rc = run_bucket_scatter(dtable, grads[0].to(at::kFloat).contiguous(), s[0].contiguous(), ctx->saved_data["columns"].toInt(),
+                                              ctx->saved_data["q_start"].toInt(), std::nullopt, std::nullopt);
+            if (rc != FWA_OK) raise_status(rc, "fwa_bucket_scatter");
+            return {dtable, at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()};
+        });
+    }
+};
+struct SequenceAttention : torch::autograd::Function<SequenceAttention> {
+    static at::Tensor forward(AutogradContext* ctx, const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, const OptTensor& table, const OptTensor& buckets,
+                              const OptTensor& q_lengths, const OptTensor& k_lengths, const OptTensor& q_start, int64_t heads, double scale, bool causal) {
+        at::Tensor o, stats;
+        const int rc = run_sequence_forward(o, stats, true, q, k, v, heads, scale, table, buckets, q_lengths, k_lengths, q_start, causal, std::nullopt, std::nullopt,
+                                            std::nullopt);
+        if (rc != FWA_OK) raise_status(rc, "fwa_sequence_forward");
+        ctx->save_for_backward({q, k, v, o, stats, or_undefined(table), or_undefined(buckets), or_undefined(q_lengths), or_undefined(k_lengths), or_undefined(q_start)});
+        ctx->saved_data["heads"] = heads;
+        ctx->saved_data["scale"] = scale;
+        ctx->saved_data["causal"] = causal;
+        return o;
+    }
+    static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
+        return with_python_errors([&]() -> variable_list {
+            const variable_list s = ctx->get_saved_variables();
+            Grads d;
+            const int rc = run_sequence_backward(d, s[0], s[1], s[2], s[3], s[4], grads[0].contiguous(), ctx->saved_data["heads"].toInt(),
+                                                 ctx->saved_data["scale"].toDouble(), opt(s[5]), opt(s[6]), opt(s[7]), opt(s[8]), opt(s[9]),
+                                                 ctx->saved_data["causal"].toBool(), s[5].defined() && ctx->needs_input_grad(3), std::nullopt, std::nullopt,
+                                                 std::nullopt, std::nullopt, std::nullopt);
+            if (rc != FWA_OK) raise_status(rc, "fwa_sequence_backward");
+            return {d.q, d.k, d.v, d.bias, at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()};
+        });
+    }
+};
+at::Tensor bucket_bias(const at::Tensor& table, const at::Tensor& buckets, int64_t Lq, int64_t Lk, int64_t q_start, bool bf16) {
+    return BucketBias::apply(table, buckets, Lq, Lk, q_start, bf16);
+}
+at::Tensor sequence_attention(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, int64_t heads, double scale, const OptTensor& table,
+                              const OptTensor& buckets, const OptTensor& q_lengths, const OptTensor& k_lengths, const OptTensor& q_start, bool causal) {
+    return SequenceAttention::apply(q, k, v, table, buckets, q_lengths, k_lengths, q_start, heads, scale, causal);
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_fwa_torch, m) {
@@ -405,4 +674,10 @@ PYBIND11_MODULE(_fwa_torch, m) {
     m.def("attention_qkv", torch::wrap_pybind_function(&attention_qkv));
     m.def("bias_gather", &bias_gather);
     m.def("bias_scatter", &bias_scatter);
+    m.def("bucket_gather", &bucket_gather);
+    m.def("bucket_scatter", &bucket_scatter);
+    m.def("sequence_forward", &sequence_forward);
+    m.def("sequence_backward", &sequence_backward);
+    m.def("bucket_bias", torch::wrap_pybind_function(&bucket_bias));
+    m.def("sequence_attention", torch::wrap_pybind_function(&sequence_attention));
 }
