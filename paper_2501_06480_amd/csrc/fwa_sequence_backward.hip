@@ -17,20 +17,32 @@ struct BackPlan {
     FastDiv by_row_blocks, by_heads, by_key_blocks, by_splits, by_kv;
     int row_waves;       // waves with rows per head of a sequence: ceil(Lq / 32)
     float* delta;        // [N, H, Lq]
-    float* parts;        // [H][N * row_waves][2 far + 1] sums of dS by distance
-    float* lines;
+    float* ends;         // [H][N * row_waves][2]: sums of dS at and beyond -far and far
+    float* lines;        // [H][2 far + 1]: sums of dS by distance
+    float* parts;        // [H][offsets][chunks][kLine]: the same of an offset of blocks
+    int low_offset, offsets, chunks, items;
+    FastDiv by_offsets, by_chunks, by_table_blocks;
     float* part_kv;      // [splits][2][N, Lk, KV, D]
 };
 
 constexpr float kDead = __builtin_inff();
+// Rows that see few keys: one of these may have nearly all the weight, dP - delta cancels, and the rounding of o would show.  There a walk in
+// front of the other forms delta from the same products as dP.  (The rows of a causal call that see up to two tiles are a block.)
+constexpr int kFewTiles = 2;
+enum { kInner, kBelow, kAbove, kBorder };  // where the distances of a tile lie against -far and far
 
+// a sum that is not fused with a product it takes in: the two forms of the rows kernel give the same bits
+__device__ __forceinline__ float plain_sum(float a, float b) {
+#pragma clang fp contract(off)
+    return a + b;
+}
 // the weight of a score in base-2 units, against the reference of its row
 __device__ __forceinline__ float weight(float s, float ref) { return __builtin_amdgcn_exp2f(s - ref); }
 
 template <class T, int D, int W, int KT, bool TABLE>
 __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan plan) {
     constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, KS = KT / 32;
-    constexpr uint32_t kTile = KT * RB, kLine = KT + 32;
+    constexpr uint32_t kTile = KT * RB;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t base = lds_offset(lds), bias_at = base + 4u * kTile, bias_bytes = 4u * plan.bias_entries;
     const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -159,119 +171,76 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
     for (int b = 0; b < NB; ++b) seq_zero(dq[b]);
     float ds_all = 0.f, ds_below = 0.f, ds_above = 0.f, p_below = 0.f, p_above = 0.f;
     if (tiles > 0) issue(0, 0);
-    for (int t = 0; t < tiles; ++t) {
-        const uint32_t buf = (uint32_t)t & 1u;
-        begin(t, buf, t + 1 < tiles);
-        f32x16 p, dp;
-        if (tiles == 1) {
-            // few keys, of which one may have all the weight: delta from the same products as dP, so that what cancels does so exactly
-            float sum = 0.f;
+    if (tiles > 0 && tiles <= kFewTiles) {
+        float sum = 0.f;
+        for (int t = 0; t < tiles; ++t) {
+            const uint32_t buf = (uint32_t)t & 1u;
+            begin(t, buf, t + 1 < tiles);
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
+                f32x16 p, dp;
                 scores(t, buf, k, p, dp);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) sum = fmaf(p[r], dp[r], sum);
             }
-            delta = rl * seq_sum_halves(sum);
         }
+        delta = rl * seq_sum_halves(sum);
+        __syncthreads();
+        issue(0, 0);
+    }
+    for (int t = 0; t < tiles; ++t) {
+        const uint32_t buf = (uint32_t)t & 1u;
+        begin(t, buf, t + 1 < tiles);
+        f32x16 p, dp;
         float ds_tile = 0.f, p_tile = 0.f;
-        const bool near = is_near(t);
+        const int nearest = t * KT - last, furthest = t * KT + KT - 1 - first;  // distances of the tile
+        const int kind = furthest <= -far ? kBelow : nearest >= far ? kAbove : nearest > -far && furthest < far ? kInner : kBorder;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             scores(t, buf, k, p, dp);
 #pragma unroll
             for (int r = 0; r < 16; ++r) dp[r] = p[r] * (dp[r] - delta);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) ds_tile += dp[r];
+            for (int r = 0; r < 16; ++r) ds_tile = plain_sum(ds_tile, dp[r]);
             if constexpr (TABLE) {
-                if (!near)
+                if (kind == kBelow || kind == kAbove) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) p_tile += p[r];
+                } else if (kind == kBorder) {
+                    const int d = t * KT + 4 * (int)hi - pos;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int x = d + 32 * k + 8 * (r / 4) + r % 4;
+                        if (x <= -far) { ds_below += dp[r]; p_below += p[r]; }
+                        else if (x >= far) { ds_above += dp[r]; p_above += p[r]; }
+                    }
+                }
             }
             column_reader.accumulate(dq, base + buf * 2u * kTile, k, dp);
         }
-        ds_all += ds_tile;
+        ds_all = plain_sum(ds_all, ds_tile);
         if constexpr (TABLE) {
-            if (!near && t * KT + KT - 1 - first <= -far) { ds_below += ds_tile; p_below += p_tile; }
-            else if (!near) { ds_above += ds_tile; p_above += p_tile; }
+            if (kind == kBelow) { ds_below += ds_tile; p_below += p_tile; }
+            else if (kind == kAbove) { ds_above += ds_tile; p_above += p_tile; }
         }
     }
     // The dS of a row add up to zero; what they add up to is what delta is off by, times the row's weights.  dQ of 16-bit data keeps
     // it (it is below the roundings of dS); dK and the sums by distance, which are not rounded, get the better delta.
     const float off = rl * seq_sum_halves(ds_all);
-    delta += off;
+    delta = plain_sum(delta, off);
 
     if constexpr (TABLE) {
-        float sum_below = rl * (ds_below - off * p_below), sum_above = rl * (ds_above - off * p_above);
-        // sums by distance where the distances tell
-        int t0 = first - far - KT + 1, t1 = (far + last + KT - 1);
-        t0 = t0 < 0 ? 0 : t0 / KT + 1;
-        t1 = t1 < 0 ? 0 : t1 / KT;
-        if (t1 > tiles) t1 = tiles;
-        const uint32_t line_at = bias_at + 2u * bias_bytes + wave * (8u * kLine), mine = line_at + 4u * kLine * hi;
-        const int wave_last = first + 32 * (int)wave + 31;
-        const bool writes = i0 + 32 * (int)wave < a.Lq;
-        const size_t width = 2 * (size_t)far + 1;
-        float* const out = plan.parts + (((size_t)head * a.N + n) * plan.row_waves + (block * W + (int)wave)) * width;
-        // entry e of the two lines, one for each half of the wave: distance e + t KT - wave_last
-        for (uint32_t e = lane; e < 2u * kLine; e += 64u) seq_lds_put(line_at + 4u * e, 0.f);
-        auto flush = [&](int from, int count) {
-            if ((int)lane < count) {
-                const float x = seq_lds_f32(line_at + 4u * lane) + seq_lds_f32(line_at + 4u * (kLine + lane));
-                const int d = from + (int)lane;
-                if (d <= -far) sum_below += x;
-                else if (d >= far) sum_above += x;
-                else if (writes) out[far + d] = x;
-            }
-        };
-        __syncthreads();  // the tiles of the first walk have been read by all waves
-        if (t0 < t1) issue(t0, 0);
-        for (int t = t0; t < t1; ++t) {
-            const uint32_t buf = (uint32_t)(t - t0) & 1u;
-            begin(t, buf, t + 1 < t1);
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                f32x16 p, dp;
-                scores(t, buf, k, p, dp);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float x = rl * p[r] * (dp[r] - delta);
-                    // lanes of a half have places of their own, and a wave's additions are made in its order
-                    __hip_atomic_fetch_add((__attribute__((address_space(3))) float*)(uintptr_t)(mine + 4u * (31u - c + 4u * hi) + 4u * (32 * k + 8 * (r / 4) + r % 4)), x,
-                                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                }
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-            flush(t * KT - wave_last, KT);
-            const float x = seq_lds_f32(mine + 4u * (KT + c));
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-            seq_lds_put(mine + 4u * c, x);
-#pragma unroll
-            for (int k = 1; k <= KS; ++k) seq_lds_put(mine + 4u * (32 * k + c), 0.f);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-        }
-        int from = 1 << 30, to = 1 << 30;
-        if (t0 < t1) {
-            flush(t1 * KT - wave_last, 31);
-            from = t0 * KT - wave_last;
-            to = t1 * KT - wave_last + 31;
-        }
-        if (writes) {
-            for (int d = 1 - far + (int)lane; d < far; d += 64)
-                if (d < from || d >= to) out[far + d] = 0.f;
-        }
+        // Pairs at or beyond far in either direction, all in one column of the table each: their sums, of the wave's rows.  The others are
+        // added up by distance in seq_table_kernel, with the delta that is known now.
+        float sum_below = dead ? 0.f : rl * (ds_below - off * p_below), sum_above = dead ? 0.f : rl * (ds_above - off * p_above);
 #pragma unroll
         for (int x = 32; x > 0; x /= 2) {
             sum_below += __shfl_xor(sum_below, x, 64);
             sum_above += __shfl_xor(sum_above, x, 64);
         }
-        if (writes && lane == 0) {
-            if (far == 0) out[0] = sum_below + sum_above;
-            else {
-                out[0] = sum_below;
-                out[2 * (size_t)far] = sum_above;
-            }
-        }
+        const int rw = block * W + (int)wave;
+        if (lane == 0 && rw < plan.row_waves)
+            *reinterpret_cast<f32x2*>(plan.ends + 2 * (((size_t)head * a.N + n) * plan.row_waves + rw)) = f32x2{sum_below, sum_above};
     }
 
     if (i >= a.Lq) return;
@@ -287,6 +256,211 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
             for (int e = 0; e < 4; ++e) x[e] = dead ? 0.f : dq[b][4 * q + e] * f;
             seq_store4<T>(to, 32 * b + 8 * q + 4 * hi, x[0], x[1], x[2], x[3]);
         }
+}
+
+// Sums of dS by distance, -far < d < far.  Blocks of 128 queries and 64 keys whose first key stands 64 x positions behind the
+// first query, x an offset, have the same distance in the same place: a workgroup adds the dS of such blocks of one head, of all
+// sequences and all rows (its share of them, a chunk), up in registers, 32 queries a wave, and forms the sums along the diagonals
+// once at its end.  The bias of a place is the same for all of them and stays in registers too.
+constexpr int kTableRows = 128, kTableKeys = 64, kLine = 192;
+
+template <class T, int D>
+__global__ void __launch_bounds__(256) seq_table_kernel(SeqArgs a, BackPlan plan) {
+    constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, KT = RB >= 512 ? 32 : kTableKeys, KS = KT / 32, HALVES = kTableKeys / KT;
+    constexpr uint32_t kTile = KT * RB;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const uint32_t base = lds_offset(lds);
+    const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t hi = lane >> 5, c = lane & 31u;
+    uint32_t rest = fastdiv(blockIdx.x, plan.by_chunks);
+    const int chunk = (int)(blockIdx.x - rest * plan.by_chunks.d);
+    const int head = (int)fastdiv(rest, plan.by_offsets), kv = head / plan.group;
+    const int offset = plan.low_offset + (int)(rest - (uint32_t)head * plan.by_offsets.d);
+    const int far = a.far;
+    const float* const table = a.table + (size_t)head * a.nb;
+    const float scale = a.scale * kLog2e;
+
+    SeqRowReader<RB> row_reader;
+    row_reader.init(hi, c);
+    const uint32_t kld = (uint32_t)(a.ldk * E);
+    SeqLoader<RB, KT, 4> load;
+    load.init(wave, lane, kld);
+
+    f32x16 sum[2], b[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        seq_zero(sum[k]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            b[k][r] = seq_bias_at(table, a.buckets, a.nb, far, kTableKeys * offset + 32 * k + 8 * (r / 4) + 4 * (int)hi + r % 4 - 32 * (int)wave - (int)c);
+    }
+
+    // the next block of the chunk with a pair in it, and its sizes
+    const int per = (plan.items + plan.chunks - 1) / plan.chunks, end = (chunk + 1) * per < plan.items ? (chunk + 1) * per : plan.items;
+    struct Block { int item, n, i0, qlen, klen, start, j0; };
+    auto find = [&](int item) {
+        Block x{item, 0, 0, 0, 0, 0, 0};
+        for (; x.item < end; ++x.item) {
+            x.n = (int)fastdiv((uint32_t)x.item, plan.by_table_blocks);
+            x.i0 = kTableRows * (x.item - x.n * (int)plan.by_table_blocks.d);
+            x.qlen = seq_length(a.q_len, x.n, a.Lq);
+            x.klen = seq_length(a.k_len, x.n, a.Lk);
+            x.start = seq_start(a.q_start, x.n);
+            x.j0 = x.start + x.i0 + kTableKeys * offset;
+            if (x.i0 < x.qlen && x.j0 < x.klen && x.j0 + kTableKeys > 0) break;
+        }
+        return x;
+    };
+    // keys in front of the first one are not loaded either: the rows' offsets count from the first key that exists, and wrap
+    auto issue = [&](const Block& x, int half, uint32_t buf) {
+        const int j = x.j0 + half * KT, from = j < 0 ? 0 : j;
+        const int rows = x.klen - from < KT + j - from ? x.klen - from : KT + j - from;
+        const size_t at = (((size_t)x.n * a.Lk + from) * a.ldk + (size_t)kv * D) * E;
+        const uint32_t bytes = rows > 0 ? (uint32_t)(rows - 1) * kld + RB : 0u, shift = (uint32_t)(from - j) * kld;
+        const u32x4 ks = lds_source(static_cast<const char*>(a.k) + at, bytes), vs = lds_source(static_cast<const char*>(a.v) + at, bytes);
+        const uint32_t to = base + buf * 2u * kTile;
+#pragma unroll
+        for (int i = 0; i < load.kLoads; ++i) {
+            load_to_lds(ks, load.off[i] - shift, to + load.to + (uint32_t)i * 4096u);
+            load_to_lds(vs, load.off[i] - shift, to + kTile + load.to + (uint32_t)i * 4096u);
+        }
+    };
+
+    Block now = find(chunk * per);
+    // what no load fills: its scores are shut out, but zero times what LDS may hold has to be zero
+    for (uint32_t o = threadIdx.x * 16u; o < 4u * kTile; o += 4096u) *reinterpret_cast<u32x4*>(lds + o) = u32x4{0u, 0u, 0u, 0u};
+    __syncthreads();
+    uint32_t buf = 0;
+    if (now.item < end) issue(now, 0, 0);
+    while (now.item < end) {
+        const int i = now.i0 + (int)(32u * wave + c);
+        u32x4 qf[NC], gf[NC];
+#pragma unroll
+        for (int s = 0; s < NC; ++s) qf[s] = gf[s] = u32x4{0u, 0u, 0u, 0u};
+        float ref = 0.f, l = kDead, delta = 0.f;
+        if (i < now.qlen) {
+            const size_t row = ((size_t)now.n * a.H + head) * a.Lq + i, at_row = (size_t)now.n * a.Lq + i, channel = (size_t)head * D;
+            const f32x2 stat = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
+            if (stat[0] != -__builtin_inff()) {
+                ref = stat[0];
+                l = stat[1];
+                delta = plan.delta[row];
+            }
+            const char* const qp = static_cast<const char*>(a.q) + (at_row * a.ldq + channel) * E + 16u * hi;
+            const char* const gp = static_cast<const char*>(a.d_o) + (at_row * a.ldg + channel) * E + 16u * hi;
+#pragma unroll
+            for (int s = 0; s < NC; ++s) {
+                qf[s] = *reinterpret_cast<const u32x4*>(qp + 32 * s);
+                gf[s] = *reinterpret_cast<const u32x4*>(gp + 32 * s);
+            }
+        }
+        const int pos = now.start + i, lim = l == kDead ? 0 : (a.causal && pos + 1 < now.klen ? pos + 1 : now.klen);
+        const Block next = find(now.item + 1);
+#pragma unroll
+        for (int half = 0; half < HALVES; ++half, buf ^= 1u) {
+            lds_loads_done();
+            __syncthreads();
+            if (half + 1 < HALVES) issue(now, half + 1, buf ^ 1u);
+            else if (next.item < end) issue(next, 0, buf ^ 1u);
+            const uint32_t kt = base + buf * 2u * kTile, vt = kt + kTile;
+            const int j0 = now.j0 + half * KT + 4 * (int)hi;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const int block = half * KS + k;
+                f32x16 p, dp;
+                seq_zero(p);
+                seq_zero(dp);
+#pragma unroll
+                for (int x = 0; x < NC; ++x) p = seq_dot<T>(row_reader.read(kt, x, k), qf[x], p);
+#pragma unroll
+                for (int x = 0; x < NC; ++x) dp = seq_dot<T>(row_reader.read(vt, x, k), gf[x], dp);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int j = j0 + 32 * k + 8 * (r / 4) + r % 4;
+                    const float s = fmaf(p[r], scale, b[block][r]);
+                    const float w = __builtin_amdgcn_exp2f((s - ref) - l), x = w * (dp[r] - delta);
+                    sum[block][r] += j >= 0 && j < lim ? x : 0.f;
+                }
+            }
+        }
+        now = next;
+    }
+
+    // Diagonals of the wave's two squares of 32: each goes through LDS, rows of keys 33 apart; a lane follows one of the 63.
+    __syncthreads();
+    const uint32_t square = base + wave * (33u * 32u * 4u), each = base + 4u * (33u * 32u * 4u);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) seq_lds_put(square + 4u * (33u * (8 * (r / 4) + 4 * hi + r % 4) + c), sum[k][r]);
+        __syncthreads();
+        float x = 0.f;
+        for (int cc = 0; cc < 32; ++cc) {
+            const int key = (int)lane - 31 + cc;
+            if (key >= 0 && key < 32) x += seq_lds_f32(square + 4u * (uint32_t)(33 * key + cc));
+        }
+        seq_lds_put(each + 4u * (64u * (2u * wave + k) + lane), x);  // key - row = lane - 31 of the square; lane 63: nothing
+        __syncthreads();
+    }
+    // place x of the line: key - row = x - 127 in the block
+    if (threadIdx.x < kLine) {
+        float x = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int at = (int)threadIdx.x - 96 + 32 * w - 32 * k;
+                if (at >= 0 && at < 63) x += seq_lds_f32(each + 4u * (uint32_t)(64 * (2 * w + k) + at));
+            }
+        plan.parts[(size_t)blockIdx.x * kLine + threadIdx.x] = x;
+    }
+}
+
+// Lines of one head by distance: what the offsets that meet a distance have of it, and the two ends.
+__global__ void __launch_bounds__(256) seq_lines_kernel(SeqArgs a, BackPlan plan) {
+    const int head = (int)blockIdx.y, far = a.far;
+    float* const line = plan.lines + (size_t)head * (2 * (size_t)far + 1);
+    if (blockIdx.x == 0) {
+        const float* const ends = plan.ends + 2 * (size_t)head * a.N * plan.row_waves;
+        const long long count = a.N * plan.row_waves;
+        f32x2 sum = {0.f, 0.f};
+        for (long long w = threadIdx.x; w < count; w += 256) {
+            const f32x2 x = *reinterpret_cast<const f32x2*>(ends + 2 * w);
+            sum[0] += x[0];
+            sum[1] += x[1];
+        }
+        __shared__ float sums[2][256];
+        sums[0][threadIdx.x] = sum[0];
+        sums[1][threadIdx.x] = sum[1];
+        for (unsigned x = 128; x > 0; x /= 2) {
+            __syncthreads();
+            if (threadIdx.x < x) {
+                sums[0][threadIdx.x] += sums[0][threadIdx.x + x];
+                sums[1][threadIdx.x] += sums[1][threadIdx.x + x];
+            }
+        }
+        if (threadIdx.x == 0) {
+            if (far == 0) line[0] = sums[0][0] + sums[1][0];
+            else {
+                line[0] = sums[0][0];
+                line[2 * (size_t)far] = sums[1][0];
+            }
+        }
+        return;
+    }
+    // four threads a distance share its chunks
+    const int d = ((int)blockIdx.x - 1) * 64 + (int)(threadIdx.x >> 2) - far + 1;
+    float sum = 0.f;
+    if (d < far)
+        for (int x = 0; x < plan.offsets; ++x) {
+            const int at = d - kTableKeys * (plan.low_offset + x) + kTableRows - 1;
+            if (at < 0 || at >= kTableRows + kTableKeys - 1) continue;
+            const float* const src = plan.parts + ((size_t)head * plan.offsets + x) * plan.chunks * kLine + at;
+            for (int w = (int)(threadIdx.x & 3u); w < plan.chunks; w += 4) sum += src[(size_t)w * kLine];
+        }
+    sum += __shfl_xor(sum, 1, 64);
+    sum += __shfl_xor(sum, 2, 64);
+    if (d < far && (threadIdx.x & 3u) == 0) line[far + d] = sum;
 }
 
 // Half data: P and dS are taken 2^6 times as large and the sums divided again, since a probability of 2^-14 and less (keys by the
@@ -492,26 +666,37 @@ __global__ void __launch_bounds__(256) seq_join_keys_kernel(SeqArgs a, BackPlan 
 }
 
 template <class Kernel>
-hipError_t start(Kernel* kernel, unsigned grid, int block, size_t lds, hipStream_t s, const SeqArgs& a, const BackPlan& plan) {
-    if (grid == 0) return hipSuccess;  // no queries, or no keys
+hipError_t start(Kernel* kernel, dim3 grid, int block, size_t lds, hipStream_t s, const SeqArgs& a, const BackPlan& plan) {
+    if (grid.x == 0) return hipSuccess;  // no queries, or no keys
     const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3(grid), dim3(block), lds, s, a, plan);
+    hipLaunchKernelGGL(kernel, grid, dim3(block), lds, s, a, plan);
     return hipGetLastError();
+}
+
+template <class T, int D>
+hipError_t launch_table(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
+    constexpr int RB = D * SeqSize<T>::value;
+    const size_t tiles = 4 * (size_t)(RB >= 512 ? 32 : kTableKeys) * RB, squares = 4 * 33 * 32 * 4 + 8 * 64 * 4;
+    hipError_t e = start(&seq_table_kernel<T, D>, dim3((unsigned)(a.H * plan.offsets * plan.chunks)), 256, tiles > squares ? tiles : squares, s, a, plan);
+    if (e != hipSuccess) return e;
+    e = start(&seq_lines_kernel, dim3(1u + (unsigned)((2 * a.far - 1 + 63) / 64), (unsigned)a.H), 256, 0, s, a, plan);
+    if (e != hipSuccess) return e;
+    return launch_bucket_sums(plan.lines, nullptr, a.buckets, a.dtable, a.H, a.nb, a.far, 1, s);
 }
 
 template <class T, int D, int W>
 hipError_t launch(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
     constexpr int KT = seq_forward_keys(D * SeqSize<T>::value, W);
     const size_t tiles = 4 * (size_t)KT * D * SeqSize<T>::value, bias = 2 * sizeof(float) * plan.bias_entries;
-    hipError_t e = a.dtable ? start(&seq_rows_kernel<T, D, W, KT, true>, plan.row_grid, 64 * W, tiles + bias + W * 8 * (KT + 32), s, a, plan)
-                            : start(&seq_rows_kernel<T, D, W, KT, false>, plan.row_grid, 64 * W, tiles + bias, s, a, plan);
+    hipError_t e = a.dtable ? start(&seq_rows_kernel<T, D, W, KT, true>, dim3(plan.row_grid), 64 * W, tiles + bias, s, a, plan)
+                            : start(&seq_rows_kernel<T, D, W, KT, false>, dim3(plan.row_grid), 64 * W, tiles + bias, s, a, plan);
     if (e != hipSuccess) return e;
     if (a.dtable) {
-        e = launch_bucket_sums(plan.parts, plan.lines, a.buckets, a.dtable, a.H, a.nb, a.far, a.N * plan.row_waves, s);
+        e = launch_table<T, D>(a, plan, s);
         if (e != hipSuccess) return e;
     }
-    e = start(&seq_keys_kernel<T, D, W, KT>, plan.key_grid, 64 * W, tiles + 24 * KT + bias, s, a, plan);
+    e = start(&seq_keys_kernel<T, D, W, KT>, dim3(plan.key_grid), 64 * W, tiles + 24 * KT + bias, s, a, plan);
     if (e != hipSuccess || plan.splits == 1 || a.Lk == 0) return e;
     const size_t threads = (size_t)a.N * a.Lk * a.KV * D / 2, blocks = (threads + 255) / 256;
     hipLaunchKernelGGL((seq_join_keys_kernel<T, D>), dim3((unsigned)blocks), dim3(256), 0, s, a, plan);
@@ -557,10 +742,40 @@ bool back_plan(const SeqArgs& a, BackPlan& p) {
     p.by_splits = make_fastdiv((uint32_t)p.splits);
     p.by_kv = make_fastdiv((uint32_t)a.KV);
     p.bias_entries = a.table ? (uint32_t)(KT + block - 1) : 0u;
+
+    // offsets of blocks with distances between -far and far, and, where all start at 0, with a pair in them
+    const int blocks = (a.Lq + kTableRows - 1) / kTableRows;
+    auto down = [](long long x, int y) { return (int)(x >= 0 ? x / y : -((y - 1 - x) / y)); };  // floor
+    int low = down(-(long long)a.far - kTableKeys + 1, kTableKeys) + 1, high = down((long long)a.far + kTableRows - 2, kTableKeys);
+    if (a.q_start == nullptr) {
+        const int most = down((long long)a.Lk - 1, kTableKeys), least = -(((blocks > 0 ? blocks - 1 : 0) * kTableRows + kTableKeys - 1) / kTableKeys);
+        high = high < most ? high : most;
+        low = low > least ? low : least;
+    }
+    if (a.causal && high > (kTableRows - 1) / kTableKeys) high = (kTableRows - 1) / kTableKeys;
+    p.low_offset = low;
+    p.offsets = high >= low ? high - low + 1 : 0;
+    if (a.far == 0) p.offsets = 0;  // every distance is at an end
+    const long long items = a.N * blocks;
+    p.items = (int)items;
+    // four workgroups a CU, in chunks of at least four blocks where that leaves as many
+    long long chunks = 4LL * cus / ((long long)a.H * (p.offsets > 0 ? p.offsets : 1));
+    if (chunks > (items + 3) / 4) chunks = (items + 3) / 4;
+    p.chunks = chunks < 1 ? 1 : (int)chunks;
+    p.by_offsets = make_fastdiv((uint32_t)(p.offsets > 0 ? p.offsets : 1));
+    p.by_chunks = make_fastdiv((uint32_t)p.chunks);
+    p.by_table_blocks = make_fastdiv((uint32_t)(blocks > 0 ? blocks : 1));
     return true;
 }
 
 size_t padded(size_t floats) { return (floats * sizeof(float) + 255) & ~(size_t)255; }
+size_t padded_ends(const SeqArgs& a, const BackPlan& p) { return padded((size_t)a.H * a.N * p.row_waves * 2); }
+size_t padded_lines(const SeqArgs& a) { return padded((size_t)a.H * (2 * (size_t)a.far + 1)); }
+// whatever the starts and causality leave of the offsets: as many workgroups as fill the device, or one for every offset
+size_t table_bytes(const SeqArgs& a, const BackPlan& p) {
+    const size_t every = (size_t)a.H * ((2 * (size_t)a.far + kTableRows + kTableKeys) / kTableKeys + 1), fill = 4 * (size_t)cu_count();
+    return padded_ends(a, p) + padded_lines(a) + padded((every > fill ? every : fill) * kLine);
+}
 
 }  // namespace
 
@@ -570,10 +785,7 @@ size_t seq_backward_workspace(const SeqArgs& a, bool want_dtable) {
     if (!back_plan(a, p)) return 0;
     size_t bytes = padded((size_t)a.N * a.H * a.Lq);
     if (p.splits > 1) bytes += padded((size_t)p.splits * 2 * a.N * a.Lk * a.KV * a.D);
-    if (want_dtable) {
-        const long long count = a.N * p.row_waves;
-        bytes += padded((size_t)a.H * count * (2 * (size_t)a.far + 1)) + bucket_lines_bytes(a.H, a.far, count);
-    }
+    if (want_dtable) bytes += table_bytes(a, p);
     return bytes;
 }
 
@@ -585,9 +797,11 @@ hipError_t launch_sequence_backward(const SeqArgs& a, void* workspace, hipStream
     ws += padded((size_t)a.N * a.H * a.Lq);
     p.part_kv = reinterpret_cast<float*>(ws);
     if (p.splits > 1) ws += padded((size_t)p.splits * 2 * a.N * a.Lk * a.KV * a.D);
-    p.parts = reinterpret_cast<float*>(ws);
-    if (a.dtable) ws += padded((size_t)a.H * a.N * p.row_waves * (2 * (size_t)a.far + 1));
+    p.ends = reinterpret_cast<float*>(ws);
+    ws += padded_ends(a, p);
     p.lines = reinterpret_cast<float*>(ws);
+    ws += padded_lines(a);
+    p.parts = reinterpret_cast<float*>(ws);
     if (a.dtype == 0) return launch<SeqF32>(a, p, s);
     return a.dtype == 1 ? launch<SeqBf16>(a, p, s) : launch<SeqF16>(a, p, s);
 }
