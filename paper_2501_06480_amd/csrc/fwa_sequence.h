@@ -204,14 +204,50 @@ __device__ __forceinline__ void seq_store4(char* row, uint32_t channel, float a,
     }
 }
 
+// Which workgroup has which part of which unit (a head of a sequence).  Workgroups go to the 8 XCDs in turn, each with an L2 of its own,
+// and an XCD's to its 32 CUs.  Units are dealt to the XCDs in turn too, whole ones, whose keys then stay in one L2, and each sequence's heads
+// to all XCDs, since sequences differ in length: contiguous ranges of units, a long sequence on two XCDs, left the CUs of the others
+// idle (encoder of 4 ragged sequences, 16 heads: 102 us).  Few units that 8 does not divide are dealt by parts instead.
+// Causal parts differ in size: every second round of an XCD's 32 goes backwards, so that a CU's parts come to one sum.
+struct SeqDeal {
+    uint32_t units, each, per_xcd;
+    int whole, snake;
+    FastDiv by_each;
+};
+inline unsigned seq_deal(SeqDeal& d, long long units, long long each, bool snake) {
+    d.units = (uint32_t)units;
+    d.each = (uint32_t)each;
+    d.whole = units % 8 == 0 || units >= 64;
+    d.per_xcd = (uint32_t)((units + 7) / 8 * each);
+    d.snake = snake;
+    d.by_each = make_fastdiv(d.each > 0 ? d.each : 1u);
+    return (unsigned)(d.whole ? 8LL * d.per_xcd : units * each);
+}
+// false: nothing to do
+__device__ __forceinline__ bool seq_dealt(const SeqDeal& d, uint32_t block, uint32_t& unit, uint32_t& part) {
+    if (d.whole) {
+        uint32_t at = block >> 3;
+        const uint32_t round = at >> 5;
+        if (d.snake && (round & 1u) && 32u * round + 32u <= d.per_xcd) at = 64u * round + 31u - at;
+        const uint32_t turn = fastdiv(at, d.by_each);
+        part = at - turn * d.each;
+        unit = 8u * turn + (block & 7u);
+        return unit < d.units;
+    }
+    unit = fastdiv(block, d.by_each);
+    part = block - unit * d.each;
+    return true;
+}
+
 // How a forward call is laid out on the device.
 struct SeqPlan {
     int group;           // heads of queries per head of keys
     int packed;          // one block has the rows of a whole group (few rows: group * Lq <= 32)
     int waves, blocks, splits;
     unsigned grid;
-    uint32_t xcd_q, xcd_r, bias_entries;
-    FastDiv by_splits, by_blocks, by_heads;
+    SeqDeal deal;
+    uint32_t bias_entries;
+    FastDiv by_splits, by_heads;
     size_t rows;         // N * H * Lq
     float* part_o;       // [splits][rows][D], not divided by the sum
     float* part_ml;      // [splits][rows][2]

@@ -13,8 +13,9 @@ namespace {
 struct BackPlan {
     int group, waves, row_blocks, key_blocks, splits;
     unsigned row_grid, key_grid;
-    uint32_t row_q, row_r, key_q, key_r, bias_entries;
-    FastDiv by_row_blocks, by_heads, by_key_blocks, by_splits, by_kv;
+    SeqDeal row_deal, key_deal;
+    uint32_t bias_entries;
+    FastDiv by_heads, by_splits, by_kv;
     int row_waves;       // waves with rows per head of a sequence: ceil(Lq / 32)
     float* delta;        // [N, H, Lq]
     float* ends;         // [H][N * row_waves][2]: sums of dS at and beyond -far and far
@@ -48,11 +49,11 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
     const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t hi = lane >> 5, c = lane & 31u;
 
-    uint32_t at = xcd_logical_block(blockIdx.x, plan.row_q, plan.row_r);
-    uint32_t rest = fastdiv(at, plan.by_row_blocks);
-    int block = (int)(at - rest * plan.by_row_blocks.d);
-    const long long n = fastdiv(rest, plan.by_heads);
-    const int head = (int)(rest - (uint32_t)n * plan.by_heads.d), kv = head / plan.group;
+    uint32_t unit, part;
+    if (!seq_dealt(plan.row_deal, blockIdx.x, unit, part)) return;
+    int block = (int)part;
+    const long long n = fastdiv(unit, plan.by_heads);
+    const int head = (int)(unit - (uint32_t)n * plan.by_heads.d), kv = head / plan.group;
     if (a.causal) block = plan.row_blocks - 1 - block;
     const int i0 = block * 32 * W, i = i0 + (int)(32u * wave + c);
     const int span_rows = a.Lq - i0 < 32 * W ? a.Lq - i0 : 32 * W;
@@ -295,12 +296,12 @@ __global__ void __launch_bounds__(256) seq_table_kernel(SeqArgs a, BackPlan plan
             b[k][r] = seq_bias_at(table, a.buckets, a.nb, far, kTableKeys * offset + 32 * k + 8 * (r / 4) + 4 * (int)hi + r % 4 - 32 * (int)wave - (int)c);
     }
 
-    // the next block of the chunk with a pair in it, and its sizes
-    const int per = (plan.items + plan.chunks - 1) / plan.chunks, end = (chunk + 1) * per < plan.items ? (chunk + 1) * per : plan.items;
+    // the next block of the chunk (every plan.chunks-th: sequences differ in length) with a pair in it, and its sizes
+    const int end = plan.items;
     struct Block { int item, n, i0, qlen, klen, start, j0; };
     auto find = [&](int item) {
         Block x{item, 0, 0, 0, 0, 0, 0};
-        for (; x.item < end; ++x.item) {
+        for (; x.item < end; x.item += plan.chunks) {
             x.n = (int)fastdiv((uint32_t)x.item, plan.by_table_blocks);
             x.i0 = kTableRows * (x.item - x.n * (int)plan.by_table_blocks.d);
             x.qlen = seq_length(a.q_len, x.n, a.Lq);
@@ -326,7 +327,7 @@ __global__ void __launch_bounds__(256) seq_table_kernel(SeqArgs a, BackPlan plan
         }
     };
 
-    Block now = find(chunk * per);
+    Block now = find(chunk);
     // what no load fills: its scores are shut out, but zero times what LDS may hold has to be zero
     for (uint32_t o = threadIdx.x * 16u; o < 4u * kTile; o += 4096u) *reinterpret_cast<u32x4*>(lds + o) = u32x4{0u, 0u, 0u, 0u};
     __syncthreads();
@@ -355,7 +356,7 @@ __global__ void __launch_bounds__(256) seq_table_kernel(SeqArgs a, BackPlan plan
             }
         }
         const int pos = now.start + i, lim = l == kDead ? 0 : (a.causal && pos + 1 < now.klen ? pos + 1 : now.klen);
-        const Block next = find(now.item + 1);
+        const Block next = find(now.item + plan.chunks);
 #pragma unroll
         for (int half = 0; half < HALVES; ++half, buf ^= 1u) {
             lds_loads_done();
@@ -477,14 +478,11 @@ __global__ void __launch_bounds__(64 * W) seq_keys_kernel(SeqArgs a, BackPlan pl
     const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t hi = lane >> 5, c = lane & 31u;
 
-    uint32_t at = xcd_logical_block(blockIdx.x, plan.key_q, plan.key_r);
-    uint32_t rest = fastdiv(at, plan.by_splits);
-    const int split = (int)(at - rest * plan.by_splits.d);
-    at = rest;
-    rest = fastdiv(at, plan.by_key_blocks);
-    const int block = (int)(at - rest * plan.by_key_blocks.d);
-    const long long n = fastdiv(rest, plan.by_kv);
-    const int kv = (int)(rest - (uint32_t)n * plan.by_kv.d);
+    uint32_t unit, part;
+    if (!seq_dealt(plan.key_deal, blockIdx.x, unit, part)) return;
+    const int block = (int)fastdiv(part, plan.by_splits), split = (int)part - block * (int)plan.by_splits.d;
+    const long long n = fastdiv(unit, plan.by_kv);
+    const int kv = (int)(unit - (uint32_t)n * plan.by_kv.d);
     const int j0 = block * 32 * W, j = j0 + (int)(32u * wave + c), j_last = j0 + 32 * W - 1;
     const int qlen = seq_length(a.q_len, n, a.Lq), klen = seq_length(a.k_len, n, a.Lk), start = seq_start(a.q_start, n);
 
@@ -621,14 +619,14 @@ __global__ void __launch_bounds__(64 * W) seq_keys_kernel(SeqArgs a, BackPlan pl
     const size_t row = (size_t)n * a.Lk + j;
     if (plan.splits > 1) {
         const size_t values = (size_t)a.N * a.Lk * a.KV * D, to = (row * a.KV + kv) * D;
-        float* const part = plan.part_kv + (size_t)split * 2 * values + to;
+        float* const into = plan.part_kv + (size_t)split * 2 * values + to;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const uint32_t ch = 32 * b + 8 * q + 4 * hi;
-                *reinterpret_cast<f32x4*>(part + ch) = f32x4{dk[b][4 * q], dk[b][4 * q + 1], dk[b][4 * q + 2], dk[b][4 * q + 3]};
-                *reinterpret_cast<f32x4*>(part + values + ch) = f32x4{dv[b][4 * q], dv[b][4 * q + 1], dv[b][4 * q + 2], dv[b][4 * q + 3]};
+                *reinterpret_cast<f32x4*>(into + ch) = f32x4{dk[b][4 * q], dk[b][4 * q + 1], dk[b][4 * q + 2], dk[b][4 * q + 3]};
+                *reinterpret_cast<f32x4*>(into + values + ch) = f32x4{dv[b][4 * q], dv[b][4 * q + 1], dv[b][4 * q + 2], dv[b][4 * q + 3]};
             }
         return;
     }
@@ -729,16 +727,11 @@ bool back_plan(const SeqArgs& a, BackPlan& p) {
     if (splits > all / 2) splits = all / 2;
     if (splits > 16) splits = 16;
     p.splits = splits < 1 ? 1 : (int)splits;
-    if (rows * 64 * p.waves > 4.0e9 || keys * p.splits * 64 * p.waves > 4.0e9) return false;
-    p.row_grid = (unsigned)rows;
-    p.key_grid = (unsigned)((long long)keys * p.splits);
-    p.row_q = p.row_grid / 8u;
-    p.row_r = p.row_grid % 8u;
-    p.key_q = p.key_grid / 8u;
-    p.key_r = p.key_grid % 8u;
-    p.by_row_blocks = make_fastdiv((uint32_t)(p.row_blocks > 0 ? p.row_blocks : 1));
+    // threads of a launch
+    if ((rows + 8.0 * p.row_blocks) * 64 * p.waves > 4.0e9 || (keys + 8.0 * p.key_blocks) * p.splits * 64 * p.waves > 4.0e9) return false;
+    p.row_grid = seq_deal(p.row_deal, a.N * a.H, p.row_blocks, a.causal && p.row_blocks > 1);
+    p.key_grid = seq_deal(p.key_deal, a.N * a.KV, (long long)p.key_blocks * p.splits, a.causal && p.key_blocks > 1);
     p.by_heads = make_fastdiv((uint32_t)a.H);
-    p.by_key_blocks = make_fastdiv((uint32_t)(p.key_blocks > 0 ? p.key_blocks : 1));
     p.by_splits = make_fastdiv((uint32_t)p.splits);
     p.by_kv = make_fastdiv((uint32_t)a.KV);
     p.bias_entries = a.table ? (uint32_t)(KT + block - 1) : 0u;

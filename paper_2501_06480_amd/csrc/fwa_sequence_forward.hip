@@ -23,16 +23,13 @@ __global__ void __launch_bounds__(64 * W) seq_forward_kernel(SeqArgs a, SeqPlan 
     const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t hi = lane >> 5, c = lane & 31u, slot = 32u * wave + c;
 
-    // block -> split of the keys, block of rows, head (or group of heads that share keys), sequence
-    uint32_t at = xcd_logical_block(blockIdx.x, plan.xcd_q, plan.xcd_r);
-    uint32_t rest = fastdiv(at, plan.by_splits);
-    const int split = (int)(at - rest * plan.by_splits.d);
-    at = rest;
-    rest = fastdiv(at, plan.by_blocks);
-    int block = (int)(at - rest * plan.by_blocks.d);
-    at = rest;
-    const long long n = fastdiv(at, plan.by_heads);
-    const int hk = (int)(at - (uint32_t)n * plan.by_heads.d);  // head, or head of the keys where the rows of a group are packed
+    // workgroup -> sequence, head (or group of heads that share keys), block of rows, split of the keys
+    uint32_t unit, part;
+    if (!seq_dealt(plan.deal, blockIdx.x, unit, part)) return;
+    int block = (int)fastdiv(part, plan.by_splits);
+    const int split = (int)part - block * (int)plan.by_splits.d;
+    const long long n = fastdiv(unit, plan.by_heads);
+    const int hk = (int)(unit - (uint32_t)n * plan.by_heads.d);  // head, or head of the keys where the rows of a group are packed
     if (a.causal) block = plan.blocks - 1 - block;             // those with most keys first
     const int G = plan.group, i0 = block * 32 * W;
     const int kv = plan.packed ? hk : hk / G;
@@ -172,15 +169,15 @@ __global__ void __launch_bounds__(64 * W) seq_forward_kernel(SeqArgs a, SeqPlan 
     if (i >= qlen) { m = -__builtin_inff(); l = 0.f; }
     const size_t row = ((size_t)n * a.H + head) * a.Lq + i;
     if (plan.splits > 1) {
-        const size_t part = (size_t)split * plan.rows + row;
-        float* const to = plan.part_o + part * D;
+        const size_t mine = (size_t)split * plan.rows + row;
+        float* const to = plan.part_o + mine * D;
         if (l != 0.f)  // nothing reads a part without weight
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     *reinterpret_cast<f32x4*>(to + 32 * b + 8 * q + 4 * hi) = f32x4{o[b][4 * q], o[b][4 * q + 1], o[b][4 * q + 2], o[b][4 * q + 3]};
-        if (hi == 0) *reinterpret_cast<f32x2*>(plan.part_ml + 2 * part) = f32x2{m, l};
+        if (hi == 0) *reinterpret_cast<f32x2*>(plan.part_ml + 2 * mine) = f32x2{m, l};
         return;
     }
     const bool any = l != 0.f;  // NaN too
@@ -272,12 +269,9 @@ bool seq_forward_plan(const SeqArgs& a, SeqPlan& p) {
     if (splits > tiles / 2) splits = tiles / 2;
     if (splits > 64) splits = 64;
     p.splits = splits < 1 ? 1 : (int)splits;
-    if (base * p.splits * 64.0 * p.waves > 4.0e9) return false;  // threads of a launch
-    p.grid = (unsigned)((long long)base * p.splits);
-    p.xcd_q = p.grid / 8u;
-    p.xcd_r = p.grid % 8u;
+    if ((base * p.splits + 8.0 * p.blocks * p.splits) * 64.0 * p.waves > 4.0e9) return false;  // threads of a launch
+    p.grid = seq_deal(p.deal, (long long)a.N * (p.packed ? a.KV : a.H), (long long)p.blocks * p.splits, a.causal && p.blocks > 1);
     p.by_splits = make_fastdiv((uint32_t)p.splits);
-    p.by_blocks = make_fastdiv((uint32_t)p.blocks);
     p.by_heads = make_fastdiv((uint32_t)(p.packed ? a.KV : a.H));
     p.rows = (size_t)a.N * a.H * a.Lq;
     p.bias_entries = a.table == nullptr ? 0 : p.packed ? (uint32_t)(p.group * (KT + a.Lq - 1)) : (uint32_t)(KT + 32 * p.waves - 1);
