@@ -141,6 +141,9 @@ struct SeqArgs {
 // 16-bit data (five workgroups on a CU).
 constexpr int seq_forward_keys(int row_bytes, int waves) { return row_bytes >= 512 || (waves == 1 && row_bytes >= 256) ? 32 : 64; }
 
+// Keys resp. queries per tile of the backward.
+constexpr int seq_backward_rows(int row_bytes) { return row_bytes >= 256 ? 32 : 64; }
+
 hipError_t launch_sequence_forward(const SeqArgs& a, void* workspace, hipStream_t s);
 size_t seq_forward_workspace(const SeqArgs& a);
 hipError_t launch_sequence_backward(const SeqArgs& a, void* workspace, hipStream_t s);

@@ -47,6 +47,28 @@ __device__ __forceinline__ constexpr uint32_t seq_swizzle(uint32_t row) {
     else return ((row & 3u) << 2) | ((row >> 2) & 3u);
 }
 
+// N loads of load_to_lds() (fwa_device.h, and its wait states) one behind the other, 16 bytes a lane each, to LDS places STEP bytes apart: the
+// descriptor is old enough for all once it is for the first, and m0 is put back once.
+template <int N, int STEP>
+__device__ __forceinline__ void seq_loads_to_lds(const u32x4& r, const uint32_t* off, uint32_t lds_off) {
+    uint32_t saved;
+    if constexpr (N == 1) {
+        load_to_lds(r, off[0], lds_off);
+    } else if constexpr (N == 2) {
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
+                     "s_add_u32 m0, m0, %5\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen lds\n\ts_mov_b32 m0, %0"
+                     : "=&s"(saved) : "s"(lds_off), "v"(off[0]), "v"(off[1]), "s"(r), "i"(STEP) : "memory", "scc");
+    } else {
+        static_assert(N % 4 == 0, "one, two or a multiple of four loads");
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\tbuffer_load_dwordx4 %2, %6, 0 offen lds\n\t"
+                     "s_add_u32 m0, m0, %7\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %6, 0 offen lds\n\t"
+                     "s_add_u32 m0, m0, %7\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %6, 0 offen lds\n\t"
+                     "s_add_u32 m0, m0, %7\n\ts_nop 0\n\tbuffer_load_dwordx4 %5, %6, 0 offen lds\n\ts_mov_b32 m0, %0"
+                     : "=&s"(saved) : "s"(lds_off), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(r), "i"(STEP) : "memory", "scc");
+        if constexpr (N > 4) seq_loads_to_lds<N - 4, STEP>(r, off + 4, lds_off + 4u * STEP);
+    }
+}
+
 // The loads of one tile of ROWS rows by WAVES waves: wave-uniform descriptor, 1024 bytes of LDS per load.
 template <int RB, int ROWS, int WAVES>
 struct SeqLoader {
@@ -63,14 +85,18 @@ struct SeqLoader {
             off[i] = row * row_bytes + ((place ^ seq_swizzle<RB>(row)) * 16u);
         }
     }
-    // rows from `first` on (64-bit), `rows` of which exist; `lds` = the tile's place
-    __device__ __forceinline__ void issue(const char* first, int rows, uint32_t row_bytes, uint32_t lds) const {
-        const uint32_t n = rows < ROWS ? (rows > 0 ? (uint32_t)rows : 0u) : (uint32_t)ROWS;
-        const u32x4 src = lds_source(first, n ? (n - 1u) * row_bytes + RB : 0u);
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) load_to_lds(src, off[i], lds + to + (uint32_t)i * (1024u * WAVES));
+    // `bytes` of the rows from `first` on exist; `lds` = the tile's place
+    __device__ __forceinline__ void issue(uintptr_t first, uint32_t bytes, uint32_t lds) const {
+        const u32x4 src = {(uint32_t)first, (uint32_t)(first >> 32) & 0xffffu, bytes, 0x00020000u};
+        seq_loads_to_lds<kLoads, 1024 * WAVES>(src, off, lds + to);
     }
 };
+// Bytes from the first of `rows` rows to the end of the last, of at most `most` rows (scalar: the rows of a tile that exist).
+template <int RB>
+__device__ __forceinline__ uint32_t seq_tile_bytes(int rows, int most, uint32_t row_bytes) {
+    const int n = rows < most ? rows : most;
+    return n > 0 ? (uint32_t)(n - 1) * row_bytes + RB : 0u;
+}
 
 __device__ __forceinline__ u32x4 seq_lds_b128(uint32_t at) {
     return *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)at;
@@ -192,6 +218,37 @@ __device__ __forceinline__ int seq_start(const int32_t* starts, long long n) {
     const int x = starts[n];
     return x < -kSeqFarthest ? -kSeqFarthest : (x > kSeqFarthest ? kSeqFarthest : x);
 }
+
+// Tiles of `size` keys from key 0 on that have a pair with a distance between -far and far, of queries at the positions first .. last:
+// t0 .. t1 - 1.  Tiles in front of t0 lie at or beyond -far altogether, those from t1 on at or beyond far.  Without a table all count as the
+// latter.
+__device__ __forceinline__ void seq_near_tiles(bool table, int first, int last, int far, int size, int& t0, int& t1) {
+    t0 = t1 = 0;
+    if (!table) return;
+    const int x = first - far - size + 1, y = far + last + size - 1;
+    t0 = x < 0 ? 0 : x / size + 1;
+    t1 = y < 0 ? 0 : y / size;
+    if (t1 < t0) t1 = t0;
+}
+
+// Tiles of `size` rows from row 0 on that start below row x: ceil(x / size), at least 0.
+__device__ __forceinline__ int seq_tiles_up_to(int x, int size) { return x > 0 ? (x + size - 1) / size : 0; }
+
+// A thread's entry of the bias by distance of the tiles to come, for workgroups with a thread for each entry: the map a tile ahead of the table,
+// both ahead of their use, so that neither is waited for.  Entries outside the table are 0.
+struct SeqBiasAhead {
+    uint32_t column, of;  // column of the tile after next; that of `value`
+    float value;
+    __device__ __forceinline__ void find(const int32_t* buckets, int far, int distance) {
+        const int at = distance < -far ? -far : (distance > far ? far : distance);
+        column = (uint32_t)buckets[far + at];
+    }
+    __device__ __forceinline__ void fetch(const float* row, int nb) {
+        of = column;
+        value = row[column < (uint32_t)nb ? column : 0u];
+    }
+    __device__ __forceinline__ float get(int nb) const { return of < (uint32_t)nb ? seq_bias_log2(value) : 0.f; }
+};
 
 // Four neighbouring channels of a row, rounded to the type.
 template <class T>

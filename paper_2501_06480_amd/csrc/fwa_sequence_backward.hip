@@ -7,6 +7,8 @@
 // blocks of keys, has no fixed order.  Both products of a tile use its P and dS as they stand in registers (fwa_sequence.h).
 #include "fwa_sequence.h"
 
+#include <type_traits>
+
 namespace fwa {
 namespace {
 
@@ -30,15 +32,17 @@ constexpr float kDead = __builtin_inff();
 // Rows that see few keys: one of these may have nearly all the weight, dP - delta cancels, and the rounding of o would show.  There a walk in
 // front of the other forms delta from the same products as dP.  (The rows of a causal call that see up to two tiles are a block.)
 constexpr int kFewTiles = 2;
-enum { kInner, kBelow, kAbove, kBorder };  // where the distances of a tile lie against -far and far
 
+// Whether no query of a sequence sees more than one key: its weight is one and stays so, and all but dV is exactly zero, which products and their
+// differences need not be to the last bit.
+__device__ __forceinline__ bool seq_lone(bool causal, int start, int qlen, int klen) {
+    return klen <= 1 || (causal && start + qlen <= 1);
+}
 // a sum that is not fused with a product it takes in: the two forms of the rows kernel give the same bits
 __device__ __forceinline__ float plain_sum(float a, float b) {
 #pragma clang fp contract(off)
     return a + b;
 }
-// the weight of a score in base-2 units, against the reference of its row
-__device__ __forceinline__ float weight(float s, float ref) { return __builtin_amdgcn_exp2f(s - ref); }
 
 template <class T, int D, int W, int KT, bool TABLE>
 __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan plan) {
@@ -73,11 +77,16 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
     row_reader.init(hi, c);
     SeqColumnReader<T, D> column_reader;
     column_reader.init(hi, c);
-    auto issue = [&](int t, uint32_t buf) {
-        const size_t row = (size_t)t * KT;
-        const uint32_t to = base + buf * 2u * kTile;
-        load.issue(kp + row * kld, klen - t * KT, kld, to);
-        load.issue(vp + row * kld, klen - t * KT, kld, to + kTile);
+    // addresses of the next tile to ask for, and the rows from there on
+    uintptr_t next_k = reinterpret_cast<uintptr_t>(kp), next_v = reinterpret_cast<uintptr_t>(vp);
+    int next_rows = klen;
+    auto issue = [&](uint32_t buf) {
+        const uint32_t bytes = seq_tile_bytes<RB>(next_rows, KT, kld);
+        load.issue(next_k, bytes, base + buf * 2u * kTile);
+        load.issue(next_v, bytes, base + buf * 2u * kTile + kTile);
+        next_k += KT * kld;
+        next_v += KT * kld;
+        next_rows -= KT;
     };
 
     const size_t row = ((size_t)n * a.H + head) * a.Lq + i;
@@ -90,7 +99,7 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
         const f32x2 stat = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
         dead = stat[0] == -__builtin_inff();
         ref = dead ? 0.f : stat[0];
-        rl = dead ? 0.f : __builtin_amdgcn_exp2f(-stat[1]);
+        rl = dead || seq_lone(a.causal, start, qlen, klen) ? 0.f : __builtin_amdgcn_exp2f(-stat[1]);
         const size_t at_row = (size_t)n * a.Lq + i, channel = (size_t)head * D;
         const char* const qp = static_cast<const char*>(a.q) + (at_row * a.ldq + channel) * E + 16u * hi;
         const char* const gp = static_cast<const char*>(a.d_o) + (at_row * a.ldg + channel) * E + 16u * hi;
@@ -126,104 +135,161 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
     const float* const table = a.table ? a.table + (size_t)head * a.nb : nullptr;
     const int far = a.far;
     const float below = table ? seq_bias_at(table, a.buckets, a.nb, far, -far) : 0.f, above = table ? seq_bias_at(table, a.buckets, a.nb, far, far) : 0.f;
+    const bool modest = !__any(!(fabsf(below) < 256.f && fabsf(above) < 256.f));  // as in the forward
     const uint32_t entries = (uint32_t)(KT + span_rows - 1), my_bias = bias_at + 4u * ((uint32_t)(last - pos) + 4u * hi);
     const int lim = dead ? 0 : (a.causal && pos + 1 < klen ? pos + 1 : klen);
     const float scale = a.scale * kLog2e;
-    auto is_near = [&](int t) { return table && t * KT - last < far && t * KT + KT - 1 - first > -far; };
+    int near0, near1, mask0 = klen / KT;
+    seq_near_tiles(table != nullptr, first, last, far, KT, near0, near1);
+    if (a.causal && first < klen) {
+        const int to = first + 1 > 0 ? (first + 1) / KT : 0;
+        mask0 = to < mask0 ? to : mask0;
+    }
+    if (some_dead) mask0 = 0;
 
-    // before the barrier of tile t: its bias; behind it: the loads of the tile that follows
-    auto begin = [&](int t, uint32_t buf, bool more) {
-        if (is_near(t))
-            for (uint32_t e = threadIdx.x; e < entries; e += 64u * W)
-                seq_lds_put(bias_at + buf * bias_bytes + 4u * e, seq_bias_at(table, a.buckets, a.nb, far, t * KT - last + (int)e));
+    SeqBiasAhead ahead = {0u, 0u, 0.f};
+    auto find = [&](int t) { if (W == 4 && t >= near0 && t < near1) ahead.find(a.buckets, far, t * KT - last + (int)threadIdx.x); };
+    auto fetch = [&](int t) { if (W == 4 && t >= near0 && t < near1) ahead.fetch(table, a.nb); };
+    // before the barrier of tile t: its bias; behind it: what the tiles that follow need
+    auto begin = [&](int t, uint32_t buf) {
+        if (t >= near0 && t < near1) {
+            if constexpr (W == 4) {
+                if (threadIdx.x < entries) seq_lds_put(bias_at + buf * bias_bytes + 4u * threadIdx.x, ahead.get(a.nb));
+            } else {
+                for (uint32_t e = threadIdx.x; e < entries; e += 64u * W)
+                    seq_lds_put(bias_at + buf * bias_bytes + 4u * e, seq_bias_at(table, a.buckets, a.nb, far, t * KT - last + (int)e));
+            }
+        }
         lds_loads_done();
         __syncthreads();
-        if (more) issue(t + 1, buf ^ 1u);
+        fetch(t + 1);
+        find(t + 2);
+        if (t + 1 < tiles) issue(buf ^ 1u);
     };
-    // weights exp2(s - ref), the row's sum not divided out, and dP of a block of 32 keys
-    auto scores = [&](int t, uint32_t buf, int k, f32x16& p, f32x16& dp) {
-        const uint32_t kt = base + buf * 2u * kTile, vt = kt + kTile;
-        const int j0 = t * KT;
-        seq_zero(p);
-        seq_zero(dp);
+    auto start_walk = [&]() {
+        find(0);
+        fetch(0);
+        find(1);
+        next_k = reinterpret_cast<uintptr_t>(kp);
+        next_v = reinterpret_cast<uintptr_t>(vp);
+        next_rows = klen;
+        if (tiles > 0) issue(0);
+    };
+    // Q K^T of tile t, or, where the bias is not one value or pairs are shut out, the scores; the exponent of a weight, the row's sum not divided
+    // out, is s mul + minus
+    struct Exponent { float mul, minus; };
+    auto scores = [&](auto parity, int t, f32x16 (&s)[KS]) -> Exponent {
+        constexpr uint32_t B = decltype(parity)::value;
+        const uint32_t kt = base + B * 2u * kTile;
 #pragma unroll
-        for (int x = 0; x < NC; ++x) p = seq_dot<T>(row_reader.read(kt, x, k), qf[x], p);
+        for (int k = 0; k < KS; ++k) {
+            seq_zero(s[k]);
 #pragma unroll
-        for (int x = 0; x < NC; ++x) dp = seq_dot<T>(row_reader.read(vt, x, k), gf[x], dp);
-        if (is_near(t)) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) p[r] = fmaf(p[r], scale, seq_lds_f32(my_bias + buf * bias_bytes + 4u * (32 * k + 8 * (r / 4) + r % 4)));
-        } else {
-            const float b = j0 + KT - 1 - first <= -far ? below : above;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) p[r] = fmaf(p[r], scale, b);
+            for (int x = 0; x < NC; ++x) s[k] = seq_dot<T>(row_reader.read(kt, x, k), qf[x], s[k]);
         }
-        if (some_dead || j0 + KT > klen || (a.causal && j0 + KT - 1 > first)) {
-            const int room = lim - j0 - 4 * (int)hi;
+        const float flat = t < near0 ? below : above;
+        const bool near = t >= near0 && t < near1, plain = modest && !near && t < mask0;
+        if (!plain) {
+            if (near) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) p[r] = 32 * k + 8 * (r / 4) + r % 4 < room ? p[r] : -__builtin_inff();
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[k][r] = fmaf(s[k][r], scale, seq_lds_f32(my_bias + B * bias_bytes + 4u * (32 * k + 8 * (r / 4) + r % 4)));
+            } else {
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[k][r] = fmaf(s[k][r], scale, flat);
+            }
+            if (t >= mask0) {
+                const int room = lim - t * KT - 4 * (int)hi;
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[k][r] = 32 * k + 8 * (r / 4) + r % 4 < room ? s[k][r] : -__builtin_inff();
+            }
         }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = weight(p[r], ref);
+        return {plain ? scale : 1.f, plain ? flat - ref : -ref};
     };
 
     f32x16 dq[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) seq_zero(dq[b]);
     float ds_all = 0.f, ds_below = 0.f, ds_above = 0.f, p_below = 0.f, p_above = 0.f;
-    if (tiles > 0) issue(0, 0);
+    start_walk();
     if (tiles > 0 && tiles <= kFewTiles) {
         float sum = 0.f;
-        for (int t = 0; t < tiles; ++t) {
-            const uint32_t buf = (uint32_t)t & 1u;
-            begin(t, buf, t + 1 < tiles);
+        auto look = [&](auto parity, int t) {
+            constexpr uint32_t B = decltype(parity)::value;
+            begin(t, B);
+            f32x16 s[KS];
+            const Exponent e = scores(parity, t, s);
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                f32x16 p, dp;
-                scores(t, buf, k, p, dp);
+                f32x16 dp;
+                seq_zero(dp);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sum = fmaf(p[r], dp[r], sum);
+                for (int x = 0; x < NC; ++x) dp = seq_dot<T>(row_reader.read(base + B * 2u * kTile + kTile, x, k), gf[x], dp);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum = fmaf(__builtin_amdgcn_exp2f(fmaf(s[k][r], e.mul, e.minus)), dp[r], sum);
             }
-        }
+        };
+        look(std::integral_constant<uint32_t, 0>{}, 0);
+        if (tiles > 1) look(std::integral_constant<uint32_t, 1>{}, 1);
         delta = rl * seq_sum_halves(sum);
         __syncthreads();
-        issue(0, 0);
+        start_walk();
     }
-    for (int t = 0; t < tiles; ++t) {
-        const uint32_t buf = (uint32_t)t & 1u;
-        begin(t, buf, t + 1 < tiles);
-        f32x16 p, dp;
+    f32x16 minus_delta;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) minus_delta[r] = -delta;
+    auto step = [&](auto parity, int t) {
+        constexpr uint32_t B = decltype(parity)::value;
+        begin(t, B);
+        f32x16 s[KS];
+        const Exponent ex = scores(parity, t, s);
         float ds_tile = 0.f, p_tile = 0.f;
-        const int nearest = t * KT - last, furthest = t * KT + KT - 1 - first;  // distances of the tile
-        const int kind = furthest <= -far ? kBelow : nearest >= far ? kAbove : nearest > -far && furthest < far ? kInner : kBorder;
+        // distances of the tile: all at or beyond an end, or some of them
+        const int nearest = t * KT - last, furthest = t * KT + KT - 1 - first;
+        const bool border = TABLE && t >= near0 && t < near1 && (nearest <= -far || furthest >= far);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            scores(t, buf, k, p, dp);
+            f32x16 ds = minus_delta;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) dp[r] = p[r] * (dp[r] - delta);
+            for (int x = 0; x < NC; ++x) ds = seq_dot<T>(row_reader.read(base + B * 2u * kTile + kTile, x, k), gf[x], ds);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) ds_tile = plain_sum(ds_tile, dp[r]);
-            if constexpr (TABLE) {
-                if (kind == kBelow || kind == kAbove) {
+            for (int r = 0; r < 16; ++r) {
+                s[k][r] = __builtin_amdgcn_exp2f(fmaf(s[k][r], ex.mul, ex.minus));
+                ds[r] *= s[k][r];
+                ds_tile = plain_sum(ds_tile, ds[r]);
+                if constexpr (TABLE) p_tile += s[k][r];
+            }
+            column_reader.accumulate(dq, base + B * 2u * kTile, k, ds);
+            if (border) {
+                int d = t * KT + 4 * (int)hi - pos;
+                asm volatile("" : "+v"(d));  // a branch, not selections in every tile
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) p_tile += p[r];
-                } else if (kind == kBorder) {
-                    const int d = t * KT + 4 * (int)hi - pos;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int x = d + 32 * k + 8 * (r / 4) + r % 4;
-                        if (x <= -far) { ds_below += dp[r]; p_below += p[r]; }
-                        else if (x >= far) { ds_above += dp[r]; p_above += p[r]; }
-                    }
+                for (int r = 0; r < 16; ++r) {
+                    const int x = d + 32 * k + 8 * (r / 4) + r % 4;
+                    ds_below += x <= -far ? ds[r] : 0.f;
+                    p_below += x <= -far ? s[k][r] : 0.f;
+                    ds_above += x >= far && x > -far ? ds[r] : 0.f;
+                    p_above += x >= far && x > -far ? s[k][r] : 0.f;
                 }
             }
-            column_reader.accumulate(dq, base + buf * 2u * kTile, k, dp);
         }
         ds_all = plain_sum(ds_all, ds_tile);
         if constexpr (TABLE) {
-            if (kind == kBelow) { ds_below += ds_tile; p_below += p_tile; }
-            else if (kind == kAbove) { ds_above += ds_tile; p_above += p_tile; }
+            const bool is_below = t < near0, is_above = t >= near1;
+            ds_below += is_below ? ds_tile : 0.f;
+            p_below += is_below ? p_tile : 0.f;
+            ds_above += is_above ? ds_tile : 0.f;
+            p_above += is_above ? p_tile : 0.f;
         }
+    };
+    for (int t = 0; t < tiles; t += 2) {
+        step(std::integral_constant<uint32_t, 0>{}, t);
+        if (t + 1 < tiles) step(std::integral_constant<uint32_t, 1>{}, t + 1);
     }
     // The dS of a row add up to zero; what they add up to is what delta is off by, times the row's weights.  dQ of 16-bit data keeps
     // it (it is below the roundings of dS); dK and the sums by distance, which are not rounded, get the better delta.
@@ -308,7 +374,7 @@ __global__ void __launch_bounds__(256) seq_table_kernel(SeqArgs a, BackPlan plan
             x.klen = seq_length(a.k_len, x.n, a.Lk);
             x.start = seq_start(a.q_start, x.n);
             x.j0 = x.start + x.i0 + kTableKeys * offset;
-            if (x.i0 < x.qlen && x.j0 < x.klen && x.j0 + kTableKeys > 0) break;
+            if (x.i0 < x.qlen && x.j0 < x.klen && x.j0 + kTableKeys > 0 && !seq_lone(a.causal, x.start, x.qlen, x.klen)) break;
         }
         return x;
     };
@@ -318,13 +384,11 @@ __global__ void __launch_bounds__(256) seq_table_kernel(SeqArgs a, BackPlan plan
         const int rows = x.klen - from < KT + j - from ? x.klen - from : KT + j - from;
         const size_t at = (((size_t)x.n * a.Lk + from) * a.ldk + (size_t)kv * D) * E;
         const uint32_t bytes = rows > 0 ? (uint32_t)(rows - 1) * kld + RB : 0u, shift = (uint32_t)(from - j) * kld;
-        const u32x4 ks = lds_source(static_cast<const char*>(a.k) + at, bytes), vs = lds_source(static_cast<const char*>(a.v) + at, bytes);
-        const uint32_t to = base + buf * 2u * kTile;
+        SeqLoader<RB, KT, 4> shifted = load;
 #pragma unroll
-        for (int i = 0; i < load.kLoads; ++i) {
-            load_to_lds(ks, load.off[i] - shift, to + load.to + (uint32_t)i * 4096u);
-            load_to_lds(vs, load.off[i] - shift, to + kTile + load.to + (uint32_t)i * 4096u);
-        }
+        for (int i = 0; i < load.kLoads; ++i) shifted.off[i] -= shift;
+        shifted.issue(reinterpret_cast<uintptr_t>(a.k) + at, bytes, base + buf * 2u * kTile);
+        shifted.issue(reinterpret_cast<uintptr_t>(a.v) + at, bytes, base + buf * 2u * kTile + kTile);
     };
 
     Block now = find(chunk);
@@ -472,9 +536,10 @@ constexpr float seq_lift() { return __is_same(T, SeqF16) ? 6.f : 0.f; }
 template <class T, int D, int W, int QT>
 __global__ void __launch_bounds__(64 * W) seq_keys_kernel(SeqArgs a, BackPlan plan) {
     constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, QS = QT / 32;
-    constexpr uint32_t kTile = QT * RB;
+    constexpr uint32_t kTile = QT * RB, kStat = 16u * QT;  // of each row: exponent's addend, reference, logarithm of the sum, minus delta
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const uint32_t base = lds_offset(lds), stat_at = base + 4u * kTile, bias_at = stat_at + 2u * 12u * QT, bias_bytes = 4u * plan.bias_entries;
+    const uint32_t base = lds_offset(lds), stat_at = base + 4u * kTile, zero_at = stat_at + 2u * kStat, bias_at = zero_at + 4u * QT + 16u,
+                   bias_bytes = 4u * plan.bias_entries;
     const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t hi = lane >> 5, c = lane & 31u;
 
@@ -501,17 +566,20 @@ __global__ void __launch_bounds__(64 * W) seq_keys_kernel(SeqArgs a, BackPlan pl
     SeqColumnReader<T, D> column_reader;
     column_reader.init(hi, c);
 
-    int g = 0, t = q0;  // of the tile that is loaded next
+    // a tile: of the queries, and which of the heads
+    struct Place { int g, t; };
+    auto behind = [&](Place x) { return x.t + 1 == q1 ? Place{x.g + 1, q0} : Place{x.g, x.t + 1}; };
+    Place now{0, q0};
     if (each > 0) {
-        g = s0 / each;
-        t = q0 + s0 - g * each;
+        now.g = s0 / each;
+        now.t = q0 + s0 - now.g * each;
     }
-    auto issue = [&](uint32_t buf) {
-        const int head = kv * plan.group + g;
-        const size_t row = (size_t)n * a.Lq + (size_t)t * QT;
+    auto issue = [&](const Place& x, uint32_t buf) {
+        const int head = kv * plan.group + x.g;
+        const size_t row = (size_t)n * a.Lq + (size_t)x.t * QT;
         const uint32_t to = base + buf * 2u * kTile;
-        load_q.issue(static_cast<const char*>(a.q) + (row * a.ldq + (size_t)head * D) * E, qlen - t * QT, qld, to);
-        load_g.issue(static_cast<const char*>(a.d_o) + (row * a.ldg + (size_t)head * D) * E, qlen - t * QT, gld, to + kTile);
+        load_q.issue(reinterpret_cast<uintptr_t>(a.q) + (row * a.ldq + (size_t)head * D) * E, seq_tile_bytes<RB>(qlen - x.t * QT, QT, qld), to);
+        load_g.issue(reinterpret_cast<uintptr_t>(a.d_o) + (row * a.ldg + (size_t)head * D) * E, seq_tile_bytes<RB>(qlen - x.t * QT, QT, gld), to + kTile);
     };
 
     u32x4 kf[NC], vf[NC];
@@ -540,83 +608,179 @@ __global__ void __launch_bounds__(64 * W) seq_keys_kernel(SeqArgs a, BackPlan pl
     }
     const int far = a.far;
     const float scale = a.scale * kLog2e;
-    if (s0 < s1) issue(0);
-    for (int s = s0; s < s1; ++s) {
-        const uint32_t buf = (uint32_t)(s - s0) & 1u, qt = base + buf * 2u * kTile, gt = qt + kTile, stat = stat_at + buf * (12u * QT);
-        const int head = kv * plan.group + g, i0 = t * QT, first = start + i0;
-        const float* const table = a.table ? a.table + (size_t)head * a.nb : nullptr;
-        const bool near = table && j0 - (first + QT - 1) < far && j_last - first > -far;
-        if (near)
-            for (uint32_t e = threadIdx.x; e < (uint32_t)(QT + 32 * W - 1); e += 64u * W)
-                seq_lds_put(bias_at + buf * bias_bytes + 4u * e, seq_bias_at(table, a.buckets, a.nb, far, j_last - first - (int)e));
-        for (uint32_t e = threadIdx.x; e < (uint32_t)QT; e += 64u * W) {
-            float ref = 0.f, l = kDead, delta = 0.f;
-            if (i0 + (int)e < qlen) {
-                const size_t row = ((size_t)n * a.H + head) * a.Lq + i0 + e;
-                const f32x2 x = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
-                if (x[0] != -__builtin_inff()) {
-                    ref = x[0];
-                    l = x[1] - seq_lift<T>();
-                    delta = plan.delta[row];
-                }
-            }
-            seq_lds_put(stat + 4u * e, ref);
-            seq_lds_put(stat + 4u * (QT + e), l);
-            seq_lds_put(stat + 4u * (2 * QT + e), delta);
+    for (uint32_t e = threadIdx.x; e < (uint32_t)QT; e += 64u * W) seq_lds_put(zero_at + 4u * e, 0.f);
+
+    // tiles of queries as the keys of this block see them: near0 .. near1 - 1 with distances between -far and far (those before are at or
+    // beyond far, those behind at or beyond -far); causality shuts pairs out up to mask1 - 1, the end of the keys in every tile
+    int near0 = 0, near1 = 0, mask1 = a.causal ? seq_tiles_up_to(j_last - start, QT) : 0;
+    if (a.table) {
+        near0 = seq_tiles_up_to(j0 - start - far - QT + 1, QT);
+        near1 = seq_tiles_up_to(j_last - start + far, QT);
+        if (near1 < near0) near1 = near0;
+    }
+    if (j_last >= klen) mask1 = 1 << 30;
+    const int from_row = j < klen ? (a.causal ? j - start : -(1 << 30)) : 1 << 30;  // query from which on the lane's key is seen
+    float below = 0.f, above = 0.f;
+    bool modest = true;
+    int ends_of = -1;  // the head whose they are
+    auto ends = [&](int g) {
+        if (!a.table || g == ends_of) return;
+        ends_of = g;
+        const float* const row = a.table + (size_t)(kv * plan.group + g) * a.nb;
+        below = seq_bias_at(row, a.buckets, a.nb, far, -far);
+        above = seq_bias_at(row, a.buckets, a.nb, far, far);
+        modest = fabsf(below) < 256.f && fabsf(above) < 256.f;
+    };
+
+    // a thread's row of the statistics, and entry of the bias, of the tiles to come
+    f32x2 stat_ahead = {0.f, 0.f};
+    float delta_ahead = 0.f;
+    bool row_ahead = false;
+    auto fetch_stats = [&](const Place& x) {
+        const int i = x.t * QT + (int)threadIdx.x;
+        row_ahead = threadIdx.x < (uint32_t)QT && i < qlen;
+        if (row_ahead) {
+            const size_t row = ((size_t)n * a.H + kv * plan.group + x.g) * a.Lq + i;
+            stat_ahead = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
+            delta_ahead = plan.delta[row];
         }
-        if (++t == q1) {
-            t = q0;
-            ++g;
+    };
+    SeqBiasAhead ahead = {0u, 0u, 0.f};
+    auto is_near = [&](int t) { return t >= near0 && t < near1; };
+    auto find = [&](const Place& x) { if (W == 4 && is_near(x.t)) ahead.find(a.buckets, far, j_last - start - x.t * QT - (int)threadIdx.x); };
+    auto fetch = [&](const Place& x) { if (W == 4 && is_near(x.t)) ahead.fetch(a.table + (size_t)(kv * plan.group + x.g) * a.nb, a.nb); };
+
+    Place next = behind(now);
+    if (s0 < s1) {
+        issue(now, 0);
+        fetch_stats(now);
+        find(now);
+        fetch(now);
+        if (s0 + 1 < s1) find(next);
+    }
+    auto step = [&](auto parity, int s) {
+        constexpr uint32_t B = decltype(parity)::value;
+        const uint32_t qt = base + B * 2u * kTile, gt = qt + kTile, stat = stat_at + B * kStat;
+        const bool near = is_near(now.t);
+        ends(now.g);
+        const float flat = now.t < near0 ? above : below;
+        if (near) {
+            if constexpr (W == 4) {
+                if (threadIdx.x < (uint32_t)(QT + 32 * W - 1)) seq_lds_put(bias_at + B * bias_bytes + 4u * threadIdx.x, ahead.get(a.nb));
+            } else {
+                for (uint32_t e = threadIdx.x; e < (uint32_t)(QT + 32 * W - 1); e += 64u * W)
+                    seq_lds_put(bias_at + B * bias_bytes + 4u * e,
+                                seq_bias_at(a.table + (size_t)(kv * plan.group + now.g) * a.nb, a.buckets, a.nb, far, j_last - start - now.t * QT - (int)e));
+            }
+        }
+        if (threadIdx.x < (uint32_t)QT) {
+            const bool live = row_ahead && stat_ahead[0] != -__builtin_inff();
+            const float ref = live ? stat_ahead[0] : 0.f, l = live ? stat_ahead[1] - seq_lift<T>() : kDead;
+            seq_lds_put(stat + 4u * threadIdx.x, flat - (ref + l));
+            seq_lds_put(stat + 4u * (QT + threadIdx.x), ref);
+            seq_lds_put(stat + 4u * (2 * QT + threadIdx.x), l);
+            seq_lds_put(stat + 4u * (3 * QT + threadIdx.x), live ? -delta_ahead : 0.f);
+        }
+        // Reference and sum as one number, for the exponent's one fused operation: of 16-bit data, whose own rounding is the larger one while the
+        // reference is not
+        if (wave == 0) {
+            const bool large = __any(threadIdx.x < (uint32_t)QT && row_ahead && fabsf(stat_ahead[0]) > 1024.f && stat_ahead[0] != -__builtin_inff());
+            if (lane == 0) seq_lds_put(zero_at + 4u * QT + 4u * B, large ? 1.f : 0.f);
         }
         lds_loads_done();
         __syncthreads();
-        if (s + 1 < s1) issue(buf ^ 1u);
+        const Place after = behind(next);
+        if (s + 1 < s1) {
+            fetch_stats(next);
+            fetch(next);
+            if (s + 2 < s1) find(after);
+            issue(next, B ^ 1u);
+        }
+        const int first = now.t * QT;
+        bool plain = !__is_same(T, SeqF32) && modest && !near && now.t >= mask1;
+        if (plain) plain = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, seq_lds_f32(zero_at + 4u * QT + 4u * B))) == 0;
 
-        const float far_bias = table && !near ? seq_bias_at(table, a.buckets, a.nb, far, j_last - first <= -far ? -far : far) : 0.f;
-        const bool masked = j_last >= klen || (a.causal && j_last > first);
-        const int from_row = j < klen ? (a.causal ? j - first : -(1 << 30)) : 1 << 30;  // rows from which on the lane's key is seen
+        f32x16 p[QS];
 #pragma unroll
         for (int k = 0; k < QS; ++k) {
-            f32x16 p, dp;
-            seq_zero(p);
-            seq_zero(dp);
+            seq_zero(p[k]);
 #pragma unroll
-            for (int x = 0; x < NC; ++x) p = seq_dot<T>(row_reader.read(qt, x, k), kf[x], p);
-#pragma unroll
-            for (int x = 0; x < NC; ++x) dp = seq_dot<T>(row_reader.read(gt, x, k), vf[x], dp);
+            for (int x = 0; x < NC; ++x) p[k] = seq_dot<T>(row_reader.read(qt, x, k), kf[x], p[k]);
+        }
+        if (!plain) {
             if (near) {
-                const uint32_t my_bias = bias_at + buf * bias_bytes + 4u * ((uint32_t)(j_last - j) + 4u * hi);
+                const uint32_t my_bias = bias_at + B * bias_bytes + 4u * ((uint32_t)(j_last - j) + 4u * hi);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) p[r] = fmaf(p[r], scale, seq_lds_f32(my_bias + 4u * (32 * k + 8 * (r / 4) + r % 4)));
+                for (int k = 0; k < QS; ++k)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) p[k][r] = fmaf(p[k][r], scale, seq_lds_f32(my_bias + 4u * (32 * k + 8 * (r / 4) + r % 4)));
             } else {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) p[r] = fmaf(p[r], scale, far_bias);
-            }
-            if (masked) {
-                const int room = from_row - 4 * (int)hi;
+                for (int k = 0; k < QS; ++k)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) p[r] = 32 * k + 8 * (r / 4) + r % 4 >= room ? p[r] : -__builtin_inff();
+                    for (int r = 0; r < 16; ++r) p[k][r] = fmaf(p[k][r], scale, flat);
             }
+            if (now.t < mask1) {
+                const int room = from_row - first - 4 * (int)hi;
+#pragma unroll
+                for (int k = 0; k < QS; ++k)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) p[k][r] = 32 * k + 8 * (r / 4) + r % 4 >= room ? p[k][r] : -__builtin_inff();
+            }
+            // the reference first: it cancels against the score however large a bias made both
+#pragma unroll
+            for (int k = 0; k < QS; ++k)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t rows = stat + 4u * (QT + 32 * k + 8 * q) + 16u * hi;
+                    const f32x4 ref = seq_lds_f32x4(rows), l = seq_lds_f32x4(rows + 4u * QT);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[k][4 * q + e] = (p[k][4 * q + e] - ref[e]) - l[e];
+                }
+        }
+        const float mul = plain ? scale : 1.f;
+        const uint32_t addend = plain ? stat : zero_at;
+#pragma unroll
+        for (int k = 0; k < QS; ++k) {
+            f32x16 ds;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const uint32_t rows = stat + 4u * (32 * k + 8 * q) + 16u * hi;
-                const f32x4 ref = seq_lds_f32x4(rows), l = seq_lds_f32x4(rows + 4u * QT), delta = seq_lds_f32x4(rows + 8u * QT);
+                const f32x4 minus_delta = seq_lds_f32x4(stat + 4u * (3 * QT + 32 * k + 8 * q) + 16u * hi);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ds[4 * q + e] = minus_delta[e];
+            }
+#pragma unroll
+            for (int x = 0; x < NC; ++x) ds = seq_dot<T>(row_reader.read(gt, x, k), vf[x], ds);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4 add = seq_lds_f32x4(addend + 4u * (32 * k + 8 * q) + 16u * hi);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int r = 4 * q + e;
-                    // the reference first: it cancels against the score however large a bias made both
-                    p[r] = __builtin_amdgcn_exp2f((p[r] - ref[e]) - l[e]);
-                    dp[r] = p[r] * (dp[r] - delta[e]);
+                    p[k][r] = __builtin_amdgcn_exp2f(fmaf(p[k][r], mul, add[e]));
+                    ds[r] *= p[k][r];
                 }
             }
-            column_reader.accumulate(dv, gt, k, p);
-            column_reader.accumulate(dk, qt, k, dp);
+            column_reader.accumulate(dv, gt, k, p[k]);
+            column_reader.accumulate(dk, qt, k, ds);
         }
+        now = next;
+        next = after;
+    };
+    for (int s = s0; s < s1; s += 2) {
+        step(std::integral_constant<uint32_t, 0>{}, s);
+        if (s + 1 < s1) step(std::integral_constant<uint32_t, 1>{}, s + 1);
     }
 
     if (j >= a.Lk) return;
     const float down = __builtin_amdgcn_exp2f(-seq_lift<T>());
+    const bool lone = seq_lone(a.causal, start, qlen, klen);
+    const float fk = lone ? 0.f : a.scale * down;
     const size_t row = (size_t)n * a.Lk + j;
+    if (lone) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) seq_zero(dk[b]);
+    }
     if (plan.splits > 1) {
         const size_t values = (size_t)a.N * a.Lk * a.KV * D, to = (row * a.KV + kv) * D;
         float* const into = plan.part_kv + (size_t)split * 2 * values + to;
@@ -633,7 +797,6 @@ __global__ void __launch_bounds__(64 * W) seq_keys_kernel(SeqArgs a, BackPlan pl
     const size_t to = (row * a.lddk + (size_t)kv * D) * E;
     char* const dkp = static_cast<char*>(a.dk) + to;
     char* const dvp = static_cast<char*>(a.dv) + to;
-    const float fk = a.scale * down;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -685,7 +848,7 @@ hipError_t launch_table(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
 
 template <class T, int D, int W>
 hipError_t launch(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
-    constexpr int KT = seq_forward_keys(D * SeqSize<T>::value, W);
+    constexpr int KT = seq_backward_rows(D * SeqSize<T>::value);
     const size_t tiles = 4 * (size_t)KT * D * SeqSize<T>::value, bias = 2 * sizeof(float) * plan.bias_entries;
     hipError_t e = a.dtable ? start(&seq_rows_kernel<T, D, W, KT, true>, dim3(plan.row_grid), 64 * W, tiles + bias, s, a, plan)
                             : start(&seq_rows_kernel<T, D, W, KT, false>, dim3(plan.row_grid), 64 * W, tiles + bias, s, a, plan);
@@ -694,7 +857,7 @@ hipError_t launch(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
         e = launch_table<T, D>(a, plan, s);
         if (e != hipSuccess) return e;
     }
-    e = start(&seq_keys_kernel<T, D, W, KT>, dim3(plan.key_grid), 64 * W, tiles + 24 * KT + bias, s, a, plan);
+    e = start(&seq_keys_kernel<T, D, W, KT>, dim3(plan.key_grid), 64 * W, tiles + 36 * KT + 16 + bias, s, a, plan);
     if (e != hipSuccess || plan.splits == 1 || a.Lk == 0) return e;
     const size_t threads = (size_t)a.N * a.Lk * a.KV * D / 2, blocks = (threads + 255) / 256;
     hipLaunchKernelGGL((seq_join_keys_kernel<T, D>), dim3((unsigned)blocks), dim3(256), 0, s, a, plan);
@@ -716,7 +879,7 @@ bool back_plan(const SeqArgs& a, BackPlan& p) {
     const int cus = cu_count();
     p.group = a.H / a.KV;
     p.waves = a.Lq <= 32 && a.Lk <= 32 ? 1 : 4;
-    const int KT = seq_forward_keys(a.D * (a.dtype == 0 ? 4 : 2), p.waves), block = 32 * p.waves;
+    const int KT = seq_backward_rows(a.D * (a.dtype == 0 ? 4 : 2)), block = 32 * p.waves;
     p.row_blocks = (a.Lq + block - 1) / block;
     p.key_blocks = (a.Lk + block - 1) / block;
     p.row_waves = (a.Lq + 31) / 32;

@@ -7,6 +7,8 @@
 // tiles through LDS, two of each so that the next are on their way during the products.
 #include "fwa_sequence.h"
 
+#include <type_traits>
+
 namespace fwa {
 namespace {
 
@@ -60,11 +62,17 @@ __global__ void __launch_bounds__(64 * W) seq_forward_kernel(SeqArgs a, SeqPlan 
     row_reader.init(hi, c);
     SeqColumnReader<T, D> column_reader;
     column_reader.init(hi, c);
-    auto issue = [&](int t) {
-        const size_t row = (size_t)t * KT;
-        const uint32_t to = base + ((t - t0) & 1) * 2u * kTile;
-        load.issue(kp + row * kld, klen - t * KT, kld, to);
-        load.issue(vp + row * kld, klen - t * KT, kld, to + kTile);
+    // addresses of the next tile to ask for, and the rows from there on
+    const size_t skip = (size_t)t0 * KT * kld;
+    uintptr_t next_k = reinterpret_cast<uintptr_t>(kp) + skip, next_v = reinterpret_cast<uintptr_t>(vp) + skip;
+    int next_rows = klen - t0 * KT;
+    auto issue = [&](uint32_t buf) {
+        const uint32_t bytes = seq_tile_bytes<RB>(next_rows, KT, kld);
+        load.issue(next_k, bytes, base + buf * 2u * kTile);
+        load.issue(next_v, bytes, base + buf * 2u * kTile + kTile);
+        next_k += KT * kld;
+        next_v += KT * kld;
+        next_rows -= KT;
     };
 
     u32x4 qf[NC];
@@ -74,6 +82,12 @@ __global__ void __launch_bounds__(64 * W) seq_forward_kernel(SeqArgs a, SeqPlan 
         const char* const qp = static_cast<const char*>(a.q) + (((size_t)n * a.Lq + i) * a.ldq + (size_t)head * D) * E + 16u * hi;
 #pragma unroll
         for (int s = 0; s < NC; ++s) qf[s] = *reinterpret_cast<const u32x4*>(qp + 32 * s);
+        // a negative scale goes into the queries, so that the largest product is the largest score
+        if (a.scale < 0.f) {
+            constexpr uint32_t kSign = __is_same(T, SeqF32) ? 0x80000000u : 0x80008000u;
+#pragma unroll
+            for (int s = 0; s < NC; ++s) qf[s] ^= kSign;
+        }
     }
     // Rows of the last tile that no load fills hold zeros, or the finite rows of an earlier tile: their weights are zero, and zero times
     // whatever else LDS may hold need not be.
@@ -81,11 +95,21 @@ __global__ void __launch_bounds__(64 * W) seq_forward_kernel(SeqArgs a, SeqPlan 
         for (uint32_t o = threadIdx.x * 16u; o < 4u * kTile; o += 64u * W * 16u) *reinterpret_cast<u32x4*>(lds + o) = u32x4{0u, 0u, 0u, 0u};
         __syncthreads();
     }
-    if (t0 < t1) issue(t0);
+    if (t0 < t1) issue(0);
 
     const float* const table = a.table ? a.table + (size_t)head * a.nb : nullptr;
     const int far = a.far;
     const float below = table ? seq_bias_at(table, a.buckets, a.nb, far, -far) : 0.f, above = table ? seq_bias_at(table, a.buckets, a.nb, far, far) : 0.f;
+    // A bias that is one value for the tile joins the reference in the exponent's one fused operation; a large one, beside which the score would
+    // lose its bits in the sum and not in the difference, is added first, as everywhere else.
+    const bool modest = !__any(!(fabsf(below) < 256.f && fabsf(above) < 256.f));
+    // tiles whose distances are not all cut off: near0 .. near1 - 1; tiles with a pair that a length or causality shuts out: from mask0 on
+    int near0 = 0, near1 = 0, mask0 = klen / KT;
+    seq_near_tiles(a.table != nullptr, first, last, far, KT, near0, near1);
+    if (a.causal && first < klen) {
+        const int to = first + 1 > 0 ? (first + 1) / KT : 0;
+        mask0 = to < mask0 ? to : mask0;
+    }
     const uint32_t span = (uint32_t)(KT + span_rows - 1), entries = plan.packed ? span * G : span, bias_bytes = 4u * plan.bias_entries;
     const uint32_t my_bias = bias_at + 4u * ((uint32_t)g * span + (uint32_t)(last - pos) + 4u * hi);
     const float* const group_table = a.table + (size_t)(plan.packed ? hk * G : hk) * a.nb;
@@ -95,21 +119,39 @@ __global__ void __launch_bounds__(64 * W) seq_forward_kernel(SeqArgs a, SeqPlan 
     for (int b = 0; b < NB; ++b) seq_zero(o[b]);
     float m = -__builtin_inff(), l = 0.f;
     const int lim = a.causal && pos + 1 < klen ? pos + 1 : klen;
-    const float scale = a.scale * kLog2e;
+    const float scale = fabsf(a.scale) * kLog2e;
 
-    for (int t = t0; t < t1; ++t) {
-        const uint32_t buf = (uint32_t)(t - t0) & 1u, kt = base + buf * 2u * kTile, vt = kt + kTile;
+    SeqBiasAhead ahead = {0u, 0u, 0.f};
+    if constexpr (W == 4) {
+        if (t0 >= near0 && t0 < near1) {
+            ahead.find(a.buckets, far, t0 * KT - last + (int)threadIdx.x);
+            ahead.fetch(group_table, a.nb);
+        }
+        if (t0 + 1 >= near0 && t0 + 1 < near1) ahead.find(a.buckets, far, (t0 + 1) * KT - last + (int)threadIdx.x);
+    }
+    auto step = [&](auto parity, int t) {
+        constexpr uint32_t B = decltype(parity)::value;
+        const uint32_t kt = base + B * 2u * kTile, vt = kt + kTile;
         const int j0 = t * KT;
-        const bool near = a.table && j0 - last < far && j0 + KT - 1 - first > -far;
-        if (near)
-            for (uint32_t e = threadIdx.x; e < entries; e += 64u * W) {
-                const uint32_t ge = plan.packed ? e / span : 0u;
-                seq_lds_put(bias_at + buf * bias_bytes + 4u * e,
-                            seq_bias_at(group_table + (size_t)ge * a.nb, a.buckets, a.nb, far, j0 - last + (int)(e - ge * span)));
+        const bool near = t >= near0 && t < near1;
+        if (near) {
+            if constexpr (W == 4) {
+                if (threadIdx.x < entries) seq_lds_put(bias_at + B * bias_bytes + 4u * threadIdx.x, ahead.get(a.nb));
+            } else {
+                for (uint32_t e = threadIdx.x; e < entries; e += 64u * W) {
+                    const uint32_t ge = plan.packed ? e / span : 0u;
+                    seq_lds_put(bias_at + B * bias_bytes + 4u * e,
+                                seq_bias_at(group_table + (size_t)ge * a.nb, a.buckets, a.nb, far, j0 - last + (int)(e - ge * span)));
+                }
             }
+        }
         lds_loads_done();
         __syncthreads();
-        if (t + 1 < t1) issue(t + 1);
+        if constexpr (W == 4) {
+            if (t + 1 >= near0 && t + 1 < near1) ahead.fetch(group_table, a.nb);
+            if (t + 2 >= near0 && t + 2 < near1) ahead.find(a.buckets, far, j0 + 2 * KT - last + (int)threadIdx.x);
+        }
+        if (t + 1 < t1) issue(B ^ 1u);
 
         f32x16 s[KS];
 #pragma unroll
@@ -118,31 +160,37 @@ __global__ void __launch_bounds__(64 * W) seq_forward_kernel(SeqArgs a, SeqPlan 
 #pragma unroll
             for (int x = 0; x < NC; ++x) s[k] = seq_dot<T>(row_reader.read(kt, x, k), qf[x], s[k]);
         }
-        if (near) {
+        // exponent of a weight: s mul + add - reference
+        const float flat = t < near0 ? below : above;
+        const bool plain = modest && !near && t < mask0;
+        if (!plain) {
+            if (near) {
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
+                for (int k = 0; k < KS; ++k)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[k][r] = fmaf(s[k][r], scale, seq_lds_f32(my_bias + buf * bias_bytes + 4u * (32 * k + 8 * (r / 4) + r % 4)));
-        } else {
-            const float b = j0 + KT - 1 - first <= -far ? below : above;
+                    for (int r = 0; r < 16; ++r) s[k][r] = fmaf(s[k][r], scale, seq_lds_f32(my_bias + B * bias_bytes + 4u * (32 * k + 8 * (r / 4) + r % 4)));
+            } else {
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
+                for (int k = 0; k < KS; ++k)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[k][r] = fmaf(s[k][r], scale, b);
+                    for (int r = 0; r < 16; ++r) s[k][r] = fmaf(s[k][r], scale, flat);
+            }
+            if (t >= mask0) {
+                const int room = lim - j0 - 4 * (int)hi;
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[k][r] = 32 * k + 8 * (r / 4) + r % 4 < room ? s[k][r] : -__builtin_inff();
+            }
         }
-        if (j0 + KT > klen || (a.causal && j0 + KT - 1 > first)) {
-            const int room = lim - j0 - 4 * (int)hi;
-#pragma unroll
-            for (int k = 0; k < KS; ++k)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[k][r] = 32 * k + 8 * (r / 4) + r % 4 < room ? s[k][r] : -__builtin_inff();
-        }
+        const float mul = plain ? scale : 1.f, add = plain ? flat : 0.f;
         float top = s[0][0];
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[k][r]);
-        top = seq_max_halves(top);
+        top = fmaf(seq_max_halves(top), mul, add);
+        // the reference follows the largest score so far
         if (__any(top > m + kSlack)) {
             const float to = top > m + kSlack ? top : m, f = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
             m = to;
@@ -152,16 +200,20 @@ __global__ void __launch_bounds__(64 * W) seq_forward_kernel(SeqArgs a, SeqPlan 
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[b][r] *= f;
         }
-        const float ref = m == -__builtin_inff() ? 0.f : m;
+        const float minus = m == -__builtin_inff() ? add : add - m;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[k][r] = __builtin_amdgcn_exp2f(s[k][r] - ref);
+                s[k][r] = __builtin_amdgcn_exp2f(fmaf(s[k][r], mul, minus));
                 l += s[k][r];
             }
             column_reader.accumulate(o, vt, k, s[k]);
         }
+    };
+    for (int t = t0; t < t1; t += 2) {
+        step(std::integral_constant<uint32_t, 0>{}, t);
+        if (t + 1 < t1) step(std::integral_constant<uint32_t, 1>{}, t + 1);
     }
 
     l = seq_sum_halves(l);
