@@ -208,14 +208,18 @@ __device__ __forceinline__ float seq_bias_at(const float* row, const int32_t* bu
 // Positions are int32 of the caller's; beyond these bounds every distance is cut off at `far` and every comparison decided, so they are
 // cut there and sums of a position and a row cannot overflow.
 constexpr int kSeqFarthest = 1 << 29;
+// (Read through the constant address space: no kernel writes them, and the scalar unit's loads do not queue behind a tile's.)
+__device__ __forceinline__ int seq_constant(const int32_t* p, long long n) {
+    return ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)p)[n];
+}
 __device__ __forceinline__ int seq_length(const int32_t* lengths, long long n, int most) {
     if (lengths == nullptr) return most;
-    const int x = lengths[n];
+    const int x = seq_constant(lengths, n);
     return x < 0 ? 0 : (x > most ? most : x);
 }
 __device__ __forceinline__ int seq_start(const int32_t* starts, long long n) {
     if (starts == nullptr) return 0;
-    const int x = starts[n];
+    const int x = seq_constant(starts, n);
     return x < -kSeqFarthest ? -kSeqFarthest : (x > kSeqFarthest ? kSeqFarthest : x);
 }
 

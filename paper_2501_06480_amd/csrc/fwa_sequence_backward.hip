@@ -353,30 +353,34 @@ __global__ void __launch_bounds__(256) seq_table_kernel(SeqArgs a, BackPlan plan
     SeqLoader<RB, KT, 4> load;
     load.init(wave, lane, kld);
 
-    f32x16 sum[2], b[2];
+    // the bias of a place: key - row = e - 127 in the block
+    const uint32_t bias_at = base + 4u * kTile;
+    if (threadIdx.x < kLine - 1)
+        seq_lds_put(bias_at + 4u * threadIdx.x, seq_bias_at(table, a.buckets, a.nb, far, kTableKeys * offset + (int)threadIdx.x - kTableRows + 1));
+    const uint32_t my_bias = bias_at + 4u * (4u * hi + 127u - 32u * wave - c);
+    f32x16 sum[2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        seq_zero(sum[k]);
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-            b[k][r] = seq_bias_at(table, a.buckets, a.nb, far, kTableKeys * offset + 32 * k + 8 * (r / 4) + 4 * (int)hi + r % 4 - 32 * (int)wave - (int)c);
-    }
+    for (int k = 0; k < 2; ++k) seq_zero(sum[k]);
 
     // the next block of the chunk (every plan.chunks-th: sequences differ in length) with a pair in it, and its sizes
     const int end = plan.items;
-    struct Block { int item, n, i0, qlen, klen, start, j0; };
+    struct Block { int n, i0, qlen, klen, start, j0; };
+    auto at_item = [&](int item) {
+        Block x;
+        x.n = (int)fastdiv((uint32_t)item, plan.by_table_blocks);
+        x.i0 = kTableRows * (item - x.n * (int)plan.by_table_blocks.d);
+        x.qlen = seq_length(a.q_len, x.n, a.Lq);
+        x.klen = seq_length(a.k_len, x.n, a.Lk);
+        x.start = seq_start(a.q_start, x.n);
+        x.j0 = x.start + x.i0 + kTableKeys * offset;
+        return x;
+    };
     auto find = [&](int item) {
-        Block x{item, 0, 0, 0, 0, 0, 0};
-        for (; x.item < end; x.item += plan.chunks) {
-            x.n = (int)fastdiv((uint32_t)x.item, plan.by_table_blocks);
-            x.i0 = kTableRows * (x.item - x.n * (int)plan.by_table_blocks.d);
-            x.qlen = seq_length(a.q_len, x.n, a.Lq);
-            x.klen = seq_length(a.k_len, x.n, a.Lk);
-            x.start = seq_start(a.q_start, x.n);
-            x.j0 = x.start + x.i0 + kTableKeys * offset;
+        for (; item < end; item += plan.chunks) {
+            const Block x = at_item(item);
             if (x.i0 < x.qlen && x.j0 < x.klen && x.j0 + kTableKeys > 0 && !seq_lone(a.causal, x.start, x.qlen, x.klen)) break;
         }
-        return x;
+        return __builtin_amdgcn_readfirstlane(item);
     };
     // keys in front of the first one are not loaded either: the rows' offsets count from the first key that exists, and wrap
     auto issue = [&](const Block& x, int half, uint32_t buf) {
@@ -391,42 +395,64 @@ __global__ void __launch_bounds__(256) seq_table_kernel(SeqArgs a, BackPlan plan
         shifted.issue(reinterpret_cast<uintptr_t>(a.v) + at, bytes, base + buf * 2u * kTile + kTile);
     };
 
-    Block now = find(chunk);
     // what no load fills: its scores are shut out, but zero times what LDS may hold has to be zero
     for (uint32_t o = threadIdx.x * 16u; o < 4u * kTile; o += 4096u) *reinterpret_cast<u32x4*>(lds + o) = u32x4{0u, 0u, 0u, 0u};
     __syncthreads();
-    uint32_t buf = 0;
-    if (now.item < end) issue(now, 0, 0);
-    while (now.item < end) {
-        const int i = now.i0 + (int)(32u * wave + c);
-        u32x4 qf[NC], gf[NC];
+
+    // the rows of a block, fetched while the one before is worked on; not the wider ones, which leave room for two waves on a SIMD that way (width 128,
+    // bf16, 2 x 1023 tokens: 33 us with one)
+    constexpr bool AHEAD = RB <= 128;
+    struct Rows { u32x4 q[NC], g[NC]; f32x2 stat; float delta; };
+    auto fetch = [&](const Block& x, Rows& to) {
+        const int i = x.i0 + (int)(32u * wave + c);
+        to.stat = f32x2{-__builtin_inff(), 0.f};
+        to.delta = 0.f;
 #pragma unroll
-        for (int s = 0; s < NC; ++s) qf[s] = gf[s] = u32x4{0u, 0u, 0u, 0u};
-        float ref = 0.f, l = kDead, delta = 0.f;
-        if (i < now.qlen) {
-            const size_t row = ((size_t)now.n * a.H + head) * a.Lq + i, at_row = (size_t)now.n * a.Lq + i, channel = (size_t)head * D;
-            const f32x2 stat = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
-            if (stat[0] != -__builtin_inff()) {
-                ref = stat[0];
-                l = stat[1];
-                delta = plan.delta[row];
-            }
+        for (int s = 0; s < NC; ++s) to.q[s] = to.g[s] = u32x4{0u, 0u, 0u, 0u};
+        if (i < x.qlen) {
+            const size_t row = ((size_t)x.n * a.H + head) * a.Lq + i, at_row = (size_t)x.n * a.Lq + i, channel = (size_t)head * D;
+            to.stat = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
+            to.delta = plan.delta[row];
             const char* const qp = static_cast<const char*>(a.q) + (at_row * a.ldq + channel) * E + 16u * hi;
             const char* const gp = static_cast<const char*>(a.d_o) + (at_row * a.ldg + channel) * E + 16u * hi;
 #pragma unroll
             for (int s = 0; s < NC; ++s) {
-                qf[s] = *reinterpret_cast<const u32x4*>(qp + 32 * s);
-                gf[s] = *reinterpret_cast<const u32x4*>(gp + 32 * s);
+                to.q[s] = *reinterpret_cast<const u32x4*>(qp + 32 * s);
+                to.g[s] = *reinterpret_cast<const u32x4*>(gp + 32 * s);
             }
         }
-        const int pos = now.start + i, lim = l == kDead ? 0 : (a.causal && pos + 1 < now.klen ? pos + 1 : now.klen);
-        const Block next = find(now.item + plan.chunks);
+    };
+    int item = find(chunk);
+    Rows even, odd;
+    if (item < end) {
+        issue(at_item(item), 0, 0);
+        if constexpr (AHEAD) fetch(at_item(item), even);
+    }
+    auto step = [&](auto parity, Rows& mine, Rows& other) {
+        constexpr uint32_t P = decltype(parity)::value;
+        const Block now = at_item(item);
+        if constexpr (!AHEAD) fetch(now, mine);
+        item = find(item + plan.chunks);
+        const bool live = mine.stat[0] != -__builtin_inff();
+        const int pos = now.start + now.i0 + (int)(32u * wave + c);
+        const int lim = !live ? 0 : (a.causal && pos + 1 < now.klen ? pos + 1 : now.klen);
+        // reference and sum as one number where the reference is not large (as in the keys kernel; its rounding is one factor for the row)
+        const bool small = !__any(live && fabsf(mine.stat[0]) > 1024.f);
+        const float ref = live ? mine.stat[0] : 0.f, l = live ? mine.stat[1] : kDead;
+        const float first_off = small ? ref + l : ref, then_off = small ? 0.f : l;
+        const bool inside = now.j0 >= 0 && !__any(now.j0 + kTableKeys > lim);
 #pragma unroll
-        for (int half = 0; half < HALVES; ++half, buf ^= 1u) {
+        for (int half = 0; half < HALVES; ++half) {
+            constexpr uint32_t kStart = HALVES == 1 ? P : 0u;
+            const uint32_t buf = kStart ^ (uint32_t)(half & 1);
             lds_loads_done();
             __syncthreads();
             if (half + 1 < HALVES) issue(now, half + 1, buf ^ 1u);
-            else if (next.item < end) issue(next, 0, buf ^ 1u);
+            else if (item < end) {
+                const Block next = at_item(item);
+                if constexpr (AHEAD) fetch(next, other);
+                issue(next, 0, buf ^ 1u);
+            }
             const uint32_t kt = base + buf * 2u * kTile, vt = kt + kTile;
             const int j0 = now.j0 + half * KT + 4 * (int)hi;
 #pragma unroll
@@ -436,19 +462,32 @@ __global__ void __launch_bounds__(256) seq_table_kernel(SeqArgs a, BackPlan plan
                 seq_zero(p);
                 seq_zero(dp);
 #pragma unroll
-                for (int x = 0; x < NC; ++x) p = seq_dot<T>(row_reader.read(kt, x, k), qf[x], p);
+                for (int x = 0; x < NC; ++x) p = seq_dot<T>(row_reader.read(kt, x, k), mine.q[x], p);
 #pragma unroll
-                for (int x = 0; x < NC; ++x) dp = seq_dot<T>(row_reader.read(vt, x, k), gf[x], dp);
+                for (int x = 0; x < NC; ++x) dp = seq_dot<T>(row_reader.read(vt, x, k), mine.g[x], dp);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int j = j0 + 32 * k + 8 * (r / 4) + r % 4;
-                    const float s = fmaf(p[r], scale, b[block][r]);
-                    const float w = __builtin_amdgcn_exp2f((s - ref) - l), x = w * (dp[r] - delta);
-                    sum[block][r] += j >= 0 && j < lim ? x : 0.f;
+                for (int r = 0; r < 16; ++r)
+                    p[r] = fmaf(p[r], scale, seq_lds_f32(my_bias + 4u * (32 * block + 8 * (r / 4) + r % 4))) - first_off;
+                if (!small) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) p[r] -= then_off;
                 }
+                if (!inside) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int j = j0 + 32 * k + 8 * (r / 4) + r % 4;
+                        p[r] = j >= 0 && j < lim ? p[r] : -__builtin_inff();
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum[block][r] = fmaf(__builtin_amdgcn_exp2f(p[r]), dp[r] - mine.delta, sum[block][r]);
             }
         }
-        now = next;
+    };
+    while (item < end) {
+        step(std::integral_constant<uint32_t, 0>{}, even, odd);
+        if (item >= end) break;
+        step(std::integral_constant<uint32_t, 1>{}, AHEAD ? odd : even, even);
     }
 
     // Diagonals of the wave's two squares of 32: each goes through LDS, rows of keys 33 apart; a lane follows one of the 63.
@@ -460,9 +499,11 @@ __global__ void __launch_bounds__(256) seq_table_kernel(SeqArgs a, BackPlan plan
         for (int r = 0; r < 16; ++r) seq_lds_put(square + 4u * (33u * (8 * (r / 4) + 4 * hi + r % 4) + c), sum[k][r]);
         __syncthreads();
         float x = 0.f;
+#pragma unroll
         for (int cc = 0; cc < 32; ++cc) {
             const int key = (int)lane - 31 + cc;
-            if (key >= 0 && key < 32) x += seq_lds_f32(square + 4u * (uint32_t)(33 * key + cc));
+            const float y = seq_lds_f32(square + 4u * (uint32_t)(33 * (key & 31) + cc));
+            x += key >= 0 && key < 32 ? y : 0.f;
         }
         seq_lds_put(each + 4u * (64u * (2u * wave + k) + lane), x);  // key - row = lane - 31 of the square; lane 63: nothing
         __syncthreads();
@@ -533,12 +574,18 @@ __global__ void __launch_bounds__(256) seq_lines_kernel(SeqArgs a, BackPlan plan
 template <class T>
 constexpr float seq_lift() { return __is_same(T, SeqF16) ? 6.f : 0.f; }
 
+constexpr bool seq_keys_v_in_lds(int row_bytes) { return row_bytes == 256; }
+
 template <class T, int D, int W, int QT>
-__global__ void __launch_bounds__(64 * W) seq_keys_kernel(SeqArgs a, BackPlan plan) {
+__global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) seq_keys_kernel(SeqArgs a, BackPlan plan) {
     constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, QS = QT / 32;
+    // Rows of 256 bytes: the block's V stays in LDS, read again for every tile of queries, where K, V and both gradients would not leave registers
+    // for two waves on a SIMD.
+    constexpr bool VLDS = seq_keys_v_in_lds(RB);
     constexpr uint32_t kTile = QT * RB, kStat = 16u * QT;  // of each row: exponent's addend, reference, logarithm of the sum, minus delta
+    constexpr uint32_t kV = VLDS ? 32u * W * RB : 0u;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const uint32_t base = lds_offset(lds), stat_at = base + 4u * kTile, zero_at = stat_at + 2u * kStat, bias_at = zero_at + 4u * QT + 16u,
+    const uint32_t base = lds_offset(lds), v_at = base + 4u * kTile, stat_at = v_at + kV, zero_at = stat_at + 2u * kStat, bias_at = zero_at + 4u * QT + 16u,
                    bias_bytes = 4u * plan.bias_entries;
     const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t hi = lane >> 5, c = lane & 31u;
@@ -582,9 +629,13 @@ __global__ void __launch_bounds__(64 * W) seq_keys_kernel(SeqArgs a, BackPlan pl
         load_g.issue(reinterpret_cast<uintptr_t>(a.d_o) + (row * a.ldg + (size_t)head * D) * E, seq_tile_bytes<RB>(qlen - x.t * QT, QT, gld), to + kTile);
     };
 
-    u32x4 kf[NC], vf[NC];
+    u32x4 kf[NC], vf[VLDS ? 1 : NC];
 #pragma unroll
-    for (int s = 0; s < NC; ++s) kf[s] = vf[s] = u32x4{0u, 0u, 0u, 0u};
+    for (int s = 0; s < NC; ++s) {
+        kf[s] = u32x4{0u, 0u, 0u, 0u};
+        if constexpr (!VLDS) vf[s] = u32x4{0u, 0u, 0u, 0u};
+    }
+    const uint32_t kld = (uint32_t)(a.ldk * E);
     if (j < klen) {
         const size_t from = (((size_t)n * a.Lk + j) * a.ldk + (size_t)kv * D) * E + 16u * hi;
         const char* const kp = static_cast<const char*>(a.k) + from;
@@ -592,12 +643,19 @@ __global__ void __launch_bounds__(64 * W) seq_keys_kernel(SeqArgs a, BackPlan pl
 #pragma unroll
         for (int s = 0; s < NC; ++s) {
             kf[s] = *reinterpret_cast<const u32x4*>(kp + 32 * s);
-            vf[s] = *reinterpret_cast<const u32x4*>(vp + 32 * s);
+            if constexpr (!VLDS) vf[s] = *reinterpret_cast<const u32x4*>(vp + 32 * s);
         }
     }
-    if (qlen % QT != 0 && s0 < s1) {
-        for (uint32_t o = threadIdx.x * 16u; o < 4u * kTile; o += 64u * W * 16u) *reinterpret_cast<u32x4*>(lds + o) = u32x4{0u, 0u, 0u, 0u};
+    if ((qlen % QT != 0 || (VLDS && j_last >= klen)) && s0 < s1) {
+        for (uint32_t o = threadIdx.x * 16u; o < 4u * kTile + kV; o += 64u * W * 16u) *reinterpret_cast<u32x4*>(lds + o) = u32x4{0u, 0u, 0u, 0u};
         __syncthreads();
+    }
+    if constexpr (VLDS) {
+        if (s0 < s1) {
+            SeqLoader<RB, 32 * W, W> load_v;
+            load_v.init(wave, lane, kld);
+            load_v.issue(reinterpret_cast<uintptr_t>(a.v) + (((size_t)n * a.Lk + j0) * a.ldk + (size_t)kv * D) * E, seq_tile_bytes<RB>(klen - j0, 32 * W, kld), v_at);
+        }
     }
 
     f32x16 dk[NB], dv[NB];
@@ -750,7 +808,10 @@ __global__ void __launch_bounds__(64 * W) seq_keys_kernel(SeqArgs a, BackPlan pl
                 for (int e = 0; e < 4; ++e) ds[4 * q + e] = minus_delta[e];
             }
 #pragma unroll
-            for (int x = 0; x < NC; ++x) ds = seq_dot<T>(row_reader.read(gt, x, k), vf[x], ds);
+            for (int x = 0; x < NC; ++x) {
+                if constexpr (VLDS) ds = seq_dot<T>(row_reader.read(gt, x, k), row_reader.read(v_at + 32u * RB * wave, x, 0), ds);
+                else ds = seq_dot<T>(row_reader.read(gt, x, k), vf[x], ds);
+            }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const f32x4 add = seq_lds_f32x4(addend + 4u * (32 * k + 8 * q) + 16u * hi);
@@ -838,7 +899,7 @@ hipError_t start(Kernel* kernel, dim3 grid, int block, size_t lds, hipStream_t s
 template <class T, int D>
 hipError_t launch_table(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
     constexpr int RB = D * SeqSize<T>::value;
-    const size_t tiles = 4 * (size_t)(RB >= 512 ? 32 : kTableKeys) * RB, squares = 4 * 33 * 32 * 4 + 8 * 64 * 4;
+    const size_t tiles = 4 * (size_t)(RB >= 512 ? 32 : kTableKeys) * RB + kLine * 4, squares = 4 * 33 * 32 * 4 + 8 * 64 * 4;
     hipError_t e = start(&seq_table_kernel<T, D>, dim3((unsigned)(a.H * plan.offsets * plan.chunks)), 256, tiles > squares ? tiles : squares, s, a, plan);
     if (e != hipSuccess) return e;
     e = start(&seq_lines_kernel, dim3(1u + (unsigned)((2 * a.far - 1 + 63) / 64), (unsigned)a.H), 256, 0, s, a, plan);
@@ -857,7 +918,7 @@ hipError_t launch(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
         e = launch_table<T, D>(a, plan, s);
         if (e != hipSuccess) return e;
     }
-    e = start(&seq_keys_kernel<T, D, W, KT>, dim3(plan.key_grid), 64 * W, tiles + 36 * KT + 16 + bias, s, a, plan);
+    e = start(&seq_keys_kernel<T, D, W, KT>, dim3(plan.key_grid), 64 * W, tiles + (seq_keys_v_in_lds(D * SeqSize<T>::value) ? 32 * W * D * SeqSize<T>::value : 0) + 36 * KT + 16 + bias, s, a, plan);
     if (e != hipSuccess || plan.splits == 1 || a.Lk == 0) return e;
     const size_t threads = (size_t)a.N * a.Lk * a.KV * D / 2, blocks = (threads + 255) / 256;
     hipLaunchKernelGGL((seq_join_keys_kernel<T, D>), dim3((unsigned)blocks), dim3(256), 0, s, a, plan);
@@ -914,9 +975,9 @@ bool back_plan(const SeqArgs& a, BackPlan& p) {
     if (a.far == 0) p.offsets = 0;  // every distance is at an end
     const long long items = a.N * blocks;
     p.items = (int)items;
-    // four workgroups a CU, in chunks of at least four blocks where that leaves as many
+    // four workgroups a CU
     long long chunks = 4LL * cus / ((long long)a.H * (p.offsets > 0 ? p.offsets : 1));
-    if (chunks > (items + 3) / 4) chunks = (items + 3) / 4;
+    if (chunks > items) chunks = items;
     p.chunks = chunks < 1 ? 1 : (int)chunks;
     p.by_offsets = make_fastdiv((uint32_t)(p.offsets > 0 ? p.offsets : 1));
     p.by_chunks = make_fastdiv((uint32_t)p.chunks);
