@@ -137,10 +137,9 @@ struct SeqArgs {
     long long ldq, ldk, ldo, ldg, lddq, lddk;  // elements between rows of q; of k and v; of o; of d_o; of dq; of dk and dv
 };
 
-// Keys per tile of the forward: two tiles each of K and V take at most 64 KB of LDS, and 32 KB where a workgroup is one wave of
-// 16-bit data (five workgroups on a CU).
-constexpr int seq_forward_keys(int row_bytes, int waves) { return row_bytes >= 512 || (waves == 1 && row_bytes >= 256) ? 32 : 64; }
-
+// Waves of a workgroup that share out the keys, two tiles each of K and V a wave in 64 KB of LDS, and keys per tile of the forward.
+constexpr int seq_keys_waves(int row_bytes) { return row_bytes >= 512 ? 1 : row_bytes >= 256 ? 2 : 4; }
+constexpr int seq_forward_keys(int row_bytes, bool keys) { return row_bytes >= 512 || keys ? 32 : 64; }
 // Keys resp. queries per tile of the backward.
 constexpr int seq_backward_rows(int row_bytes) { return row_bytes >= 256 ? 32 : 64; }
 

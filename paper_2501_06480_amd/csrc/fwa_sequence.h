@@ -85,12 +85,16 @@ struct SeqLoader {
             off[i] = row * row_bytes + ((place ^ seq_swizzle<RB>(row)) * 16u);
         }
     }
-    // `bytes` of the rows from `first` on exist; `lds` = the tile's place
-    __device__ __forceinline__ void issue(uintptr_t first, uint32_t bytes, uint32_t lds) const {
-        const u32x4 src = {(uint32_t)first, (uint32_t)(first >> 32) & 0xffffu, bytes, 0x00020000u};
-        seq_loads_to_lds<kLoads, 1024 * WAVES>(src, off, lds + to);
-    }
+    // rows from the source's base on, as many as its bytes reach; `lds` = the tile's place
+    __device__ __forceinline__ void issue(const u32x4& source, uint32_t lds) const { seq_loads_to_lds<kLoads, 1024 * WAVES>(source, off, lds + to); }
 };
+// The source of a tensor's tiles, in four scalar registers from tile to tile.
+__device__ __forceinline__ u32x4 seq_source(const void* base) { return lds_source(base, 0u); }
+__device__ __forceinline__ void seq_advance(u32x4& source, uint64_t bytes) {
+    const uint64_t at = (((uint64_t)source[1] << 32) | source[0]) + bytes;
+    source[0] = (uint32_t)at;
+    source[1] = (uint32_t)(at >> 32);
+}
 // Bytes from the first of `rows` rows to the end of the last, of at most `most` rows (scalar: the rows of a tile that exist).
 template <int RB>
 __device__ __forceinline__ uint32_t seq_tile_bytes(int rows, int most, uint32_t row_bytes) {
@@ -265,27 +269,31 @@ __device__ __forceinline__ void seq_store4(char* row, uint32_t channel, float a,
     }
 }
 
-// Which workgroup has which part of which unit (a head of a sequence).  Workgroups go to the 8 XCDs in turn, each with an L2 of its own,
-// and an XCD's to its 32 CUs.  Units are dealt to the XCDs in turn too, whole ones, whose keys then stay in one L2, and each sequence's heads
-// to all XCDs, since sequences differ in length: contiguous ranges of units, a long sequence on two XCDs, left the CUs of the others
-// idle (encoder of 4 ragged sequences, 16 heads: 102 us).  Few units that 8 does not divide are dealt by parts instead.
-// Causal parts differ in size: every second round of an XCD's 32 goes backwards, so that a CU's parts come to one sum.
+// Which workgroup has which part of which head of which sequence.  Workgroups go to the 8 XCDs in turn, each with an L2 of its own, and an XCD's to its
+// 32 CUs.  Heads are dealt to the XCDs in turn, whole ones, whose keys then stay in one L2, and each sequence's to all XCDs, since sequences differ in
+// length (contiguous ranges of all heads of all sequences left the CUs of most XCDs idle: encoder of 4 ragged sequences, 16 heads, 102 us against 91).
+// Few heads that 8 does not divide are dealt by parts.  Causal parts differ in size: every second round of an XCD's 32 goes backwards,
+// so that a CU's parts come to one sum.
 struct SeqDeal {
-    uint32_t units, each, per_xcd;
+    uint32_t units, each, per_xcd, heads;
     int whole, snake;
-    FastDiv by_each;
+    FastDiv by_each, by_heads;
 };
-inline unsigned seq_deal(SeqDeal& d, long long units, long long each, bool snake) {
+inline unsigned seq_deal(SeqDeal& d, long long sequences, int heads, long long each, bool snake) {
+    const long long units = sequences * heads;
     d.units = (uint32_t)units;
     d.each = (uint32_t)each;
+    d.heads = (uint32_t)heads;
     d.whole = units % 8 == 0 || units >= 64;
     d.per_xcd = (uint32_t)((units + 7) / 8 * each);
     d.snake = snake;
     d.by_each = make_fastdiv(d.each > 0 ? d.each : 1u);
+    d.by_heads = make_fastdiv((uint32_t)heads);
     return (unsigned)(d.whole ? 8LL * d.per_xcd : units * each);
 }
 // false: nothing to do
-__device__ __forceinline__ bool seq_dealt(const SeqDeal& d, uint32_t block, uint32_t& unit, uint32_t& part) {
+__device__ __forceinline__ bool seq_dealt(const SeqDeal& d, uint32_t block, uint32_t& sequence, uint32_t& head, uint32_t& part) {
+    uint32_t unit;
     if (d.whole) {
         uint32_t at = block >> 3;
         const uint32_t round = at >> 5;
@@ -293,10 +301,13 @@ __device__ __forceinline__ bool seq_dealt(const SeqDeal& d, uint32_t block, uint
         const uint32_t turn = fastdiv(at, d.by_each);
         part = at - turn * d.each;
         unit = 8u * turn + (block & 7u);
-        return unit < d.units;
+        if (unit >= d.units) return false;
+    } else {
+        unit = fastdiv(block, d.by_each);
+        part = block - unit * d.each;
     }
-    unit = fastdiv(block, d.by_each);
-    part = block - unit * d.each;
+    sequence = fastdiv(unit, d.by_heads);
+    head = unit - sequence * d.heads;
     return true;
 }
 
@@ -304,11 +315,12 @@ __device__ __forceinline__ bool seq_dealt(const SeqDeal& d, uint32_t block, uint
 struct SeqPlan {
     int group;           // heads of queries per head of keys
     int packed;          // one block has the rows of a whole group (few rows: group * Lq <= 32)
+    int keys;            // the waves of a workgroup share out the keys, not the rows
     int waves, blocks, splits;
     unsigned grid;
     SeqDeal deal;
     uint32_t bias_entries;
-    FastDiv by_splits, by_heads;
+    FastDiv by_splits;
     size_t rows;         // N * H * Lq
     float* part_o;       // [splits][rows][D], not divided by the sum
     float* part_ml;      // [splits][rows][2]

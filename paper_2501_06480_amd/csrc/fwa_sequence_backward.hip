@@ -13,11 +13,11 @@ namespace fwa {
 namespace {
 
 struct BackPlan {
-    int group, waves, row_blocks, key_blocks, splits;
+    int group, keys, waves, key_waves, row_blocks, key_blocks, splits;
     unsigned row_grid, key_grid;
     SeqDeal row_deal, key_deal;
-    uint32_t bias_entries;
-    FastDiv by_heads, by_splits, by_kv;
+    uint32_t row_bias, key_bias;
+    FastDiv by_splits;
     int row_waves;       // waves with rows per head of a sequence: ceil(Lq / 32)
     float* delta;        // [N, H, Lq]
     float* ends;         // [H][N * row_waves][2]: sums of dS at and beyond -far and far
@@ -44,23 +44,26 @@ __device__ __forceinline__ float plain_sum(float a, float b) {
     return a + b;
 }
 
-template <class T, int D, int W, int KT, bool TABLE>
+// Two forms, as in the forward: the waves have 32 rows each and share the tiles, or (KEYS) the same 32 rows and every W-th tile each.
+template <class T, int D, int W, int KT, bool TABLE, bool KEYS>
 __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan plan) {
     constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, KS = KT / 32;
+    constexpr int ROWS = KEYS ? 32 : 32 * W, TURN = KEYS ? W : 1;
     constexpr uint32_t kTile = KT * RB;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const uint32_t base = lds_offset(lds), bias_at = base + 4u * kTile, bias_bytes = 4u * plan.bias_entries;
     const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t hi = lane >> 5, c = lane & 31u;
+    const uint32_t hi = lane >> 5, c = lane & 31u, bias_bytes = 4u * plan.row_bias;
+    const uint32_t base = lds_offset(lds) + (KEYS ? wave * 4u * kTile : 0u);
+    const uint32_t bias_at = lds_offset(lds) + (KEYS ? 4u * W * kTile + wave * 2u * bias_bytes : 4u * kTile);
 
-    uint32_t unit, part;
-    if (!seq_dealt(plan.row_deal, blockIdx.x, unit, part)) return;
+    uint32_t sequence, unit, part;
+    if (!seq_dealt(plan.row_deal, blockIdx.x, sequence, unit, part)) return;
     int block = (int)part;
-    const long long n = fastdiv(unit, plan.by_heads);
-    const int head = (int)(unit - (uint32_t)n * plan.by_heads.d), kv = head / plan.group;
+    const long long n = sequence;
+    const int head = (int)unit, kv = head / plan.group;
     if (a.causal) block = plan.row_blocks - 1 - block;
-    const int i0 = block * 32 * W, i = i0 + (int)(32u * wave + c);
-    const int span_rows = a.Lq - i0 < 32 * W ? a.Lq - i0 : 32 * W;
+    const int i0 = block * ROWS, i = i0 + (int)(KEYS ? c : 32u * wave + c);
+    const int span_rows = a.Lq - i0 < ROWS ? a.Lq - i0 : ROWS;
     const int qlen = seq_length(a.q_len, n, a.Lq), klen = seq_length(a.k_len, n, a.Lk), start = seq_start(a.q_start, n);
     const int first = start + i0, last = first + span_rows - 1, pos = i < a.Lq ? start + i : last;
 
@@ -71,22 +74,24 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
     const char* const kp = static_cast<const char*>(a.k) + ((size_t)n * a.Lk * a.ldk + (size_t)kv * D) * E;
     const char* const vp = static_cast<const char*>(a.v) + ((size_t)n * a.Lk * a.ldk + (size_t)kv * D) * E;
     const uint32_t kld = (uint32_t)(a.ldk * E);
-    SeqLoader<RB, KT, W> load;
-    load.init(wave, lane, kld);
+    SeqLoader<RB, KT, KEYS ? 1 : W> load;
+    load.init(KEYS ? 0u : wave, lane, kld);
     SeqRowReader<RB> row_reader;
     row_reader.init(hi, c);
     SeqColumnReader<T, D> column_reader;
     column_reader.init(hi, c);
-    // addresses of the next tile to ask for, and the rows from there on
-    uintptr_t next_k = reinterpret_cast<uintptr_t>(kp), next_v = reinterpret_cast<uintptr_t>(vp);
-    int next_rows = klen;
+    // the next tile to ask for, and the rows from there on
+    const int mine0 = KEYS ? (int)wave : 0;
+    u32x4 next_k = seq_source(kp), next_v = seq_source(vp);
+    int next_rows;
+    const uint32_t whole = (KT - 1u) * kld + RB, rest = seq_tile_bytes<RB>(klen % KT, KT, kld);
     auto issue = [&](uint32_t buf) {
-        const uint32_t bytes = seq_tile_bytes<RB>(next_rows, KT, kld);
-        load.issue(next_k, bytes, base + buf * 2u * kTile);
-        load.issue(next_v, bytes, base + buf * 2u * kTile + kTile);
-        next_k += KT * kld;
-        next_v += KT * kld;
-        next_rows -= KT;
+        next_k[2] = next_v[2] = next_rows >= KT ? whole : rest;
+        load.issue(next_k, base + buf * 2u * kTile);
+        load.issue(next_v, base + buf * 2u * kTile + kTile);
+        seq_advance(next_k, (uint64_t)(TURN * KT) * kld);
+        seq_advance(next_v, (uint64_t)(TURN * KT) * kld);
+        next_rows -= TURN * KT;
     };
 
     const size_t row = ((size_t)n * a.H + head) * a.Lq + i;
@@ -128,7 +133,7 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
     delta = seq_sum_halves(delta);
     const bool some_dead = __any(dead);
     if (klen % KT != 0 && tiles > 0) {  // rows that no load fills: as in the forward
-        for (uint32_t o = threadIdx.x * 16u; o < 4u * kTile; o += 64u * W * 16u) *reinterpret_cast<u32x4*>(lds + o) = u32x4{0u, 0u, 0u, 0u};
+        for (uint32_t o = threadIdx.x * 16u; o < (KEYS ? 4u * W : 4u) * kTile; o += 64u * W * 16u) *reinterpret_cast<u32x4*>(lds + o) = u32x4{0u, 0u, 0u, 0u};
         __syncthreads();
     }
 
@@ -147,39 +152,58 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
     }
     if (some_dead) mask0 = 0;
 
+    const uint32_t entry = KEYS ? lane : threadIdx.x;  // of the bias of a near tile: one for each thread at most
+    static_assert(KT + ROWS - 1 <= (KEYS ? 64 : 64 * W), "a thread for each distance of a tile");
     SeqBiasAhead ahead = {0u, 0u, 0.f};
-    auto find = [&](int t) { if (W == 4 && t >= near0 && t < near1) ahead.find(a.buckets, far, t * KT - last + (int)threadIdx.x); };
-    auto fetch = [&](int t) { if (W == 4 && t >= near0 && t < near1) ahead.fetch(table, a.nb); };
+    auto find = [&](int t) { if (t >= near0 && t < near1) ahead.find(a.buckets, far, t * KT - last + (int)entry); };
+    auto fetch = [&](int t) { if (t >= near0 && t < near1) ahead.fetch(table, a.nb); };
     // before the barrier of tile t: its bias; behind it: what the tiles that follow need
     auto begin = [&](int t, uint32_t buf) {
-        if (t >= near0 && t < near1) {
-            if constexpr (W == 4) {
-                if (threadIdx.x < entries) seq_lds_put(bias_at + buf * bias_bytes + 4u * threadIdx.x, ahead.get(a.nb));
-            } else {
-                for (uint32_t e = threadIdx.x; e < entries; e += 64u * W)
-                    seq_lds_put(bias_at + buf * bias_bytes + 4u * e, seq_bias_at(table, a.buckets, a.nb, far, t * KT - last + (int)e));
-            }
-        }
+        if (t >= near0 && t < near1 && entry < entries) seq_lds_put(bias_at + buf * bias_bytes + 4u * entry, ahead.get(a.nb));
         lds_loads_done();
-        __syncthreads();
-        fetch(t + 1);
-        find(t + 2);
-        if (t + 1 < tiles) issue(buf ^ 1u);
+        if constexpr (!KEYS) __syncthreads();
+        fetch(t + TURN);
+        find(t + 2 * TURN);
+        if (t + TURN < tiles) issue(buf ^ 1u);
     };
     auto start_walk = [&]() {
-        find(0);
-        fetch(0);
-        find(1);
-        next_k = reinterpret_cast<uintptr_t>(kp);
-        next_v = reinterpret_cast<uintptr_t>(vp);
-        next_rows = klen;
-        if (tiles > 0) issue(0);
+        find(mine0);
+        fetch(mine0);
+        find(mine0 + TURN);
+        const size_t skip = (size_t)mine0 * KT * kld;
+        next_k = seq_source(kp + skip);
+        next_v = seq_source(vp + skip);
+        next_rows = klen - mine0 * KT;
+        if (mine0 < tiles) issue(0);
+    };
+    auto walk = [&](auto step) {
+        if constexpr (KEYS) {
+            uint32_t parity = 0;
+            for (int t = mine0; t < tiles; t += TURN, parity ^= 1u) step(parity, t);
+        } else {
+            for (int t = 0; t < tiles; t += 2) {
+                step(std::integral_constant<uint32_t, 0>{}, t);
+                if (t + 1 < tiles) step(std::integral_constant<uint32_t, 1>{}, t + 1);
+            }
+        }
+    };
+    // a sum over the waves that share the rows, in the order of the waves
+    auto over_waves = [&](float x) {
+        if constexpr (KEYS && W > 1) {
+            __syncthreads();
+            if (hi == 0) seq_lds_put(lds_offset(lds) + 4u * (32u * wave + c), x);
+            __syncthreads();
+            x = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) x += seq_lds_f32(lds_offset(lds) + 4u * (32u * w + c));
+        }
+        return x;
     };
     // Q K^T of tile t, or, where the bias is not one value or pairs are shut out, the scores; the exponent of a weight, the row's sum not divided
     // out, is s mul + minus
     struct Exponent { float mul, minus; };
     auto scores = [&](auto parity, int t, f32x16 (&s)[KS]) -> Exponent {
-        constexpr uint32_t B = decltype(parity)::value;
+        const uint32_t B = parity;
         const uint32_t kt = base + B * 2u * kTile;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
@@ -217,10 +241,10 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
     for (int b = 0; b < NB; ++b) seq_zero(dq[b]);
     float ds_all = 0.f, ds_below = 0.f, ds_above = 0.f, p_below = 0.f, p_above = 0.f;
     start_walk();
-    if (tiles > 0 && tiles <= kFewTiles) {
+    if (tiles > 0 && tiles <= kFewTiles * (KEYS ? W : 1)) {
         float sum = 0.f;
-        auto look = [&](auto parity, int t) {
-            constexpr uint32_t B = decltype(parity)::value;
+        walk([&](auto parity, int t) {
+            const uint32_t B = parity;
             begin(t, B);
             f32x16 s[KS];
             const Exponent e = scores(parity, t, s);
@@ -233,18 +257,16 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
 #pragma unroll
                 for (int r = 0; r < 16; ++r) sum = fmaf(__builtin_amdgcn_exp2f(fmaf(s[k][r], e.mul, e.minus)), dp[r], sum);
             }
-        };
-        look(std::integral_constant<uint32_t, 0>{}, 0);
-        if (tiles > 1) look(std::integral_constant<uint32_t, 1>{}, 1);
-        delta = rl * seq_sum_halves(sum);
+        });
+        delta = rl * over_waves(seq_sum_halves(sum));
         __syncthreads();
         start_walk();
     }
     f32x16 minus_delta;
 #pragma unroll
     for (int r = 0; r < 16; ++r) minus_delta[r] = -delta;
-    auto step = [&](auto parity, int t) {
-        constexpr uint32_t B = decltype(parity)::value;
+    walk([&](auto parity, int t) {
+        const uint32_t B = parity;
         begin(t, B);
         f32x16 s[KS];
         const Exponent ex = scores(parity, t, s);
@@ -286,14 +308,10 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
             ds_above += is_above ? ds_tile : 0.f;
             p_above += is_above ? p_tile : 0.f;
         }
-    };
-    for (int t = 0; t < tiles; t += 2) {
-        step(std::integral_constant<uint32_t, 0>{}, t);
-        if (t + 1 < tiles) step(std::integral_constant<uint32_t, 1>{}, t + 1);
-    }
+    });
     // The dS of a row add up to zero; what they add up to is what delta is off by, times the row's weights.  dQ of 16-bit data keeps
     // it (it is below the roundings of dS); dK and the sums by distance, which are not rounded, get the better delta.
-    const float off = rl * seq_sum_halves(ds_all);
+    const float off = rl * over_waves(seq_sum_halves(ds_all));
     delta = plain_sum(delta, off);
 
     if constexpr (TABLE) {
@@ -305,9 +323,40 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
             sum_below += __shfl_xor(sum_below, x, 64);
             sum_above += __shfl_xor(sum_above, x, 64);
         }
-        const int rw = block * W + (int)wave;
-        if (lane == 0 && rw < plan.row_waves)
+        if constexpr (KEYS && W > 1) {  // the same in every lane: sums over the waves too
+            sum_below = over_waves(sum_below);
+            sum_above = over_waves(sum_above);
+        }
+        const int rw = KEYS ? block : block * W + (int)wave;
+        if (lane == 0 && rw < plan.row_waves && (!KEYS || wave == W - 1))
             *reinterpret_cast<f32x2*>(plan.ends + 2 * (((size_t)head * a.N + n) * plan.row_waves + rw)) = f32x2{sum_below, sum_above};
+    }
+
+    if constexpr (KEYS && W > 1) {
+        // dQ of all waves: rows 4 floats apart from a multiple of the banks; the last wave has it, the others are done
+        constexpr uint32_t kRow = 4u * (D + 4);
+        const uint32_t all = lds_offset(lds);
+        __syncthreads();
+        if (wave != W - 1) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *(__attribute__((address_space(3))) f32x4*)(uintptr_t)(all + kRow * (32u * wave + c) + 4u * (32 * b + 8 * q + 4 * hi)) =
+                        f32x4{dq[b][4 * q], dq[b][4 * q + 1], dq[b][4 * q + 2], dq[b][4 * q + 3]};
+        }
+        __syncthreads();
+        if (wave != W - 1) return;
+#pragma unroll
+        for (int w = 0; w < W - 1; ++w)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4 x = seq_lds_f32x4(all + kRow * (32u * w + c) + 4u * (32 * b + 8 * q + 4 * hi));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dq[b][4 * q + e] += x[e];
+                }
     }
 
     if (i >= a.Lq) return;
@@ -391,8 +440,8 @@ __global__ void __launch_bounds__(256) seq_table_kernel(SeqArgs a, BackPlan plan
         SeqLoader<RB, KT, 4> shifted = load;
 #pragma unroll
         for (int i = 0; i < load.kLoads; ++i) shifted.off[i] -= shift;
-        shifted.issue(reinterpret_cast<uintptr_t>(a.k) + at, bytes, base + buf * 2u * kTile);
-        shifted.issue(reinterpret_cast<uintptr_t>(a.v) + at, bytes, base + buf * 2u * kTile + kTile);
+        shifted.issue(lds_source(static_cast<const char*>(a.k) + at, bytes), base + buf * 2u * kTile);
+        shifted.issue(lds_source(static_cast<const char*>(a.v) + at, bytes), base + buf * 2u * kTile + kTile);
     };
 
     // what no load fills: its scores are shut out, but zero times what LDS may hold has to be zero
@@ -586,15 +635,15 @@ __global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) 
     constexpr uint32_t kV = VLDS ? 32u * W * RB : 0u;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t base = lds_offset(lds), v_at = base + 4u * kTile, stat_at = v_at + kV, zero_at = stat_at + 2u * kStat, bias_at = zero_at + 4u * QT + 16u,
-                   bias_bytes = 4u * plan.bias_entries;
+                   bias_bytes = 4u * plan.key_bias;
     const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t hi = lane >> 5, c = lane & 31u;
 
-    uint32_t unit, part;
-    if (!seq_dealt(plan.key_deal, blockIdx.x, unit, part)) return;
+    uint32_t sequence, unit, part;
+    if (!seq_dealt(plan.key_deal, blockIdx.x, sequence, unit, part)) return;
     const int block = (int)fastdiv(part, plan.by_splits), split = (int)part - block * (int)plan.by_splits.d;
-    const long long n = fastdiv(unit, plan.by_kv);
-    const int kv = (int)(unit - (uint32_t)n * plan.by_kv.d);
+    const long long n = sequence;
+    const int kv = (int)unit;
     const int j0 = block * 32 * W, j = j0 + (int)(32u * wave + c), j_last = j0 + 32 * W - 1;
     const int qlen = seq_length(a.q_len, n, a.Lq), klen = seq_length(a.k_len, n, a.Lk), start = seq_start(a.q_start, n);
 
@@ -621,12 +670,25 @@ __global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) 
         now.g = s0 / each;
         now.t = q0 + s0 - now.g * each;
     }
+    // the next tile to ask for, and its first row in the statistics; behind the last tile of a head comes the first of the next one
+    const int head0 = kv * plan.group + now.g;
+    const size_t row0 = (size_t)n * a.Lq + (size_t)now.t * QT;
+    u32x4 next_q = seq_source(static_cast<const char*>(a.q) + (row0 * a.ldq + (size_t)head0 * D) * E);
+    u32x4 next_g = seq_source(static_cast<const char*>(a.d_o) + (row0 * a.ldg + (size_t)head0 * D) * E);
+    int64_t next_row = (int64_t)(((size_t)n * a.H + head0) * a.Lq) + (int64_t)now.t * QT;
+    const int64_t back = (int64_t)(each > 0 ? each - 1 : 0) * QT;
+    const uint64_t on_q = (uint64_t)QT * qld, on_g = (uint64_t)QT * gld, over_q = (uint64_t)(D * E - back * (int64_t)qld), over_g = (uint64_t)(D * E - back * (int64_t)gld);
+    const uint32_t whole_q = (QT - 1u) * qld + RB, whole_g = (QT - 1u) * gld + RB;
+    const uint32_t rest_q = qlen % QT ? seq_tile_bytes<RB>(qlen % QT, QT, qld) : whole_q, rest_g = qlen % QT ? seq_tile_bytes<RB>(qlen % QT, QT, gld) : whole_g;
     auto issue = [&](const Place& x, uint32_t buf) {
-        const int head = kv * plan.group + x.g;
-        const size_t row = (size_t)n * a.Lq + (size_t)x.t * QT;
-        const uint32_t to = base + buf * 2u * kTile;
-        load_q.issue(reinterpret_cast<uintptr_t>(a.q) + (row * a.ldq + (size_t)head * D) * E, seq_tile_bytes<RB>(qlen - x.t * QT, QT, qld), to);
-        load_g.issue(reinterpret_cast<uintptr_t>(a.d_o) + (row * a.ldg + (size_t)head * D) * E, seq_tile_bytes<RB>(qlen - x.t * QT, QT, gld), to + kTile);
+        const bool last = x.t + 1 == q1;
+        next_q[2] = last ? rest_q : whole_q;
+        next_g[2] = last ? rest_g : whole_g;
+        load_q.issue(next_q, base + buf * 2u * kTile);
+        load_g.issue(next_g, base + buf * 2u * kTile + kTile);
+        seq_advance(next_q, last ? over_q : on_q);
+        seq_advance(next_g, last ? over_g : on_g);
+        next_row += last ? a.Lq - back : (int64_t)QT;
     };
 
     u32x4 kf[NC], vf[VLDS ? 1 : NC];
@@ -654,7 +716,7 @@ __global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) 
         if (s0 < s1) {
             SeqLoader<RB, 32 * W, W> load_v;
             load_v.init(wave, lane, kld);
-            load_v.issue(reinterpret_cast<uintptr_t>(a.v) + (((size_t)n * a.Lk + j0) * a.ldk + (size_t)kv * D) * E, seq_tile_bytes<RB>(klen - j0, 32 * W, kld), v_at);
+            load_v.issue(lds_source(static_cast<const char*>(a.v) + (((size_t)n * a.Lk + j0) * a.ldk + (size_t)kv * D) * E, seq_tile_bytes<RB>(klen - j0, 32 * W, kld)), v_at);
         }
     }
 
@@ -698,9 +760,8 @@ __global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) 
         const int i = x.t * QT + (int)threadIdx.x;
         row_ahead = threadIdx.x < (uint32_t)QT && i < qlen;
         if (row_ahead) {
-            const size_t row = ((size_t)n * a.H + kv * plan.group + x.g) * a.Lq + i;
-            stat_ahead = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
-            delta_ahead = plan.delta[row];
+            stat_ahead = reinterpret_cast<const f32x2*>(a.stats + 2 * next_row)[threadIdx.x];
+            delta_ahead = (plan.delta + next_row)[threadIdx.x];
         }
     };
     SeqBiasAhead ahead = {0u, 0u, 0.f};
@@ -710,8 +771,8 @@ __global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) 
 
     Place next = behind(now);
     if (s0 < s1) {
-        issue(now, 0);
         fetch_stats(now);
+        issue(now, 0);
         find(now);
         fetch(now);
         if (s0 + 1 < s1) find(next);
@@ -907,18 +968,29 @@ hipError_t launch_table(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
     return launch_bucket_sums(plan.lines, nullptr, a.buckets, a.dtable, a.H, a.nb, a.far, 1, s);
 }
 
+template <class T, int D, int W, int KT, bool KEYS>
+hipError_t launch_rows(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
+    constexpr size_t tiles = 4 * (size_t)KT * D * SeqSize<T>::value * (KEYS ? W : 1), sums = KEYS && W > 1 ? (size_t)W * 32 * 4 * (D + 4) : 0;
+    const size_t bias = 2 * sizeof(float) * plan.row_bias * (KEYS ? W : 1), lds = tiles + bias > sums ? tiles + bias : sums;
+    return a.dtable ? start(&seq_rows_kernel<T, D, W, KT, true, KEYS>, dim3(plan.row_grid), 64 * W, lds, s, a, plan)
+                    : start(&seq_rows_kernel<T, D, W, KT, false, KEYS>, dim3(plan.row_grid), 64 * W, lds, s, a, plan);
+}
 template <class T, int D, int W>
+hipError_t launch_keys(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
+    constexpr int RB = D * SeqSize<T>::value, KT = seq_backward_rows(RB);
+    const size_t tiles = 4 * (size_t)KT * RB + (seq_keys_v_in_lds(RB) ? 32 * W * RB : 0), bias = 2 * sizeof(float) * plan.key_bias;
+    return start(&seq_keys_kernel<T, D, W, KT>, dim3(plan.key_grid), 64 * W, tiles + 36 * KT + 16 + bias, s, a, plan);
+}
+template <class T, int D>
 hipError_t launch(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
-    constexpr int KT = seq_backward_rows(D * SeqSize<T>::value);
-    const size_t tiles = 4 * (size_t)KT * D * SeqSize<T>::value, bias = 2 * sizeof(float) * plan.bias_entries;
-    hipError_t e = a.dtable ? start(&seq_rows_kernel<T, D, W, KT, true>, dim3(plan.row_grid), 64 * W, tiles + bias, s, a, plan)
-                            : start(&seq_rows_kernel<T, D, W, KT, false>, dim3(plan.row_grid), 64 * W, tiles + bias, s, a, plan);
+    constexpr int RB = D * SeqSize<T>::value;
+    hipError_t e = plan.keys ? launch_rows<T, D, seq_keys_waves(RB), 32, true>(a, plan, s) : launch_rows<T, D, 4, seq_backward_rows(RB), false>(a, plan, s);
     if (e != hipSuccess) return e;
     if (a.dtable) {
         e = launch_table<T, D>(a, plan, s);
         if (e != hipSuccess) return e;
     }
-    e = start(&seq_keys_kernel<T, D, W, KT>, dim3(plan.key_grid), 64 * W, tiles + (seq_keys_v_in_lds(D * SeqSize<T>::value) ? 32 * W * D * SeqSize<T>::value : 0) + 36 * KT + 16 + bias, s, a, plan);
+    e = plan.key_waves == 1 ? launch_keys<T, D, 1>(a, plan, s) : launch_keys<T, D, 4>(a, plan, s);
     if (e != hipSuccess || plan.splits == 1 || a.Lk == 0) return e;
     const size_t threads = (size_t)a.N * a.Lk * a.KV * D / 2, blocks = (threads + 255) / 256;
     hipLaunchKernelGGL((seq_join_keys_kernel<T, D>), dim3((unsigned)blocks), dim3(256), 0, s, a, plan);
@@ -926,23 +998,22 @@ hipError_t launch(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
 }
 template <class T>
 hipError_t launch(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
-    if (plan.waves == 1) {
-        if (a.D == 32) return launch<T, 32, 1>(a, plan, s);
-        if (a.D == 64) return launch<T, 64, 1>(a, plan, s);
-        return launch<T, 128, 1>(a, plan, s);
-    }
-    if (a.D == 32) return launch<T, 32, 4>(a, plan, s);
-    if (a.D == 64) return launch<T, 64, 4>(a, plan, s);
-    return launch<T, 128, 4>(a, plan, s);
+    if (a.D == 32) return launch<T, 32>(a, plan, s);
+    if (a.D == 64) return launch<T, 64>(a, plan, s);
+    return launch<T, 128>(a, plan, s);
 }
 
 bool back_plan(const SeqArgs& a, BackPlan& p) {
     const int cus = cu_count();
     p.group = a.H / a.KV;
-    p.waves = a.Lq <= 32 && a.Lk <= 32 ? 1 : 4;
-    const int KT = seq_backward_rows(a.D * (a.dtype == 0 ? 4 : 2)), block = 32 * p.waves;
+    const int RB = a.D * (a.dtype == 0 ? 4 : 2), KT = seq_backward_rows(RB);
+    // rows: as in the forward
+    p.keys = (double)a.N * a.H * ((a.Lq + 127) / 128) < cus;
+    p.waves = p.keys ? seq_keys_waves(RB) : 4;
+    p.key_waves = a.Lk <= 32 ? 1 : 4;
+    const int block = p.keys ? 32 : 32 * p.waves, key_block = 32 * p.key_waves;
     p.row_blocks = (a.Lq + block - 1) / block;
-    p.key_blocks = (a.Lk + block - 1) / block;
+    p.key_blocks = (a.Lk + key_block - 1) / key_block;
     p.row_waves = (a.Lq + 31) / 32;
     const double rows = (double)a.N * a.H * p.row_blocks, keys = (double)a.N * a.KV * p.key_blocks;
     // Too few blocks of keys for the device: their queries are shared out, no more than leaves each two tiles.
@@ -952,13 +1023,12 @@ bool back_plan(const SeqArgs& a, BackPlan& p) {
     if (splits > 16) splits = 16;
     p.splits = splits < 1 ? 1 : (int)splits;
     // threads of a launch
-    if ((rows + 8.0 * p.row_blocks) * 64 * p.waves > 4.0e9 || (keys + 8.0 * p.key_blocks) * p.splits * 64 * p.waves > 4.0e9) return false;
-    p.row_grid = seq_deal(p.row_deal, a.N * a.H, p.row_blocks, a.causal && p.row_blocks > 1);
-    p.key_grid = seq_deal(p.key_deal, a.N * a.KV, (long long)p.key_blocks * p.splits, a.causal && p.key_blocks > 1);
-    p.by_heads = make_fastdiv((uint32_t)a.H);
+    if ((rows + 8.0 * p.row_blocks) * 64 * p.waves > 4.0e9 || (keys + 8.0 * p.key_blocks) * p.splits * 64 * p.key_waves > 4.0e9) return false;
+    p.row_grid = seq_deal(p.row_deal, a.N, a.H, p.row_blocks, a.causal && p.row_blocks > 1);
+    p.key_grid = seq_deal(p.key_deal, a.N, a.KV, (long long)p.key_blocks * p.splits, a.causal && p.key_blocks > 1);
     p.by_splits = make_fastdiv((uint32_t)p.splits);
-    p.by_kv = make_fastdiv((uint32_t)a.KV);
-    p.bias_entries = a.table ? (uint32_t)(KT + block - 1) : 0u;
+    p.row_bias = a.table ? (uint32_t)((p.keys ? 32 : KT) + block - 1) : 0u;
+    p.key_bias = a.table ? (uint32_t)(KT + key_block - 1) : 0u;
 
     // offsets of blocks with distances between -far and far, and, where all start at 0, with a pair in them
     const int blocks = (a.Lq + kTableRows - 1) / kTableRows;

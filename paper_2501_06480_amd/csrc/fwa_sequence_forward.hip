@@ -16,36 +16,47 @@ namespace {
 // scaled anew a few times instead of at every tile.  Their type's precision is relative; half data reach 2^15.
 constexpr float kSlack = 6.f;
 
-template <class T, int D, int W, int KT>
-__global__ void __launch_bounds__(64 * W) seq_forward_kernel(SeqArgs a, SeqPlan plan) {
+// Waves per SIMD that the registers are held to: rows of 128 bytes come to a few registers more than three waves have otherwise (encoder of 4 x 2048
+// tokens, 12 heads: 82 us with two, 68 with three).
+[[maybe_unused]] constexpr int seq_forward_waves(int row_bytes, bool keys) { return row_bytes == 128 && !keys ? 3 : 1; }
+
+// Two forms.  Rows: the W waves of a workgroup have 32 rows each and share the tiles.  KEYS: all have the same 32 rows and every W-th tile each,
+// in buffers of their own without a barrier, and join what they have at the end: W times the parallel work where rows are few, for W
+// times the loads of K and V.
+template <class T, int D, int W, int KT, bool KEYS>
+__global__ void __launch_bounds__(64 * W, seq_forward_waves(D * SeqSize<T>::value, KEYS)) seq_forward_kernel(SeqArgs a, SeqPlan plan) {
     constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, KS = KT / 32;
+    constexpr int ROWS = KEYS ? 32 : 32 * W, TURN = KEYS ? W : 1;  // of a workgroup; from a wave's tile to its next one
     constexpr uint32_t kTile = KT * RB;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const uint32_t base = lds_offset(lds), bias_at = base + 4u * kTile;
     const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t hi = lane >> 5, c = lane & 31u, slot = 32u * wave + c;
+    const uint32_t hi = lane >> 5, c = lane & 31u, slot = KEYS ? c : 32u * wave + c;
+    const uint32_t bias_bytes = 4u * plan.bias_entries;
+    const uint32_t base = lds_offset(lds) + (KEYS ? wave * 4u * kTile : 0u);
+    const uint32_t bias_at = lds_offset(lds) + (KEYS ? 4u * W * kTile + wave * 2u * bias_bytes : 4u * kTile);
 
     // workgroup -> sequence, head (or group of heads that share keys), block of rows, split of the keys
-    uint32_t unit, part;
-    if (!seq_dealt(plan.deal, blockIdx.x, unit, part)) return;
+    uint32_t sequence, unit, part;
+    if (!seq_dealt(plan.deal, blockIdx.x, sequence, unit, part)) return;
     int block = (int)fastdiv(part, plan.by_splits);
     const int split = (int)part - block * (int)plan.by_splits.d;
-    const long long n = fastdiv(unit, plan.by_heads);
-    const int hk = (int)(unit - (uint32_t)n * plan.by_heads.d);  // head, or head of the keys where the rows of a group are packed
+    const long long n = sequence;
+    const int hk = (int)unit;  // head, or head of the keys where the rows of a group are packed
     if (a.causal) block = plan.blocks - 1 - block;             // those with most keys first
-    const int G = plan.group, i0 = block * 32 * W;
-    const int kv = plan.packed ? hk : hk / G;
+    const bool packed = KEYS && plan.packed;
+    const int G = plan.group, i0 = block * ROWS;
+    const int kv = packed ? hk : hk / G;
     int head = hk, i = i0 + (int)slot, g = 0;
-    if (plan.packed) {
+    if (packed) {
         g = (int)slot / a.Lq;
         i = (int)slot - g * a.Lq;
         head = hk * G + g;
     }
-    const int span_rows = plan.packed ? a.Lq : (a.Lq - i0 < 32 * W ? a.Lq - i0 : 32 * W);
-    const bool exists = plan.packed ? g < G : i < a.Lq;
+    const int span_rows = packed ? a.Lq : (a.Lq - i0 < ROWS ? a.Lq - i0 : ROWS);
+    const bool exists = packed ? g < G : i < a.Lq;
     const int qlen = seq_length(a.q_len, n, a.Lq), klen = seq_length(a.k_len, n, a.Lk), start = seq_start(a.q_start, n);
     const int first = start + i0, last = first + span_rows - 1, pos = exists ? start + i : last;
-    if (!exists) { head = plan.packed ? hk * G : hk; g = 0; }
+    if (!exists) { head = packed ? hk * G : hk; g = 0; }
 
     int kend = i0 < qlen ? klen : 0;
     if (a.causal && kend > last + 1) kend = last + 1 > 0 ? last + 1 : 0;
@@ -56,24 +67,48 @@ __global__ void __launch_bounds__(64 * W) seq_forward_kernel(SeqArgs a, SeqPlan 
     const char* const vp = static_cast<const char*>(a.v) + ((size_t)n * a.Lk * a.ldk + (size_t)kv * D) * E;
     const uint32_t kld = (uint32_t)(a.ldk * E);
 
-    SeqLoader<RB, KT, W> load;
-    load.init(wave, lane, kld);
+    SeqLoader<RB, KT, KEYS ? 1 : W> load;
+    load.init(KEYS ? 0u : wave, lane, kld);
     SeqRowReader<RB> row_reader;
     row_reader.init(hi, c);
     SeqColumnReader<T, D> column_reader;
     column_reader.init(hi, c);
-    // addresses of the next tile to ask for, and the rows from there on
-    const size_t skip = (size_t)t0 * KT * kld;
-    uintptr_t next_k = reinterpret_cast<uintptr_t>(kp) + skip, next_v = reinterpret_cast<uintptr_t>(vp) + skip;
-    int next_rows = klen - t0 * KT;
+    // the next tile to ask for, and the rows from there on
+    const int mine0 = KEYS ? t0 + (int)wave : t0;
+    const size_t skip = (size_t)mine0 * KT * kld;
+    u32x4 next_k = seq_source(kp + skip), next_v = seq_source(vp + skip);
+    int next_rows = klen - mine0 * KT;
+    const uint32_t whole = (KT - 1u) * kld + RB, rest = seq_tile_bytes<RB>(klen % KT, KT, kld);
     auto issue = [&](uint32_t buf) {
-        const uint32_t bytes = seq_tile_bytes<RB>(next_rows, KT, kld);
-        load.issue(next_k, bytes, base + buf * 2u * kTile);
-        load.issue(next_v, bytes, base + buf * 2u * kTile + kTile);
-        next_k += KT * kld;
-        next_v += KT * kld;
-        next_rows -= KT;
+        next_k[2] = next_v[2] = next_rows >= KT ? whole : rest;
+        load.issue(next_k, base + buf * 2u * kTile);
+        load.issue(next_v, base + buf * 2u * kTile + kTile);
+        seq_advance(next_k, (uint64_t)(TURN * KT) * kld);
+        seq_advance(next_v, (uint64_t)(TURN * KT) * kld);
+        next_rows -= TURN * KT;
     };
+
+    const float* const table = a.table ? a.table + (size_t)head * a.nb : nullptr;
+    const int far = a.far;
+    // tiles whose distances are not all cut off: near0 .. near1 - 1; tiles with a pair that a length or causality shuts out: from mask0 on
+    int near0 = 0, near1 = 0, mask0 = klen / KT;
+    seq_near_tiles(a.table != nullptr, first, last, far, KT, near0, near1);
+    if (a.causal && first < klen) {
+        const int to = first + 1 > 0 ? (first + 1) / KT : 0;
+        mask0 = to < mask0 ? to : mask0;
+    }
+    // the bias of a near tile, by distance, for each head of the block; a thread's entry is looked up ahead where each has one
+    const uint32_t span = (uint32_t)(KT + span_rows - 1), entries = packed ? span * G : span;
+    const uint32_t my_bias = bias_at + 4u * ((uint32_t)g * span + (uint32_t)(last - pos) + 4u * hi);
+    const float* const group_table = a.table + (size_t)(packed ? hk * G : hk) * a.nb;
+    const uint32_t entry = KEYS ? lane : threadIdx.x, entry_head = packed && entry < entries ? entry / span : 0u;
+    const bool one_each = entries <= (KEYS ? 64u : 64u * W);
+    const float* const entry_table = KEYS ? group_table + (size_t)entry_head * a.nb : group_table;
+    const int entry_distance = (int)(entry - entry_head * span) - last;
+    SeqBiasAhead ahead = {0u, 0u, 0.f};
+    auto find = [&](int t) { if (one_each && t >= near0 && t < near1) ahead.find(a.buckets, far, t * KT + entry_distance); };
+    auto fetch = [&](int t) { if (one_each && t >= near0 && t < near1) ahead.fetch(entry_table, a.nb); };
+    find(mine0);
 
     u32x4 qf[NC];
 #pragma unroll
@@ -89,30 +124,19 @@ __global__ void __launch_bounds__(64 * W) seq_forward_kernel(SeqArgs a, SeqPlan 
             for (int s = 0; s < NC; ++s) qf[s] ^= kSign;
         }
     }
-    // Rows of the last tile that no load fills hold zeros, or the finite rows of an earlier tile: their weights are zero, and zero times
-    // whatever else LDS may hold need not be.
-    if (klen % KT != 0 && t0 < t1) {
-        for (uint32_t o = threadIdx.x * 16u; o < 4u * kTile; o += 64u * W * 16u) *reinterpret_cast<u32x4*>(lds + o) = u32x4{0u, 0u, 0u, 0u};
-        __syncthreads();
-    }
-    if (t0 < t1) issue(0);
-
-    const float* const table = a.table ? a.table + (size_t)head * a.nb : nullptr;
-    const int far = a.far;
     const float below = table ? seq_bias_at(table, a.buckets, a.nb, far, -far) : 0.f, above = table ? seq_bias_at(table, a.buckets, a.nb, far, far) : 0.f;
+    fetch(mine0);
+    find(mine0 + TURN);
     // A bias that is one value for the tile joins the reference in the exponent's one fused operation; a large one, beside which the score would
     // lose its bits in the sum and not in the difference, is added first, as everywhere else.
     const bool modest = !__any(!(fabsf(below) < 256.f && fabsf(above) < 256.f));
-    // tiles whose distances are not all cut off: near0 .. near1 - 1; tiles with a pair that a length or causality shuts out: from mask0 on
-    int near0 = 0, near1 = 0, mask0 = klen / KT;
-    seq_near_tiles(a.table != nullptr, first, last, far, KT, near0, near1);
-    if (a.causal && first < klen) {
-        const int to = first + 1 > 0 ? (first + 1) / KT : 0;
-        mask0 = to < mask0 ? to : mask0;
+    // Rows of the last tile that no load fills hold zeros, or the finite rows of an earlier tile: their weights are zero, and zero times
+    // whatever else LDS may hold need not be.
+    if (klen % KT != 0 && t0 < t1) {
+        for (uint32_t o = threadIdx.x * 16u; o < (KEYS ? 4u * W : 4u) * kTile; o += 64u * W * 16u) *reinterpret_cast<u32x4*>(lds + o) = u32x4{0u, 0u, 0u, 0u};
+        __syncthreads();
     }
-    const uint32_t span = (uint32_t)(KT + span_rows - 1), entries = plan.packed ? span * G : span, bias_bytes = 4u * plan.bias_entries;
-    const uint32_t my_bias = bias_at + 4u * ((uint32_t)g * span + (uint32_t)(last - pos) + 4u * hi);
-    const float* const group_table = a.table + (size_t)(plan.packed ? hk * G : hk) * a.nb;
+    if (mine0 < t1) issue(0);
 
     f32x16 o[NB];
 #pragma unroll
@@ -121,37 +145,26 @@ __global__ void __launch_bounds__(64 * W) seq_forward_kernel(SeqArgs a, SeqPlan 
     const int lim = a.causal && pos + 1 < klen ? pos + 1 : klen;
     const float scale = fabsf(a.scale) * kLog2e;
 
-    SeqBiasAhead ahead = {0u, 0u, 0.f};
-    if constexpr (W == 4) {
-        if (t0 >= near0 && t0 < near1) {
-            ahead.find(a.buckets, far, t0 * KT - last + (int)threadIdx.x);
-            ahead.fetch(group_table, a.nb);
-        }
-        if (t0 + 1 >= near0 && t0 + 1 < near1) ahead.find(a.buckets, far, (t0 + 1) * KT - last + (int)threadIdx.x);
-    }
     auto step = [&](auto parity, int t) {
-        constexpr uint32_t B = decltype(parity)::value;
+        const uint32_t B = parity;
         const uint32_t kt = base + B * 2u * kTile, vt = kt + kTile;
         const int j0 = t * KT;
         const bool near = t >= near0 && t < near1;
         if (near) {
-            if constexpr (W == 4) {
-                if (threadIdx.x < entries) seq_lds_put(bias_at + B * bias_bytes + 4u * threadIdx.x, ahead.get(a.nb));
+            if (one_each) {
+                if (entry < entries) seq_lds_put(bias_at + B * bias_bytes + 4u * entry, ahead.get(a.nb));
             } else {
-                for (uint32_t e = threadIdx.x; e < entries; e += 64u * W) {
-                    const uint32_t ge = plan.packed ? e / span : 0u;
-                    seq_lds_put(bias_at + B * bias_bytes + 4u * e,
-                                seq_bias_at(group_table + (size_t)ge * a.nb, a.buckets, a.nb, far, j0 - last + (int)(e - ge * span)));
+                for (uint32_t e = entry; e < entries; e += KEYS ? 64u : 64u * W) {
+                    const uint32_t ge = e / span;
+                    seq_lds_put(bias_at + B * bias_bytes + 4u * e, seq_bias_at(group_table + (size_t)ge * a.nb, a.buckets, a.nb, far, j0 - last + (int)(e - ge * span)));
                 }
             }
         }
         lds_loads_done();
-        __syncthreads();
-        if constexpr (W == 4) {
-            if (t + 1 >= near0 && t + 1 < near1) ahead.fetch(group_table, a.nb);
-            if (t + 2 >= near0 && t + 2 < near1) ahead.find(a.buckets, far, j0 + 2 * KT - last + (int)threadIdx.x);
-        }
-        if (t + 1 < t1) issue(B ^ 1u);
+        if constexpr (!KEYS) __syncthreads();
+        fetch(t + TURN);
+        find(t + 2 * TURN);
+        if (t + TURN < t1) issue(B ^ 1u);
 
         f32x16 s[KS];
 #pragma unroll
@@ -211,12 +224,61 @@ __global__ void __launch_bounds__(64 * W) seq_forward_kernel(SeqArgs a, SeqPlan 
             column_reader.accumulate(o, vt, k, s[k]);
         }
     };
-    for (int t = t0; t < t1; t += 2) {
-        step(std::integral_constant<uint32_t, 0>{}, t);
-        if (t + 1 < t1) step(std::integral_constant<uint32_t, 1>{}, t + 1);
+    if constexpr (KEYS) {  // few tiles: less code to fetch before fewer additions for addresses
+        uint32_t parity = 0;
+        for (int t = mine0; t < t1; t += TURN, parity ^= 1u) step(parity, t);
+    } else {
+        for (int t = mine0; t < t1; t += 2) {
+            step(std::integral_constant<uint32_t, 0>{}, t);
+            if (t + 1 < t1) step(std::integral_constant<uint32_t, 1>{}, t + 1);
+        }
     }
 
     l = seq_sum_halves(l);
+    if constexpr (KEYS && W > 1) {
+        // sums of all waves through LDS, rows 4 floats apart from a multiple of the banks; the last wave has them, the others are done
+        constexpr uint32_t kRow = 4u * (D + 4);
+        const uint32_t all = lds_offset(lds), sums = all + W * 32u * kRow;
+        __syncthreads();
+        if (hi == 0) *(__attribute__((address_space(3))) f32x2*)(uintptr_t)(sums + 8u * (32u * wave + c)) = f32x2{m, l};
+        __syncthreads();
+        float top = -__builtin_inff(), total = 0.f, mine = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) top = fmaxf(top, (*(const __attribute__((address_space(3))) f32x2*)(uintptr_t)(sums + 8u * (32u * w + c)))[0]);
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const f32x2 x = *(const __attribute__((address_space(3))) f32x2*)(uintptr_t)(sums + 8u * (32u * w + c));
+            const float f = x[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[0] - top);  // a part without weight may have no reference
+            total += f * x[1];
+            if (w == (int)wave) mine = f;
+        }
+        if (wave != W - 1) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *(__attribute__((address_space(3))) f32x4*)(uintptr_t)(all + kRow * (32u * wave + c) + 4u * (32 * b + 8 * q + 4 * hi)) =
+                        f32x4{o[b][4 * q] * mine, o[b][4 * q + 1] * mine, o[b][4 * q + 2] * mine, o[b][4 * q + 3] * mine};
+        }
+        __syncthreads();
+        if (wave != W - 1) return;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[b][r] *= mine;
+#pragma unroll
+        for (int w = 0; w < W - 1; ++w)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4 x = seq_lds_f32x4(all + kRow * (32u * w + c) + 4u * (32 * b + 8 * q + 4 * hi));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[b][4 * q + e] += x[e];
+                }
+        m = top;
+        l = total;
+    }
     if (!exists) return;
     if (i >= qlen) { m = -__builtin_inff(); l = 0.f; }
     const size_t row = ((size_t)n * a.H + head) * a.Lq + i;
@@ -277,11 +339,11 @@ __global__ void __launch_bounds__(256) seq_join_kernel(SeqArgs a, SeqPlan plan) 
     if (a.stats && channel == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * row) = f32x2{any ? top : -__builtin_inff(), any ? log2f(l) : 0.f};
 }
 
-template <class T, int D, int W>
+template <class T, int D, int W, int KT, bool KEYS>
 hipError_t launch(const SeqArgs& a, SeqPlan& plan, hipStream_t s) {
-    constexpr int KT = seq_forward_keys(D * SeqSize<T>::value, W);
-    const size_t lds = 4 * (size_t)KT * D * SeqSize<T>::value + 2 * sizeof(float) * plan.bias_entries;
-    auto* const kernel = &seq_forward_kernel<T, D, W, KT>;
+    constexpr size_t tiles = 4 * (size_t)KT * D * SeqSize<T>::value * (KEYS ? W : 1), sums = KEYS && W > 1 ? (size_t)W * 32 * (4 * (D + 4) + 8) : 0;
+    const size_t bias = 2 * sizeof(float) * plan.bias_entries * (KEYS ? W : 1), lds = tiles + bias > sums ? tiles + bias : sums;
+    auto* const kernel = &seq_forward_kernel<T, D, W, KT, KEYS>;
     hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), lds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(plan.grid), dim3(64 * W), lds, s, a, plan);
@@ -291,16 +353,16 @@ hipError_t launch(const SeqArgs& a, SeqPlan& plan, hipStream_t s) {
     hipLaunchKernelGGL((seq_join_kernel<T, D>), dim3((unsigned)blocks), dim3(256), 0, s, a, plan);
     return hipGetLastError();
 }
+template <class T, int D>
+hipError_t launch(const SeqArgs& a, SeqPlan& plan, hipStream_t s) {
+    constexpr int RB = D * SeqSize<T>::value;
+    return plan.keys ? launch<T, D, seq_keys_waves(RB), seq_forward_keys(RB, true), true>(a, plan, s) : launch<T, D, 4, seq_forward_keys(RB, false), false>(a, plan, s);
+}
 template <class T>
 hipError_t launch(const SeqArgs& a, SeqPlan& plan, hipStream_t s) {
-    if (plan.waves == 1) {
-        if (a.D == 32) return launch<T, 32, 1>(a, plan, s);
-        if (a.D == 64) return launch<T, 64, 1>(a, plan, s);
-        return launch<T, 128, 1>(a, plan, s);
-    }
-    if (a.D == 32) return launch<T, 32, 4>(a, plan, s);
-    if (a.D == 64) return launch<T, 64, 4>(a, plan, s);
-    return launch<T, 128, 4>(a, plan, s);
+    if (a.D == 32) return launch<T, 32>(a, plan, s);
+    if (a.D == 64) return launch<T, 64>(a, plan, s);
+    return launch<T, 128>(a, plan, s);
 }
 
 }  // namespace
@@ -309,24 +371,29 @@ bool seq_forward_plan(const SeqArgs& a, SeqPlan& p) {
     const int size = a.dtype == 0 ? 4 : 2, cus = cu_count();
     p.group = a.H / a.KV;
     p.packed = (long long)p.group * a.Lq <= 32;
-    p.waves = p.packed || a.Lq <= 32 ? 1 : 4;
-    const int KT = seq_forward_keys(a.D * size, p.waves);
-    p.blocks = p.packed ? 1 : (a.Lq + 32 * p.waves - 1) / (32 * p.waves);
-    const double base = (double)a.N * (p.packed ? a.KV : a.H) * p.blocks;
-    // Workgroups that fill the device: a wave of its own each (four to five on a CU by LDS), or four waves each (two to four).
-    // Fewer than that share out the keys, no more than leaves each two tiles.
-    const double want = (p.waves == 1 ? 4.0 : 2.0) * cus;
-    const int tiles = (a.Lk + KT - 1) / KT;
-    long long splits = (long long)(want / (base > 1 ? base : 1));
-    if (splits > tiles / 2) splits = tiles / 2;
-    if (splits > 64) splits = 64;
+    const int RB = a.D * size;
+    const double heads = (double)a.N * (p.packed ? a.KV : a.H);
+    // Less than a workgroup of 128 rows for each CU: the waves share out the keys instead, and where that still leaves CUs without work, workgroups
+    // do too, no more of them than leaves each wave a tile.  (One for each CU, causal, 2 x 1023 tokens, 16 heads of 128: 33 us with rows, 46 with
+    // keys, which load each tile four times as often; 37 with workgroups of 64 rows.)
+    p.keys = p.packed || heads * ((a.Lq + 127) / 128) < cus;
+    p.waves = p.keys ? seq_keys_waves(RB) : 4;
+    const int KT = seq_forward_keys(RB, p.keys), rows = p.keys ? 32 : 128;
+    p.blocks = p.packed ? 1 : (a.Lq + rows - 1) / rows;
+    const double base = heads * p.blocks;
+    long long splits = 1;
+    if (p.keys) {
+        const int tiles = (a.Lk + KT - 1) / KT;
+        splits = (long long)(2.0 * cus / (base > 1 ? base : 1));
+        if (splits > tiles / p.waves) splits = tiles / p.waves;
+        if (splits > 64) splits = 64;
+    }
     p.splits = splits < 1 ? 1 : (int)splits;
     if ((base * p.splits + 8.0 * p.blocks * p.splits) * 64.0 * p.waves > 4.0e9) return false;  // threads of a launch
-    p.grid = seq_deal(p.deal, (long long)a.N * (p.packed ? a.KV : a.H), (long long)p.blocks * p.splits, a.causal && p.blocks > 1);
+    p.grid = seq_deal(p.deal, a.N, p.packed ? a.KV : a.H, (long long)p.blocks * p.splits, a.causal && p.blocks > 1);
     p.by_splits = make_fastdiv((uint32_t)p.splits);
-    p.by_heads = make_fastdiv((uint32_t)(p.packed ? a.KV : a.H));
     p.rows = (size_t)a.N * a.H * a.Lq;
-    p.bias_entries = a.table == nullptr ? 0 : p.packed ? (uint32_t)(p.group * (KT + a.Lq - 1)) : (uint32_t)(KT + 32 * p.waves - 1);
+    p.bias_entries = a.table == nullptr ? 0 : p.packed ? (uint32_t)(p.group * (KT + a.Lq - 1)) : (uint32_t)(KT + rows - 1);
     return true;
 }
 
