@@ -33,7 +33,7 @@ int check_sequence(fwa::SeqArgs& a, int64_t N, int Lq, int Lk, int heads, int kv
     if (d != 32 && d != 64 && d != 128) return FWA_ERR_UNSUPPORTED;
     if (heads > kMostHeads) return FWA_ERR_UNSUPPORTED;
     // one launch per kernel: fewer than 2^32 threads
-    if ((double)N * heads * ((Lq > Lk ? Lq : Lk) / 32 + 1.0) * 64.0 * 2.0 > 4.0e9) return FWA_ERR_UNSUPPORTED;
+    if ((double)N * heads * ((Lq > Lk ? Lq : Lk) / 128 + 1.0) * 256.0 > 3.9e9) return FWA_ERR_UNSUPPORTED;
     a.N = N; a.Lq = Lq; a.Lk = Lk; a.H = heads; a.KV = kv_heads; a.D = d; a.dtype = dtype;
     return FWA_OK;
 }

@@ -199,8 +199,8 @@ __device__ __forceinline__ void seq_zero(f32x16& x) {
 // One entry of the table in base-2 units.  Finite values keep finite in these units: the type's lowest value, which stands for a mask in
 // many programs, would otherwise turn into an infinity, and a row of nothing else would be empty instead of uniform.
 __device__ __forceinline__ float seq_bias_log2(float b) {
-    const float x = b * kLog2e;
-    return __builtin_isinf(b) ? b : fminf(fmaxf(x, -3.4e38f), 3.4e38f);
+    if (!(fabsf(b) < __builtin_inff())) return b;  // infinities and NaN
+    return fminf(fmaxf(b * kLog2e, -3.4e38f), 3.4e38f);
 }
 // The bias of distance key - query for a head's row of the table; entries of the map outside the table add nothing.
 __device__ __forceinline__ float seq_bias_at(const float* row, const int32_t* buckets, int nb, int far, int distance) {
