@@ -374,7 +374,7 @@ bool seq_forward_plan(const SeqArgs& a, SeqPlan& p) {
     const int RB = a.D * size;
     const double heads = (double)a.N * (p.packed ? a.KV : a.H);
     // Less than a workgroup of 128 rows for each CU: the waves share out the keys instead, and where that still leaves CUs without work, workgroups
-    // do too, no more of them than leaves each wave a tile.  (One for each CU, causal, 2 x 1023 tokens, 16 heads of 128: 33 us with rows, 46 with
+    // do too, no more of them than leaves each wave four tiles: a tile costs about 1 us where little runs, joining parts in memory 4.  (One for each CU, causal, 2 x 1023 tokens, 16 heads of 128: 33 us with rows, 46 with
     // keys, which load each tile four times as often; 37 with workgroups of 64 rows.)
     p.keys = p.packed || heads * ((a.Lq + 127) / 128) < cus;
     p.waves = p.keys ? seq_keys_waves(RB) : 4;
@@ -385,7 +385,7 @@ bool seq_forward_plan(const SeqArgs& a, SeqPlan& p) {
     if (p.keys) {
         const int tiles = (a.Lk + KT - 1) / KT;
         splits = (long long)(2.0 * cus / (base > 1 ? base : 1));
-        if (splits > tiles / p.waves) splits = tiles / p.waves;
+        if (splits > tiles / (4 * p.waves)) splits = tiles / (4 * p.waves);
         if (splits > 64) splits = 64;
     }
     p.splits = splits < 1 ? 1 : (int)splits;
