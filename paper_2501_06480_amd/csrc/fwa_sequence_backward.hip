@@ -18,6 +18,7 @@ struct BackPlan {
     SeqDeal row_deal, key_deal;
     uint32_t row_bias, key_bias;
     FastDiv by_splits;
+    int key_least;       // tiles of a part of a block of keys: a block has as many parts as that makes, `splits` at most
     int row_waves;       // waves with rows per head of a sequence: ceil(Lq / 32)
     float* delta;        // [N, H, Lq]
     float* ends;         // [H][N * row_waves][2]: sums of dS at and beyond -far and far
@@ -625,6 +626,18 @@ constexpr float seq_lift() { return __is_same(T, SeqF16) ? 6.f : 0.f; }
 
 constexpr bool seq_keys_v_in_lds(int row_bytes) { return row_bytes == 256; }
 
+// Tiles of queries that see a key of the block from j0 on: each of q0 .. q0 + each - 1, of every head that shares the keys.
+__device__ __forceinline__ void seq_key_tiles(bool causal, int qlen, int klen, int start, int j0, int size, int& q0, int& each) {
+    q0 = causal && j0 > start ? (j0 - start) / size : 0;
+    const int q1 = j0 < klen ? (qlen + size - 1) / size : 0;
+    each = q1 > q0 ? q1 - q0 : 0;
+}
+// Parts that a block of so many tiles has.
+__device__ __forceinline__ int seq_key_parts(int all, const BackPlan& plan) {
+    const int parts = (all + plan.key_least - 1) / plan.key_least;
+    return parts < plan.splits ? parts : plan.splits;
+}
+
 template <class T, int D, int W, int QT>
 __global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) seq_keys_kernel(SeqArgs a, BackPlan plan) {
     constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, QS = QT / 32;
@@ -647,11 +660,17 @@ __global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) 
     const int j0 = block * 32 * W, j = j0 + (int)(32u * wave + c), j_last = j0 + 32 * W - 1;
     const int qlen = seq_length(a.q_len, n, a.Lq), klen = seq_length(a.k_len, n, a.Lk), start = seq_start(a.q_start, n);
 
-    // tiles of queries with a key of this block, and the heads that share it, one after the other
-    int q0 = 0;
-    if (a.causal && j0 > start) q0 = (j0 - start) / QT;
-    const int q1 = j0 < klen ? (qlen + QT - 1) / QT : 0, each = q1 > q0 ? q1 - q0 : 0, all = each * plan.group;
-    const int per = (all + plan.splits - 1) / plan.splits, s0 = split * per, s1 = s0 + per < all ? s0 + per : all;
+    // the heads that share a block's keys one after the other
+    int q0, each, s0 = 0, s1;
+    seq_key_tiles(a.causal, qlen, klen, start, j0, QT, q0, each);
+    const int q1 = q0 + each, all = s1 = each * plan.group;
+    if (plan.splits > 1) {
+        const int parts = seq_key_parts(all, plan);
+        if (split >= parts) return;  // the joining kernel does not read it
+        const int per = (all + parts - 1) / parts;
+        s0 = split * per;
+        s1 = s0 + per < all ? s0 + per : all;
+    }
 
     const uint32_t qld = (uint32_t)(a.ldq * E), gld = (uint32_t)(a.ldg * E);
     SeqLoader<RB, QT, W> load_q, load_g;
@@ -760,8 +779,10 @@ __global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) 
         const int i = x.t * QT + (int)threadIdx.x;
         row_ahead = threadIdx.x < (uint32_t)QT && i < qlen;
         if (row_ahead) {
-            stat_ahead = reinterpret_cast<const f32x2*>(a.stats + 2 * next_row)[threadIdx.x];
-            delta_ahead = (plan.delta + next_row)[threadIdx.x];
+            const float *stats = a.stats + 2 * next_row, *deltas = plan.delta + next_row;
+            asm volatile("" : "+s"(stats), "+s"(deltas));  // in scalar registers, without an address of each thread's from tile to tile
+            stat_ahead = reinterpret_cast<const f32x2*>(stats)[threadIdx.x];
+            delta_ahead = deltas[threadIdx.x];
         }
     };
     SeqBiasAhead ahead = {0u, 0u, 0.f};
@@ -815,6 +836,9 @@ __global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) 
             if (s + 2 < s1) find(after);
             issue(next, B ^ 1u);
         }
+        // places formed anew in each tile: kept, they and others go to scratch, and what comes back from there waits for the loads of the next
+        // tile (57 us against 45, 2 x 1023 tokens, 4 heads of keys of 128)
+        if constexpr (VLDS) asm volatile("" : "+v"(row_reader.at), "+v"(column_reader.at));
         const int first = now.t * QT;
         bool plain = !__is_same(T, SeqF32) && modest && !near && now.t >= mask1;
         if (plain) plain = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, seq_lds_f32(zero_at + 4u * QT + 4u * B))) == 0;
@@ -828,7 +852,8 @@ __global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) 
         }
         if (!plain) {
             if (near) {
-                const uint32_t my_bias = bias_at + B * bias_bytes + 4u * ((uint32_t)(j_last - j) + 4u * hi);
+                uint32_t my_bias = bias_at + B * bias_bytes + 4u * ((uint32_t)(j_last - j) + 4u * hi);
+                asm volatile("" : "+v"(my_bias));  // one address and offsets, not 16 addresses kept from tile to tile
 #pragma unroll
                 for (int k = 0; k < QS; ++k)
 #pragma unroll
@@ -935,14 +960,20 @@ __global__ void __launch_bounds__(256) seq_join_keys_kernel(SeqArgs a, BackPlan 
     constexpr int E = SeqSize<T>::value;
     const size_t values = (size_t)a.N * a.Lk * a.KV * D, at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (at >= 2 * values) return;
+    const bool is_dv = at >= values;
+    const size_t in = is_dv ? at - values : at, row = in / ((size_t)a.KV * D), channel = in - row * ((size_t)a.KV * D);
+    const size_t n = row / a.Lk;
+    const int j = (int)(row - n * a.Lk);
+    int q0, each;
+    seq_key_tiles(a.causal, seq_length(a.q_len, n, a.Lq), seq_length(a.k_len, n, a.Lk), seq_start(a.q_start, n), j & -(32 * plan.key_waves),
+                  seq_backward_rows(D * E), q0, each);
+    const int parts = seq_key_parts(each * plan.group, plan);
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < plan.splits; ++s) {
+    for (int s = 0; s < parts; ++s) {
         const f32x4 x = *reinterpret_cast<const f32x4*>(plan.part_kv + (size_t)s * 2 * values + at);
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] += x[e];
     }
-    const bool is_dv = at >= values;
-    const size_t in = is_dv ? at - values : at, row = in / ((size_t)a.KV * D), channel = in - row * ((size_t)a.KV * D);
     const float f = __builtin_amdgcn_exp2f(-seq_lift<T>()) * (is_dv ? 1.f : a.scale);
     char* const to = static_cast<char*>(is_dv ? a.dv : a.dk) + row * a.lddk * E;
     seq_store4<T>(to, (uint32_t)channel, sum[0] * f, sum[1] * f, sum[2] * f, sum[3] * f);
@@ -1003,6 +1034,32 @@ hipError_t launch(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
     return launch<T, 128>(a, plan, s);
 }
 
+// Too few blocks of keys for the device: their queries are shared out, in parts of one size, two workgroups a CU, no part smaller than two tiles (four:
+// 28 us against 25.5, fp32, 4 x 515 tokens, 3 heads of 32).  Where a block's tiles are known to begin at the diagonal, those near the end
+// have fewer parts (as many parts for each block, of different sizes: 62 us against 57, 2 x 1023 tokens, 4 heads of keys of 128).
+void share_keys(const SeqArgs& a, BackPlan& p, int size, int key_block, double blocks, bool diagonal) {
+    const int cus = cu_count();
+    const long long tiles = (a.Lq + size - 1) / size, all = tiles * p.group;
+    p.splits = 1;
+    p.key_least = all > 1 ? (int)all : 1;
+    if (blocks > cus || all < 4) return;
+    const double wanted = 2.0 * cus / (double)(a.N * a.KV);  // parts, of the blocks of one head
+    auto parts = [&](long long least) {
+        if (!diagonal) return (double)p.key_blocks * (double)((all + least - 1) / least);
+        double sum = 0;
+        for (int b = 0; b < p.key_blocks; ++b) {
+            const long long q0 = (long long)b * key_block / size, own = tiles > q0 ? (tiles - q0) * p.group : 0;
+            sum += (double)((own + least - 1) / least);
+        }
+        return sum;
+    };
+    long long least = (all + 15) / 16;
+    if (least < 2) least = 2;
+    while (least < all && parts(least) > wanted) least += least / 16 + 1;
+    p.key_least = (int)least;
+    p.splits = (int)((all + least - 1) / least);
+}
+
 bool back_plan(const SeqArgs& a, BackPlan& p) {
     const int cus = cu_count();
     p.group = a.H / a.KV;
@@ -1016,16 +1073,11 @@ bool back_plan(const SeqArgs& a, BackPlan& p) {
     p.key_blocks = (a.Lk + key_block - 1) / key_block;
     p.row_waves = (a.Lq + 31) / 32;
     const double rows = (double)a.N * a.H * p.row_blocks, keys = (double)a.N * a.KV * p.key_blocks;
-    // Too few blocks of keys for the device: their queries are shared out, no more than leaves each two tiles.
-    const long long all = (long long)((a.Lq + KT - 1) / KT) * p.group;
-    long long splits = (long long)(2.0 * cus / (keys > 1 ? keys : 1));
-    if (splits > all / 2) splits = all / 2;
-    if (splits > 16) splits = 16;
-    p.splits = splits < 1 ? 1 : (int)splits;
+    share_keys(a, p, KT, key_block, keys, a.causal && a.q_start == nullptr);
     // threads of a launch
     if ((rows + 8.0 * p.row_blocks) * 64 * p.waves > 4.0e9 || (keys + 8.0 * p.key_blocks) * p.splits * 64 * p.key_waves > 4.0e9) return false;
     p.row_grid = seq_deal(p.row_deal, a.N, a.H, p.row_blocks, a.causal && p.row_blocks > 1);
-    p.key_grid = seq_deal(p.key_deal, a.N, a.KV, (long long)p.key_blocks * p.splits, a.causal && p.key_blocks > 1);
+    p.key_grid = seq_deal(p.key_deal, a.N, a.KV, (long long)p.key_blocks * p.splits, a.causal && p.key_blocks > 1 && p.splits == 1);
     p.by_splits = make_fastdiv((uint32_t)p.splits);
     p.row_bias = a.table ? (uint32_t)((p.keys ? 32 : KT) + block - 1) : 0u;
     p.key_bias = a.table ? (uint32_t)(KT + key_block - 1) : 0u;
@@ -1068,10 +1120,14 @@ size_t table_bytes(const SeqArgs& a, const BackPlan& p) {
 
 // workspace: delta, the parts of dK and dV, the sums of dS by distance
 size_t seq_backward_workspace(const SeqArgs& a, bool want_dtable) {
-    BackPlan p;
-    if (!back_plan(a, p)) return 0;
+    BackPlan p, other;
+    SeqArgs b = a;
+    b.causal = 1;  // of the two ways to share the keys out the one with more parts
+    b.q_start = nullptr;
+    if (!back_plan(a, p) || !back_plan(b, other)) return 0;
     size_t bytes = padded((size_t)a.N * a.H * a.Lq);
-    if (p.splits > 1) bytes += padded((size_t)p.splits * 2 * a.N * a.Lk * a.KV * a.D);
+    const int splits = p.splits > other.splits ? p.splits : other.splits;
+    if (splits > 1) bytes += padded((size_t)splits * 2 * a.N * a.Lk * a.KV * a.D);
     if (want_dtable) bytes += table_bytes(a, p);
     return bytes;
 }
