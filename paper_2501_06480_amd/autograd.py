@@ -10,7 +10,8 @@ Both take the mask either as a dense fp32 ``mask`` [nW, L, L] or as int32 region
 
 ``bucket_bias(table, buckets, Lq, Lk)`` is the dense bias of 1-D distances by buckets, differentiable in the table: the
 ``bias`` of a window attention of such a sequence.  ``sequence_attention(q, k, v, heads, scale, table, buckets, ...)`` is
-attention of whole sequences, which forms that bias inside its kernels.
+attention of whole sequences, which forms that bias inside its kernels.  As with any node of torch: a backward pass that is to be
+captured into a graph runs with leaves whose earlier eager graphs are gone.
 """
 from __future__ import annotations
 
