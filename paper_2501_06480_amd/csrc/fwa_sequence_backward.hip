@@ -30,6 +30,10 @@ struct BackPlan {
 };
 
 constexpr float kDead = __builtin_inff();
+// Half data: P and dS are taken 2^6 times as large and the sums divided again, since a probability of 2^-14 and less (keys by the
+// thousand) has fewer bits in that type; dS beyond 1023 overflows.
+template <class T>
+constexpr float seq_lift() { return __is_same(T, SeqF16) ? 6.f : 0.f; }
 // Rows that see few keys: one of these may have nearly all the weight, dP - delta cancels, and the rounding of o would show.  There a walk in
 // front of the other forms delta from the same products as dP.  (The rows of a causal call that see up to two tiles are a block.)
 constexpr int kFewTiles = 2;
@@ -46,6 +50,8 @@ __device__ __forceinline__ float plain_sum(float a, float b) {
 }
 
 // Two forms, as in the forward: the waves have 32 rows each and share the tiles, or (KEYS) the same 32 rows and every W-th tile each.
+// The row's sum is divided out of dQ at the end, but for half data, where it is in the exponent together with the lift: dS times a sum of thousands leaves
+// that type's range.
 // Bound by vector instructions between the three products and by the latency of a tile (4 ragged sequences of up to 2048 tokens, 12 heads of 64, bf16:
 // 111 us, vector units 43 per cent busy, matrix units 25).
 template <class T, int D, int W, int KT, bool TABLE, bool KEYS>
@@ -99,7 +105,8 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
 
     const size_t row = ((size_t)n * a.H + head) * a.Lq + i;
     bool dead = true;
-    float ref = 0.f, rl = 0.f, delta = 0.f;
+    constexpr bool HALF = __is_same(T, SeqF16);
+    float ref = 0.f, log_sum = 0.f, rl = 0.f, delta = 0.f;  // log_sum: what the exponent takes besides the reference; rl: what is left to multiply with
     u32x4 qf[NC], gf[NC];
 #pragma unroll
     for (int s = 0; s < NC; ++s) qf[s] = gf[s] = u32x4{0u, 0u, 0u, 0u};
@@ -107,7 +114,8 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
         const f32x2 stat = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
         dead = stat[0] == -__builtin_inff();
         ref = dead ? 0.f : stat[0];
-        rl = dead || seq_lone(a.causal, start, qlen, klen) ? 0.f : __builtin_amdgcn_exp2f(-stat[1]);
+        if (HALF && !dead) log_sum = stat[1] - seq_lift<T>();
+        rl = dead || seq_lone(a.causal, start, qlen, klen) ? 0.f : __builtin_amdgcn_exp2f(HALF ? -seq_lift<T>() : -stat[1]);
         const size_t at_row = (size_t)n * a.Lq + i, channel = (size_t)head * D;
         const char* const qp = static_cast<const char*>(a.q) + (at_row * a.ldq + channel) * E + 16u * hi;
         const char* const gp = static_cast<const char*>(a.d_o) + (at_row * a.ldg + channel) * E + 16u * hi;
@@ -135,6 +143,9 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
     }
     delta = seq_sum_halves(delta);
     const bool some_dead = __any(dead);
+    // one number for both where the reference is not large, as in the keys kernel
+    const bool large = HALF && __any(fabsf(ref) > 1024.f && ref != -__builtin_inff());
+    const float off_exponent = HALF ? ref + log_sum : ref;
     if (klen % KT != 0 && tiles > 0) {  // rows that no load fills: as in the forward
         for (uint32_t o = threadIdx.x * 16u; o < (KEYS ? 4u * W : 4u) * kTile; o += 64u * W * 16u) *reinterpret_cast<u32x4*>(lds + o) = u32x4{0u, 0u, 0u, 0u};
         __syncthreads();
@@ -202,8 +213,8 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
         }
         return x;
     };
-    // Q K^T of tile t, or, where the bias is not one value or pairs are shut out, the scores; the exponent of a weight, the row's sum not divided
-    // out, is s mul + minus
+    // Q K^T of tile t, or, where the bias is not one value or pairs are shut out, the scores; the exponent of a weight, the row's sum (but of half
+    // data) not divided out, is s mul + minus
     struct Exponent { float mul, minus; };
     auto scores = [&](auto parity, int t, f32x16 (&s)[KS]) -> Exponent {
         const uint32_t B = parity;
@@ -215,7 +226,7 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
             for (int x = 0; x < NC; ++x) s[k] = seq_dot<T>(row_reader.read(kt, x, k), qf[x], s[k]);
         }
         const float flat = t < near0 ? below : above;
-        const bool near = t >= near0 && t < near1, plain = modest && !near && t < mask0;
+        const bool near = t >= near0 && t < near1, plain = modest && !near && t < mask0 && !large;
         if (!plain) {
             if (near) {
 #pragma unroll
@@ -235,8 +246,14 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[k][r] = 32 * k + 8 * (r / 4) + r % 4 < room ? s[k][r] : -__builtin_inff();
             }
+            if (large) {
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[k][r] -= ref;
+            }
         }
-        return {plain ? scale : 1.f, plain ? flat - ref : -ref};
+        return {plain ? scale : 1.f, plain ? flat - off_exponent : large ? -log_sum : -off_exponent};
     };
 
     f32x16 dq[NB];
@@ -622,11 +639,6 @@ __global__ void __launch_bounds__(256) seq_lines_kernel(SeqArgs a, BackPlan plan
     sum += __shfl_xor(sum, 2, 64);
     if (d < far && (threadIdx.x & 3u) == 0) line[far + d] = sum;
 }
-
-// Half data: P and dS are taken 2^6 times as large and the sums divided again, since a probability of 2^-14 and less (keys by the
-// thousand) has fewer bits in that type; dS beyond 1023 overflows.
-template <class T>
-constexpr float seq_lift() { return __is_same(T, SeqF16) ? 6.f : 0.f; }
 
 constexpr bool seq_keys_v_in_lds(int row_bytes) { return row_bytes == 256; }
 
