@@ -948,6 +948,13 @@ __global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) 
 #pragma unroll
         for (int b = 0; b < NB; ++b) seq_zero(dk[b]);
     }
+    if (j >= klen) {  // padding has nothing of a row of NaN either
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            seq_zero(dk[b]);
+            seq_zero(dv[b]);
+        }
+    }
     if (plan.splits > 1) {
         const size_t values = (size_t)a.N * a.Lk * a.KV * D, to = (row * a.KV + kv) * D;
         float* const into = plan.part_kv + (size_t)split * 2 * values + to;
