@@ -43,6 +43,8 @@ constexpr int kFewTiles = 2;
 __device__ __forceinline__ bool seq_lone(bool causal, int start, int qlen, int klen) {
     return klen <= 1 || (causal && start + qlen <= 1);
 }
+// Whether a row's statistics are those of a row without a key; a row of NaN alone has (-inf, NaN).
+__device__ __forceinline__ bool seq_dead(const f32x2& stat) { return stat[0] == -__builtin_inff() && stat[1] == 0.f; }
 // a sum that is not fused with a product it takes in: the two forms of the rows kernel give the same bits
 __device__ __forceinline__ float plain_sum(float a, float b) {
 #pragma clang fp contract(off)
@@ -112,7 +114,7 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
     for (int s = 0; s < NC; ++s) qf[s] = gf[s] = u32x4{0u, 0u, 0u, 0u};
     if (i < qlen) {
         const f32x2 stat = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
-        dead = stat[0] == -__builtin_inff();
+        dead = seq_dead(stat);
         ref = dead ? 0.f : stat[0];
         if (HALF && !dead) log_sum = stat[1] - seq_lift<T>();
         rl = dead || seq_lone(a.causal, start, qlen, klen) ? 0.f : __builtin_amdgcn_exp2f(HALF ? -seq_lift<T>() : -stat[1]);
@@ -503,7 +505,7 @@ __global__ void __launch_bounds__(256) seq_table_kernel(SeqArgs a, BackPlan plan
         const Block now = at_item(item);
         if constexpr (!AHEAD) fetch(now, mine);
         item = find(item + plan.chunks);
-        const bool live = mine.stat[0] != -__builtin_inff();
+        const bool live = !seq_dead(mine.stat);
         const int pos = now.start + now.i0 + (int)(32u * wave + c);
         const int lim = !live ? 0 : (a.causal && pos + 1 < now.klen ? pos + 1 : now.klen);
         // reference and sum as one number where the reference is not large (as in the keys kernel; its rounding is one factor for the row)
@@ -834,7 +836,7 @@ __global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) 
             }
         }
         if (threadIdx.x < (uint32_t)QT) {
-            const bool live = row_ahead && stat_ahead[0] != -__builtin_inff();
+            const bool live = row_ahead && !seq_dead(stat_ahead);
             const float ref = live ? stat_ahead[0] : 0.f, l = live ? stat_ahead[1] - seq_lift<T>() : kDead;
             seq_lds_put(stat + 4u * threadIdx.x, flat - (ref + l));
             seq_lds_put(stat + 4u * (QT + threadIdx.x), ref);
@@ -946,7 +948,9 @@ __global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) 
     const size_t row = (size_t)n * a.Lk + j;
     if (lone) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b) seq_zero(dk[b]);
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dk[b][r] = dk[b][r] != dk[b][r] ? dk[b][r] : 0.f;
     }
     if (j >= klen) {  // padding has nothing of a row of NaN either
 #pragma unroll
