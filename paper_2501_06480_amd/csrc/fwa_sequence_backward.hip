@@ -203,15 +203,17 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
             }
         }
     };
-    // a sum over the waves that share the rows, in the order of the waves
+    // a sum over the waves that share the rows, in the order of the waves; in a place behind the tiles, whose rows that no load fills have to keep
+    // what they hold for the next walk
     auto over_waves = [&](float x) {
         if constexpr (KEYS && W > 1) {
+            const uint32_t sums = lds_offset(lds) + 4u * W * kTile + 2u * W * bias_bytes;
             __syncthreads();
-            if (hi == 0) seq_lds_put(lds_offset(lds) + 4u * (32u * wave + c), x);
+            if (hi == 0) seq_lds_put(sums + 4u * (32u * wave + c), x);
             __syncthreads();
             x = 0.f;
 #pragma unroll
-            for (int w = 0; w < W; ++w) x += seq_lds_f32(lds_offset(lds) + 4u * (32u * w + c));
+            for (int w = 0; w < W; ++w) x += seq_lds_f32(sums + 4u * (32u * w + c));
         }
         return x;
     };
@@ -1034,7 +1036,8 @@ hipError_t launch_table(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
 template <class T, int D, int W, int KT, bool KEYS>
 hipError_t launch_rows(const SeqArgs& a, const BackPlan& plan, hipStream_t s) {
     constexpr size_t tiles = 4 * (size_t)KT * D * SeqSize<T>::value * (KEYS ? W : 1), sums = KEYS && W > 1 ? (size_t)W * 32 * 4 * (D + 4) : 0;
-    const size_t bias = 2 * sizeof(float) * plan.row_bias * (KEYS ? W : 1), lds = tiles + bias > sums ? tiles + bias : sums;
+    constexpr size_t over_waves = KEYS && W > 1 ? sizeof(float) * 32 * W : 0;
+    const size_t bias = 2 * sizeof(float) * plan.row_bias * (KEYS ? W : 1), ahead = tiles + bias + over_waves, lds = ahead > sums ? ahead : sums;
     return a.dtable ? start(&seq_rows_kernel<T, D, W, KT, true, KEYS>, dim3(plan.row_grid), 64 * W, lds, s, a, plan)
                     : start(&seq_rows_kernel<T, D, W, KT, false, KEYS>, dim3(plan.row_grid), 64 * W, lds, s, a, plan);
 }
