@@ -34,9 +34,11 @@ constexpr float kDead = __builtin_inff();
 // thousand) has fewer bits in that type; dS beyond 1023 overflows.
 template <class T>
 constexpr float seq_lift() { return __is_same(T, SeqF16) ? 6.f : 0.f; }
-// Rows that see few keys: one of these may have nearly all the weight, dP - delta cancels, and the rounding of o would show.  There a walk in
-// front of the other forms delta from the same products as dP.  (The rows of a causal call that see up to two tiles are a block.)
-constexpr int kFewTiles = 2;
+// Rows that see few keys: one of these may have nearly all the weight, dP - delta cancels, and the rounding of o would show (bf16, rows of up to 128 keys of
+// width 128: elements of dQ up to 1.4e-2 off, now within half a step of each dS).  There a walk in front of the other forms delta from the same products as
+// dP.  At every width and in both forms up to this many keys, which the first block of a causal call has; waves that share out the keys
+// and have two tiles each are as quick about more.
+constexpr int kFewKeys = 128;
 
 // Whether no query of a sequence sees more than one key: its weight is one and stays so, and all but dV is exactly zero, which products and their
 // differences need not be to the last bit.
@@ -265,7 +267,7 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
     for (int b = 0; b < NB; ++b) seq_zero(dq[b]);
     float ds_all = 0.f, ds_below = 0.f, ds_above = 0.f, p_below = 0.f, p_above = 0.f;
     start_walk();
-    if (tiles > 0 && tiles <= kFewTiles * (KEYS ? W : 1)) {
+    if (tiles > 0 && (tiles * KT <= kFewKeys || (KEYS && tiles <= 2 * W))) {
         float sum = 0.f;
         walk([&](auto parity, int t) {
             const uint32_t B = parity;
