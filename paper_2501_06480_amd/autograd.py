@@ -101,6 +101,12 @@ def window_attention_qkv(qkv, scale: float, bias=None, mask=None, labels=None, m
     return _WindowAttentionQKV.apply(qkv, bias, mask, scale, labels, float(mask_value))
 
 
+def _aligned(t):
+    """A contiguous tensor at an address that the library takes: the gradient of a part of a larger tensor may start at any of its elements."""
+    t = t.contiguous()
+    return t.clone() if t.data_ptr() % 16 else t
+
+
 class _BucketBias(torch.autograd.Function):
     @staticmethod
     def forward(ctx, table, buckets, Lq, Lk, q_start, dtype):
@@ -111,7 +117,7 @@ class _BucketBias(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dbias):
         buckets, = ctx.saved_tensors
-        return (binding.fwa_bucket_scatter(dbias.float().contiguous(), buckets.contiguous(), ctx.columns, ctx.q_start),) + (None,) * 5
+        return (binding.fwa_bucket_scatter(_aligned(dbias.float()), buckets.contiguous(), ctx.columns, ctx.q_start),) + (None,) * 5
 
 
 class _SequenceAttention(torch.autograd.Function):

@@ -513,6 +513,12 @@ using torch::autograd::variable_list;
 OptTensor opt(const at::Tensor& t) { return t.defined() ? OptTensor(t) : OptTensor(); }
 at::Tensor or_undefined(const OptTensor& t) { return t ? *t : at::Tensor(); }
 
+// a contiguous tensor at an address that the library takes: the gradient of a part of a larger tensor may start at any of its elements
+at::Tensor aligned(const at::Tensor& t) {
+    const at::Tensor c = t.contiguous();
+    return reinterpret_cast<uintptr_t>(c.data_ptr()) & 15u ? c.clone() : c;
+}
+
 std::string entry_name(const char* what, const OptTensor& bias, const OptTensor& labels) {
     return std::string(what) + (labels || (bias && bias->scalar_type() == at::kBFloat16) ? "_labels" : "_strided");
 }
@@ -622,7 +628,7 @@ struct BucketBias : torch::autograd::Function<BucketBias> {
         return with_python_errors([&]() -> variable_list {
             const variable_list s = ctx->get_saved_variables();
             at::Tensor dtable;
-            const int rc = run_bucket_scatter(dtable, grads[0].to(at::kFloat).contiguous(), s[0].contiguous(), ctx->saved_data["columns"].toInt(),
+            const int rc = run_bucket_scatter(dtable, aligned(grads[0].to(at::kFloat)), s[0].contiguous(), ctx->saved_data["columns"].toInt(),
                                               ctx->saved_data["q_start"].toInt(), std::nullopt, std::nullopt);
             if (rc != FWA_OK) raise_status(rc, "fwa_bucket_scatter");
             return {dtable, at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()};
