@@ -131,7 +131,7 @@ class _SequenceAttention(torch.autograd.Function):
     @staticmethod
     def backward(ctx, d_o):
         q, k, v, o, stats, table, buckets, q_lengths, k_lengths, q_start = ctx.saved_tensors
-        dq, dk, dv, dtable = binding.fwa_sequence_backward(q, k, v, o, stats, d_o.contiguous(), ctx.heads, ctx.scale, table, buckets, q_lengths,
+        dq, dk, dv, dtable = binding.fwa_sequence_backward(q, k, v, o, stats, _aligned(d_o), ctx.heads, ctx.scale, table, buckets, q_lengths,
                                                            k_lengths, q_start, ctx.causal, want_dtable=table is not None and ctx.needs_input_grad[3])
         return (dq, dk, dv, dtable) + (None,) * 7
 

@@ -652,7 +652,7 @@ struct SequenceAttention : torch::autograd::Function<SequenceAttention> {
         return with_python_errors([&]() -> variable_list {
             const variable_list s = ctx->get_saved_variables();
             Grads d;
-            const int rc = run_sequence_backward(d, s[0], s[1], s[2], s[3], s[4], grads[0].contiguous(), ctx->saved_data["heads"].toInt(),
+            const int rc = run_sequence_backward(d, s[0], s[1], s[2], s[3], s[4], aligned(grads[0]), ctx->saved_data["heads"].toInt(),
                                                  ctx->saved_data["scale"].toDouble(), opt(s[5]), opt(s[6]), opt(s[7]), opt(s[8]), opt(s[9]),
                                                  ctx->saved_data["causal"].toBool(), s[5].defined() && ctx->needs_input_grad(3), std::nullopt, std::nullopt,
                                                  std::nullopt, std::nullopt, std::nullopt);
