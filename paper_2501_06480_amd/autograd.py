@@ -107,6 +107,14 @@ def _aligned(t):
     return t.clone() if t.data_ptr() % 16 else t
 
 
+def _saved_rows(t):
+    """A saved [N, L, C] tensor as it is, or a copy where a hook handed it back in a layout that the calls do not take."""
+    N, L, C = t.shape
+    even = t.is_contiguous() or ((C == 1 or t.stride(2) == 1) and (L <= 1 or t.stride(1) >= C) and (N <= 1 or t.stride(0) == L * t.stride(1)))
+    ld = C if t.is_contiguous() else t.stride(1) if L > 1 else t.stride(0)
+    return t if even and ld * t.element_size() % 16 == 0 and t.data_ptr() % 16 == 0 else _aligned(t)
+
+
 class _BucketBias(torch.autograd.Function):
     @staticmethod
     def forward(ctx, table, buckets, Lq, Lk, q_start, dtype):
@@ -130,7 +138,10 @@ class _SequenceAttention(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, d_o):
-        q, k, v, o, stats, table, buckets, q_lengths, k_lengths, q_start = ctx.saved_tensors
+        q, k, v, o = (_saved_rows(t) for t in ctx.saved_tensors[:4])
+        if k.stride() != v.stride():  # one stride for both
+            k, v = _aligned(k), _aligned(v)
+        stats, table, buckets, q_lengths, k_lengths, q_start = (None if t is None else _aligned(t) for t in ctx.saved_tensors[4:])
         dq, dk, dv, dtable = binding.fwa_sequence_backward(q, k, v, o, stats, _aligned(d_o), ctx.heads, ctx.scale, table, buckets, q_lengths,
                                                            k_lengths, q_start, ctx.causal, want_dtable=table is not None and ctx.needs_input_grad[3])
         return (dq, dk, dv, dtable) + (None,) * 7

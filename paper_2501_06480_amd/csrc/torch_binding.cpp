@@ -57,16 +57,20 @@ struct Rows {
     void* p;
     int64_t ld;
 };
+std::optional<int64_t> row_stride(const at::Tensor& t) {
+    const int64_t N = t.size(0), L = t.size(1), C = t.size(2);
+    if (t.is_contiguous()) return C;
+    const int64_t s0 = t.stride(0), s1 = t.stride(1), s2 = t.stride(2);
+    if ((C > 1 && s2 != 1) || (L > 1 && s1 < C) || (N > 1 && s0 != L * s1)) return std::nullopt;
+    return L > 1 ? s1 : (N > 1 ? s0 : C);
+}
 Rows rows_of(const at::Tensor& t, const char* name, const at::Tensor* like) {
     need_gpu(t, name);
     if (t.dim() != 3) value_error(std::string(name) + " must be [N, L, C]");
     if (like) need_like(t, name, *like);
-    const int64_t N = t.size(0), L = t.size(1), C = t.size(2);
-    if (t.is_contiguous()) return {t.data_ptr(), C};
-    const int64_t s0 = t.stride(0), s1 = t.stride(1), s2 = t.stride(2);
-    if ((C > 1 && s2 != 1) || (L > 1 && s1 < C) || (N > 1 && s0 != L * s1))
-        value_error(std::string(name) + ": channels must be contiguous and token rows evenly spaced");
-    return {t.data_ptr(), L > 1 ? s1 : (N > 1 ? s0 : C)};
+    const std::optional<int64_t> ld = row_stride(t);
+    if (!ld) value_error(std::string(name) + ": channels must be contiguous and token rows evenly spaced");
+    return {t.data_ptr(), *ld};
 }
 
 // The additive terms: bias [heads, L, L] fp32 or bf16, and a dense mask [nW, L, L] or int32 labels [nW, L].
@@ -635,6 +639,11 @@ struct BucketBias : torch::autograd::Function<BucketBias> {
         });
     }
 };
+// Saved tensors may come back from a hook in another layout, or at another address, than they were saved in: those the call does not take are copied.
+at::Tensor saved_rows(const at::Tensor& t) {
+    const std::optional<int64_t> ld = row_stride(t);
+    return ld && (*ld * t.element_size()) % 16 == 0 && (reinterpret_cast<uintptr_t>(t.data_ptr()) & 15u) == 0 ? t : aligned(t);
+}
 struct SequenceAttention : torch::autograd::Function<SequenceAttention> {
     static at::Tensor forward(AutogradContext* ctx, const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, const OptTensor& table, const OptTensor& buckets,
                               const OptTensor& q_lengths, const OptTensor& k_lengths, const OptTensor& q_start, int64_t heads, double scale, bool causal) {
@@ -651,9 +660,15 @@ struct SequenceAttention : torch::autograd::Function<SequenceAttention> {
     static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
         return with_python_errors([&]() -> variable_list {
             const variable_list s = ctx->get_saved_variables();
+            const auto dense = [&](int i) { return s[i].defined() ? OptTensor(aligned(s[i])) : OptTensor(); };
+            at::Tensor k = saved_rows(s[1]), v = saved_rows(s[2]);
+            if (row_stride(k) != row_stride(v)) {
+                k = aligned(k);  // one stride for both
+                v = aligned(v);
+            }
             Grads d;
-            const int rc = run_sequence_backward(d, s[0], s[1], s[2], s[3], s[4], aligned(grads[0]), ctx->saved_data["heads"].toInt(),
-                                                 ctx->saved_data["scale"].toDouble(), opt(s[5]), opt(s[6]), opt(s[7]), opt(s[8]), opt(s[9]),
+            const int rc = run_sequence_backward(d, saved_rows(s[0]), k, v, saved_rows(s[3]), aligned(s[4]), aligned(grads[0]), ctx->saved_data["heads"].toInt(),
+                                                 ctx->saved_data["scale"].toDouble(), dense(5), dense(6), dense(7), dense(8), dense(9),
                                                  ctx->saved_data["causal"].toBool(), s[5].defined() && ctx->needs_input_grad(3), std::nullopt, std::nullopt,
                                                  std::nullopt, std::nullopt, std::nullopt);
             if (rc != FWA_OK) raise_status(rc, "fwa_sequence_backward");
