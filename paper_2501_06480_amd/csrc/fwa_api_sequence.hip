@@ -51,6 +51,32 @@ int check_terms(fwa::SeqArgs& a, const float* table, const int32_t* buckets, int
     return FWA_OK;
 }
 
+// The tensors of a call as the bytes that they touch; no output may share one with an input or with another output.
+struct Touched {
+    Span ins[16], outs[8];
+    int ni = 0, no = 0;
+    void in(const Span& s) { ins[ni++] = s; }
+    void out(const Span& s) { outs[no++] = s; }
+    // what all sequence calls read besides their tensors
+    void terms(const fwa::SeqArgs& a) {
+        if (a.table) {
+            in(flat(a.table, (uint64_t)a.H * a.nb * 4));
+            in(flat(a.buckets, (2 * (uint64_t)a.far + 1) * 4));
+        }
+        for (const int32_t* p : {a.q_len, a.k_len, a.q_start})
+            if (p && a.N > 0) in(flat(p, (uint64_t)a.N * 4));
+    }
+    bool shared() const {
+        for (int x = 0; x < no; ++x) {
+            for (int y = 0; y < ni; ++y)
+                if (overlaps(outs[x], ins[y])) return true;
+            for (int y = x + 1; y < no; ++y)
+                if (overlaps(outs[x], outs[y])) return true;
+        }
+        return false;
+    }
+};
+
 }  // namespace
 
 extern "C" {
@@ -114,16 +140,16 @@ int fwa_sequence_forward(const void* q, const void* k, const void* v, void* o, f
     if (N == 0 || Lq == 0) return FWA_OK;
     if (!q || !o || (Lk > 0 && (!k || !v))) return FWA_ERR_NULL;
     if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(o) || misaligned(stats) || misaligned(workspace)) return FWA_ERR_ALIGN;
-    {
-        const Span so = span_of(o, N, Lq, heads * d, ld_o, dtype), sq = span_of(q, N, Lq, heads * d, ld_q, dtype);
-        const Span ss = flat(stats, (uint64_t)N * heads * Lq * 8);
-        if (overlaps(so, sq) || (stats && (overlaps(ss, so) || overlaps(ss, sq)))) return FWA_ERR_ALIAS;
-        for (const void* in : {k, v})
-            if (Lk > 0) {
-                const Span si = span_of(in, N, Lk, kv_heads * d, ld_kv, dtype);
-                if (overlaps(so, si) || (stats && overlaps(ss, si))) return FWA_ERR_ALIAS;
-            }
+    Touched touched;
+    touched.terms(a);
+    touched.in(span_of(q, N, Lq, heads * d, ld_q, dtype));
+    if (Lk > 0) {
+        touched.in(span_of(k, N, Lk, kv_heads * d, ld_kv, dtype));
+        touched.in(span_of(v, N, Lk, kv_heads * d, ld_kv, dtype));
     }
+    touched.out(span_of(o, N, Lq, heads * d, ld_o, dtype));
+    if (stats) touched.out(flat(stats, (uint64_t)N * heads * Lq * 8));
+    if (touched.shared()) return FWA_ERR_ALIAS;
     const size_t need = fwa::seq_forward_workspace(a);
     if (need > 0 && (!workspace || workspace_bytes < need)) return FWA_ERR_WORKSPACE;
     a.q = q; a.k = k; a.v = v; a.o = o; a.stats = stats;
@@ -155,6 +181,10 @@ int fwa_sequence_backward(const void* q, const void* k, const void* v, const voi
     if (rc != FWA_OK) return rc;
     if (dtable && !table) return FWA_ERR_NULL;
     if (misaligned(dtable)) return FWA_ERR_ALIGN;
+    Touched touched;
+    touched.terms(a);
+    if (dtable) touched.out(flat(dtable, (uint64_t)heads * columns * 4));
+    if (touched.shared()) return FWA_ERR_ALIAS;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (N == 0)  // no pairs: dtable is still overwritten
         return !dtable || fwa::launch_zero_f32(dtable, (size_t)heads * columns, st) == hipSuccess ? FWA_OK : FWA_ERR_LAUNCH;
@@ -163,33 +193,20 @@ int fwa_sequence_backward(const void* q, const void* k, const void* v, const voi
     if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(o) || misaligned(d_o) || misaligned(stats) || misaligned(dq) || misaligned(dk) ||
         misaligned(dv) || misaligned(workspace))
         return FWA_ERR_ALIGN;
-    {
-        Span ins[6], outs[4];
-        int ni = 0, no = 0;
-        if (Lq > 0) {
-            ins[ni++] = span_of(q, N, Lq, C, ld_q, dtype);
-            ins[ni++] = span_of(o, N, Lq, C, ld_o, dtype);
-            ins[ni++] = span_of(d_o, N, Lq, C, ld_do, dtype);
-            ins[ni++] = flat(stats, (uint64_t)N * heads * Lq * 8);
-            outs[no++] = span_of(dq, N, Lq, C, ld_dq, dtype);
-        }
-        if (Lk > 0) {
-            ins[ni++] = span_of(k, N, Lk, CK, ld_kv, dtype);
-            ins[ni++] = span_of(v, N, Lk, CK, ld_kv, dtype);
-            outs[no++] = span_of(dk, N, Lk, CK, ld_dkv, dtype);
-            outs[no++] = span_of(dv, N, Lk, CK, ld_dkv, dtype);
-        }
-        if (dtable) {
-            outs[no++] = flat(dtable, (uint64_t)heads * columns * 4);
-            if (overlaps(outs[no - 1], flat(table, (uint64_t)heads * columns * 4))) return FWA_ERR_ALIAS;
-        }
-        for (int x = 0; x < no; ++x) {
-            for (int y = 0; y < ni; ++y)
-                if (overlaps(outs[x], ins[y])) return FWA_ERR_ALIAS;
-            for (int y = x + 1; y < no; ++y)
-                if (overlaps(outs[x], outs[y])) return FWA_ERR_ALIAS;
-        }
+    if (Lq > 0) {
+        touched.in(span_of(q, N, Lq, C, ld_q, dtype));
+        touched.in(span_of(o, N, Lq, C, ld_o, dtype));
+        touched.in(span_of(d_o, N, Lq, C, ld_do, dtype));
+        touched.in(flat(stats, (uint64_t)N * heads * Lq * 8));
+        touched.out(span_of(dq, N, Lq, C, ld_dq, dtype));
     }
+    if (Lk > 0) {
+        touched.in(span_of(k, N, Lk, CK, ld_kv, dtype));
+        touched.in(span_of(v, N, Lk, CK, ld_kv, dtype));
+        touched.out(span_of(dk, N, Lk, CK, ld_dkv, dtype));
+        touched.out(span_of(dv, N, Lk, CK, ld_dkv, dtype));
+    }
+    if (touched.shared()) return FWA_ERR_ALIAS;
     const size_t need = fwa::seq_backward_workspace(a, dtable != nullptr);
     if (need > 0 && (!workspace || workspace_bytes < need)) return FWA_ERR_WORKSPACE;
     a.q = q; a.k = k; a.v = v; a.o = const_cast<void*>(o); a.d_o = d_o; a.stats = const_cast<float*>(stats);
