@@ -171,8 +171,9 @@ int fwa_sequence_backward(const void* q, const void* k, const void* v, const voi
                           const int32_t* q_lengths, const int32_t* k_lengths, const int32_t* q_start, int causal, int dtype, void* workspace,
                           size_t workspace_bytes, void* stream) {
     fwa::SeqArgs a = {};
-    const int C = heads * d, CK = kv_heads * d;
     int rc = check_sequence(a, N, Lq, Lk, heads, kv_heads, d, dtype);
+    if (rc != FWA_OK) return rc;
+    const int C = heads * d, CK = kv_heads * d;
     for (const int64_t ld : {ld_q, ld_o, ld_do, ld_dq})
         if (rc == FWA_OK) rc = check_row_stride(ld, C, dtype);
     for (const int64_t ld : {ld_kv, ld_dkv})
