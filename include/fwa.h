@@ -244,7 +244,7 @@ size_t fwa_bucket_scatter_workspace_bytes(int heads, int columns, int far, int L
  *   q, o      : [N, Lq, heads * d], rows ld_q resp. ld_o elements apart (sequence n begins at row n * Lq)
  *   k, v      : [N, Lk, kv_heads * d], rows ld_kv elements apart; kv_heads divides heads
  *   d         : 32, 64 or 128; dtype FWA_F32, FWA_BF16 or FWA_F16.  Lq and Lk from 0 to 2^24, heads <= 2^15, heads * Lq <= 2^28,
- *               row strides <= 2^20 elements.
+ *               row strides <= 2^20 elements, N * heads * (max(Lq, Lk) / 128 + 1) up to about 15 million (a launch's workgroups).
  *   table, buckets, columns, far : the bias B by buckets, formed inside the kernels, as in fwa_bucket_gather (with the
  *               q_start below for each sequence); table NULL: none, the other three are ignored
  *   q_lengths : NULL, or [N] int32: queries from q_lengths[n] on are padding; their rows of o are zero

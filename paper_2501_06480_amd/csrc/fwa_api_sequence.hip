@@ -150,6 +150,7 @@ int fwa_sequence_forward(const void* q, const void* k, const void* v, void* o, f
     touched.out(span_of(o, N, Lq, heads * d, ld_o, dtype));
     if (stats) touched.out(flat(stats, (uint64_t)N * heads * Lq * 8));
     if (touched.shared()) return FWA_ERR_ALIAS;
+    if (!fwa::seq_forward_fits(a)) return FWA_ERR_UNSUPPORTED;
     const size_t need = fwa::seq_forward_workspace(a);
     if (need > 0 && (!workspace || workspace_bytes < need)) return FWA_ERR_WORKSPACE;
     a.q = q; a.k = k; a.v = v; a.o = o; a.stats = stats;
@@ -208,6 +209,7 @@ int fwa_sequence_backward(const void* q, const void* k, const void* v, const voi
         touched.out(span_of(dv, N, Lk, CK, ld_dkv, dtype));
     }
     if (touched.shared()) return FWA_ERR_ALIAS;
+    if (!fwa::seq_backward_fits(a)) return FWA_ERR_UNSUPPORTED;
     const size_t need = fwa::seq_backward_workspace(a, dtable != nullptr);
     if (need > 0 && (!workspace || workspace_bytes < need)) return FWA_ERR_WORKSPACE;
     a.q = q; a.k = k; a.v = v; a.o = const_cast<void*>(o); a.d_o = d_o; a.stats = const_cast<float*>(stats);

@@ -144,8 +144,10 @@ constexpr int seq_forward_keys(int row_bytes, bool keys) { return row_bytes >= 5
 constexpr int seq_backward_rows(int row_bytes) { return row_bytes >= 256 ? 32 : 64; }
 
 hipError_t launch_sequence_forward(const SeqArgs& a, void* workspace, hipStream_t s);
+bool seq_forward_fits(const SeqArgs& a);  // a launch holds the call's workgroups
 size_t seq_forward_workspace(const SeqArgs& a);
 hipError_t launch_sequence_backward(const SeqArgs& a, void* workspace, hipStream_t s);
+bool seq_backward_fits(const SeqArgs& a);
 size_t seq_backward_workspace(const SeqArgs& a, bool want_dtable);
 hipError_t launch_bucket_gather(const float* table, const int32_t* buckets, void* bias, int heads, int nb, int far, int Lq, int Lk, int q_start, bool bf16,
                                 hipStream_t s);

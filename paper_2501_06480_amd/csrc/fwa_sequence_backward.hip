@@ -1155,6 +1155,11 @@ size_t table_bytes(const SeqArgs& a, const BackPlan& p) {
 
 }  // namespace
 
+bool seq_backward_fits(const SeqArgs& a) {
+    BackPlan p;
+    return back_plan(a, p);
+}
+
 // workspace: delta, the parts of dK and dV, the sums of dS by distance
 size_t seq_backward_workspace(const SeqArgs& a, bool want_dtable) {
     BackPlan p, other;

@@ -402,6 +402,11 @@ bool seq_forward_plan(const SeqArgs& a, SeqPlan& p) {
     return true;
 }
 
+bool seq_forward_fits(const SeqArgs& a) {
+    SeqPlan p;
+    return seq_forward_plan(a, p);
+}
+
 size_t seq_forward_workspace(const SeqArgs& a) {
     SeqPlan p;
     if (!seq_forward_plan(a, p) || p.splits == 1) return 0;
