@@ -203,11 +203,12 @@ bool few_lines(int far, long long count) { return count * (2LL * far + 1) <= 163
 
 hipError_t launch_bucket_gather(const float* table, const int32_t* buckets, void* bias, int heads, int nb, int far, int Lq, int Lk, int q_start, bool bf16,
                                 hipStream_t s) {
-    const int rows = Lk >= kGatherElements ? 1 : (kGatherElements / Lk < Lq ? kGatherElements / Lk : Lq), parts = (Lq + rows - 1) / rows;
+    int rows = Lk >= kGatherElements ? 1 : (kGatherElements / Lk < Lq ? kGatherElements / Lk : Lq);
+    while ((long long)heads * ((Lq + rows - 1) / rows) > 0xffffffLL) rows *= 2;  // a launch has fewer than 2^32 threads
+    const int parts = (Lq + rows - 1) / rows;
     const long long met = (long long)Lk + rows - 1, all = 2LL * far + 1;
     const size_t lds = (size_t)(met < all ? met : all) * sizeof(float);
     const long long grid = (long long)heads * parts;
-    if (grid > 0xffffffLL) return hipErrorInvalidValue;
     const FastDiv by_Lk = make_fastdiv((uint32_t)Lk), by_parts = make_fastdiv((uint32_t)parts);
     const void* const fn = bf16 ? reinterpret_cast<const void*>(&bucket_gather_kernel<true>) : reinterpret_cast<const void*>(&bucket_gather_kernel<false>);
     const hipError_t e = allow_lds(fn, lds);
