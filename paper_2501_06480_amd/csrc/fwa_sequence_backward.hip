@@ -41,7 +41,7 @@ constexpr float seq_lift() { return __is_same(T, SeqF16) ? 6.f : 0.f; }
 constexpr int kFewKeys = 128;
 
 // Whether no query of a sequence sees more than one key: its weight is one and stays so, and all but dV is exactly zero, which products and their
-// differences need not be to the last bit.
+// differences need not be to the last bit (and in half data need not be finite).
 __device__ __forceinline__ bool seq_lone(bool causal, int start, int qlen, int klen) {
     return klen <= 1 || (causal && start + qlen <= 1);
 }
@@ -119,7 +119,8 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
         dead = seq_dead(stat);
         ref = dead ? 0.f : stat[0];
         if (HALF && !dead) log_sum = stat[1] - seq_lift<T>();
-        rl = dead || seq_lone(a.causal, start, qlen, klen) ? 0.f : __builtin_amdgcn_exp2f(HALF ? -seq_lift<T>() : -stat[1]);
+        rl = dead ? 0.f : __builtin_amdgcn_exp2f(HALF ? -seq_lift<T>() : -stat[1]);
+        const bool lone = seq_lone(a.causal, start, qlen, klen);  // dP and delta from a d_o of zero
         const size_t at_row = (size_t)n * a.Lq + i, channel = (size_t)head * D;
         const char* const qp = static_cast<const char*>(a.q) + (at_row * a.ldq + channel) * E + 16u * hi;
         const char* const gp = static_cast<const char*>(a.d_o) + (at_row * a.ldg + channel) * E + 16u * hi;
@@ -128,7 +129,7 @@ __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan pl
 #pragma unroll
         for (int s = 0; s < NC; ++s) {
             qf[s] = *reinterpret_cast<const u32x4*>(qp + 32 * s);
-            gf[s] = *reinterpret_cast<const u32x4*>(gp + 32 * s);
+            if (!lone) gf[s] = *reinterpret_cast<const u32x4*>(gp + 32 * s);
             const u32x4 of = *reinterpret_cast<const u32x4*>(op + 32 * s);
             if constexpr (__is_same(T, SeqF32)) {
                 const f32x4 x = __builtin_bit_cast(f32x4, of), y = __builtin_bit_cast(f32x4, gf[s]);
@@ -954,7 +955,7 @@ __global__ void __launch_bounds__(64 * W, D * SeqSize<T>::value == 256 ? 2 : 1) 
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) dk[b][r] = dk[b][r] != dk[b][r] ? dk[b][r] : 0.f;
+            for (int r = 0; r < 16; ++r) dk[b][r] = dv[b][r] != dv[b][r] ? dv[b][r] : 0.f;  // NaN where P is
     }
     if (j >= klen) {  // padding has nothing of a row of NaN either
 #pragma unroll
