@@ -259,7 +259,8 @@ size_t fwa_bucket_scatter_workspace_bytes(int heads, int columns, int far, int L
  *               many keys are shared out over the keys and joined), 16-byte aligned
  * A row that sees no key, or whose scores are all -inf, gives zeros.  Table values of -inf shut pairs out; the lowest finite value
  * counts as such (a row of nothing else is uniform).  Inside the lengths q, k, v and d_o are expected to be finite: an
- * infinity or NaN in a key's row may reach queries that causality keeps from seeing it.
+ * infinity or NaN in a key's row may reach queries that causality keeps from seeing it, and one in a query's row the gradients of
+ * keys that it does not see.  Neither reaches padding or heads that do not share the keys.  The statistics of a row of NaN alone are (-inf, NaN).
  * Arithmetic: fp32 data in fp32 throughout; 16-bit data are multiplied as they are, sums, softmax and statistics are fp32, P and
  * (backward) dS are rounded once to the data's type in front of the product they enter.
  * Lengths, starts, table and buckets need 4-byte alignment only.
@@ -280,7 +281,8 @@ size_t fwa_sequence_forward_workspace_bytes(int64_t N, int Lq, int Lk, int heads
  *   dtable     : NULL, or out [heads, columns] fp32: the gradient of the table, overwritten; its terms are not rounded to the
  *                data's type
  *   workspace  : at least fwa_sequence_backward_workspace_bytes(...) bytes, 16-byte aligned
- * Bit-reproducible from run to run.  With half data dS beyond 1023 overflows.
+ * Bit-reproducible from run to run.  With half data dS beyond 1023 overflows.  dq of 16-bit data in rows of more than 128 keys
+ * takes over half a step of the data's type of sum |d_o o|, from o as it is stored, in delta.
  */
 int fwa_sequence_backward(const void* q, const void* k, const void* v, const void* o, const void* d_o, const float* stats,
                           void* dq, void* dk, void* dv, float* dtable,

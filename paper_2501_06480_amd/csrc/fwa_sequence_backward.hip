@@ -36,8 +36,8 @@ template <class T>
 constexpr float seq_lift() { return __is_same(T, SeqF16) ? 6.f : 0.f; }
 // Rows that see few keys: one of these may have nearly all the weight, dP - delta cancels, and the rounding of o would show (bf16, rows of up to 128 keys of
 // width 128: elements of dQ up to 1.4e-2 off, now within half a step of each dS).  There a walk in front of the other forms delta from the same products as
-// dP.  At every width and in both forms up to this many keys, which the first block of a causal call has; waves that share out the keys
-// and have two tiles each are as quick about more.
+// dP (70 sequences of 128 tokens, 8 heads of 128, bf16: whole backward 74 us with it, 68 without).  At every width and in both forms up to this many
+// keys, which the first block of a causal call has; waves that share out the keys take it up to two tiles each, where there are more of them.
 constexpr int kFewKeys = 128;
 
 // Whether no query of a sequence sees more than one key: its weight is one and stays so, and all but dV is exactly zero, which products and their
@@ -57,7 +57,7 @@ __device__ __forceinline__ float plain_sum(float a, float b) {
 // The row's sum is divided out of dQ at the end, but for half data, where it is in the exponent together with the lift: dS times a sum of thousands leaves
 // that type's range.
 // Bound by vector instructions between the three products and by the latency of a tile (4 ragged sequences of up to 2048 tokens, 12 heads of 64, bf16:
-// 111 us, vector units 43 per cent busy, matrix units 25).
+// 106 us, vector units 43 per cent busy, matrix units 25).
 template <class T, int D, int W, int KT, bool TABLE, bool KEYS>
 __global__ void __launch_bounds__(64 * W) seq_rows_kernel(SeqArgs a, BackPlan plan) {
     constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, KS = KT / 32;
@@ -650,8 +650,8 @@ __global__ void __launch_bounds__(256) seq_lines_kernel(SeqArgs a, BackPlan plan
 constexpr bool seq_keys_v_in_lds(int row_bytes) { return row_bytes == 256; }
 
 // The keys kernel is bound by its reads of LDS and by the latency of a tile: four products a tile, four of their operands through LDS, on two waves a SIMD
-// (4 ragged sequences of up to 2048 tokens, 12 heads of 64, bf16: 143 us, 370 TFLOP/s, LDS 30 per cent busy, matrix units 25; 2 x 1023 causal
-// tokens, 16 heads of 128 on 4: 45 us, of which 64 MB of parts).
+// (4 ragged sequences of up to 2048 tokens, 12 heads of 64, bf16: 138 us, LDS 30 per cent busy, matrix units 26; 2 x 1023 causal
+// tokens, 16 heads of 128 on 4: 44 us, of which 64 MB of parts).
 
 // Tiles of queries that see a key of the block from j0 on: each of q0 .. q0 + each - 1, of every head that shares the keys.
 __device__ __forceinline__ void seq_key_tiles(bool causal, int qlen, int klen, int start, int j0, int size, int& q0, int& each) {

@@ -24,9 +24,9 @@ constexpr float kSlack = 6.f;
 // in buffers of their own without a barrier, and join what they have at the end: W times the parallel work where rows are few, for W
 // times the loads of K and V.
 // Rows: bound by the latency of a tile, its reads of LDS and the softmax between the two products, on two or three waves a SIMD; the matrix units
-// are busy 14 to 29 per cent of the time (4 ragged sequences of up to 2048 tokens, 16 heads of 64, bf16: 72 us, 630 TFLOP/s;
-// 4001 causal tokens, 16 heads of 128, half: 107 us, 610).  Tiles of 32 keys, more buffers, scores a tile ahead and workgroups of 64 rows were slower.
-// Keys: bound by the reads of the cache (16 sequences of up to 8192 keys, 8 heads of 128: 410 MB in 87 us, 4.7 TB/s) or, for short
+// are busy 14 to 29 per cent of the time (4 ragged sequences of up to 2048 tokens, 16 heads of 64, bf16: 71 us, 640 TFLOP/s;
+// 4001 causal tokens, 16 heads of 128, half: 109 us in a kernel trace, 97 and 680 TFLOP/s in calls one behind the other).  Tiles of 32 keys, more buffers, scores a tile ahead and workgroups of 64 rows were slower.
+// Keys: bound by the reads of the cache (16 sequences of up to 8192 keys, 8 heads of 128: 410 MB in 86 us, 4.8 TB/s) or, for short
 // ones, by the launch and the latency of a tile or two (10 us).
 template <class T, int D, int W, int KT, bool KEYS>
 __global__ void __launch_bounds__(64 * W, seq_forward_waves(D * SeqSize<T>::value, KEYS)) seq_forward_kernel(SeqArgs a, SeqPlan plan) {
