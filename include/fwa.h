@@ -294,6 +294,73 @@ int fwa_sequence_backward(const void* q, const void* k, const void* v, const voi
 size_t fwa_sequence_backward_workspace_bytes(int64_t N, int Lq, int Lk, int heads, int kv_heads, int d, int far, int dtype,
                                              int want_dtable);
 
+/*
+ * Rotary positions with several axes (time, height and width of a video; row and column of an image; one for text).  Pair p of every head's
+ * channels is turned by the angle positions[r][axis_of[p]] * frequencies[p]:
+ *   (a, b) -> (a cos - b sin, b cos + a sin),  channels p and p + pairs, or (interleaved nonzero) 2 p and 2 p + 1
+ * Channels from 2 pairs on stay as they are.
+ *   x           : in,  [rows, heads * d], rows ld_x elements apart
+ *   y           : out, like x, rows ld_y apart; may be x itself (the same address and stride), else no byte of it
+ *   positions   : [position_rows, axes] int32; row r of x has row r mod position_rows of them (position_rows = L for all sequences of [N, L])
+ *   frequencies : [pairs] fp32, radians a position
+ *   axis_of     : [pairs] int32, or NULL: all pairs the first axis.  A pair with an axis outside [0, axes) is not turned.
+ *   inverse     : nonzero: by the negative angle, which is the inverse, and the gradient of x from that of y
+ * d from 1 to 512, 0 <= pairs <= d / 2, axes <= 16, dtype FWA_F32, FWA_BF16 or FWA_F16, rows * heads * d / 2 below 2e9.  Angles are formed in 64 bits and
+ * reduced to a turn there, so far positions lose nothing (2^20 of frequency 1: 1e-7 of the result, as near ones); the rotation is fp32, rounded once.
+ * positions, frequencies and axis_of need 4-byte alignment only.
+ */
+int fwa_rotary(const void* x, void* y, int64_t rows, int heads, int d, int64_t ld_x, int64_t ld_y, const int32_t* positions,
+               int64_t position_rows, int axes, const float* frequencies, const int32_t* axis_of, int pairs, int interleaved, int inverse,
+               int dtype, void* stream);
+
+/*
+ * A paged cache: keys and values of N sequences in pages of page_size rows.  The token at place t of sequence n lies in row t % page_size of
+ * page page_table[n][t / page_size].
+ *   k_pages, v_pages : [pages, page_size, kv_heads, d]; row r of page p of head h begins p * page_stride + r * token_stride + h * head_stride
+ *                      elements behind the base, so pages with a head's rows together ([pages, kv_heads, page_size, d]) are meant as well.  The strides, one set
+ *                      for both, are multiples of 16 bytes (FWA_ERR_ALIGN), reach no element twice (FWA_ERR_SHAPE), token_stride <= 2^20
+ *                      elements.  Keys and values may interleave in one buffer.
+ *   page_size        : a multiple of 16, at most 65536; width * page_size <= 2^29; the whole cache of any size
+ *   page_table       : [N, width] int32.  An entry outside [0, pages) is no page: nothing is stored there and its keys are not seen.
+ *   offsets          : [N + 1] int32, not falling: the new tokens of sequence n are rows offsets[n] .. offsets[n + 1] - 1 of the packed tensors
+ *                      [rows, heads * d].  Rows in front of offsets[0] and from offsets[N] on are left as they were.
+ *   lengths          : [N] int32: tokens of sequence n in front of the new ones; new token i has place lengths[n] + i.  Below 0 counts as 0.
+ * Both calls of a step take the same tables.  d is 32, 64 or 128, dtype FWA_F32, FWA_BF16 or FWA_F16 for all tensors, rows <= 2^24,
+ * N <= 2^20, rows * (heads + 2 kv_heads) <= 2^28.  The tables need 4-byte alignment only.
+ *
+ * fwa_page_append stores the new tokens' keys, rotated, and values in their places, and rotates their queries besides.
+ *   k, v       : [rows, kv_heads * d], rows ld_k resp. ld_v apart
+ *   positions, axes, frequencies, axis_of, pairs, interleaved : the rotation of fwa_rotary, positions [rows, axes]; NULL: one axis, the
+ *                token's place in its sequence.  pairs 0: none.
+ *   q, q_out   : NULL, or [rows, heads * d]: the rotated queries; q_out may be q itself.  heads and the strides are ignored without them.
+ * Tokens beyond width * page_size are not stored.  Two tokens of a call must not have one row of a page.
+ */
+int fwa_page_append(const void* k, const void* v, void* k_pages, void* v_pages, int64_t rows, int64_t N, int kv_heads, int d, int64_t ld_k,
+                    int64_t ld_v, int64_t pages, int page_size, int64_t page_stride, int64_t token_stride, int64_t head_stride,
+                    const int32_t* page_table, int width, const int32_t* offsets, const int32_t* lengths, const int32_t* positions,
+                    int axes, const float* frequencies, const int32_t* axis_of, int pairs, int interleaved, const void* q, void* q_out,
+                    int heads, int64_t ld_q, int64_t ld_q_out, int dtype, void* stream);
+
+/*
+ * Attention of the new tokens over the cache that already holds them: token i of sequence n sees the keys at places up to lengths[n] + i
+ * (causal nonzero) or all lengths[n] + new ones, of those within width * page_size whose page exists.
+ *   q, o      : [rows, heads * d], rows ld_q resp. ld_o apart; kv_heads divides heads
+ *   most_new  : no sequence has more new tokens; what goes beyond is not computed and its rows left as they were.  The smaller this is, the
+ *               better the call can be laid out (1 for single tokens); rows is always enough.
+ *   stats     : NULL, or out [rows, heads, 2] fp32, the row statistics as in fwa_sequence_forward
+ *   workspace : device scratch of at least fwa_page_forward_workspace_bytes(...) bytes, 16-byte aligned.  It goes by the arguments on the host, the
+ *               lengths and offsets are read on the device alone: a captured call may be replayed with others.
+ * A row that sees no key gives zeros.  Arithmetic as in fwa_sequence_forward; infinities and NaN in rows of the cache from lengths[n] + new
+ * on are never read, those in a key's row that causality shuts out may reach the rows that do not see it.
+ * Bit-reproducible from run to run.
+ */
+int fwa_page_forward(const void* q, const void* k_pages, const void* v_pages, void* o, float* stats, int64_t rows, int64_t N, int heads,
+                     int kv_heads, int d, float scale, int64_t ld_q, int64_t ld_o, int64_t pages, int page_size, int64_t page_stride,
+                     int64_t token_stride, int64_t head_stride, const int32_t* page_table, int width, const int32_t* offsets,
+                     const int32_t* lengths, int most_new, int causal, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+size_t fwa_page_forward_workspace_bytes(int64_t rows, int64_t N, int heads, int kv_heads, int d, int page_size, int width, int most_new,
+                                        int dtype);
+
 /* Static, NUL-terminated description of an error code. */
 const char* fwa_status_string(int code);
 

@@ -13,4 +13,5 @@ from .binding import (  # noqa: F401
     fwa_bias_scatter, fwa_status_string, library_path, load_library,
     fwa_bucket_gather, fwa_bucket_scatter, fwa_bucket_scatter_workspace_bytes, fwa_sequence_forward, fwa_sequence_forward_workspace_bytes,
     fwa_sequence_backward, fwa_sequence_backward_workspace_bytes, log_buckets,
+    fwa_rotary, rotary_frequencies, fwa_page_append, fwa_page_forward, fwa_page_forward_workspace_bytes,
 )

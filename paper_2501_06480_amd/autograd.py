@@ -10,7 +10,8 @@ Both take the mask either as a dense fp32 ``mask`` [nW, L, L] or as int32 region
 
 ``bucket_bias(table, buckets, Lq, Lk)`` is the dense bias of 1-D distances by buckets, differentiable in the table: the
 ``bias`` of a window attention of such a sequence.  ``sequence_attention(q, k, v, heads, scale, table, buckets, ...)`` is
-attention of whole sequences, which forms that bias inside its kernels.  As with any node of torch: a backward pass that is to be
+attention of whole sequences, which forms that bias inside its kernels.  ``rotary(x, heads, positions, frequencies, ...)`` turns queries or keys
+by their positions, differentiable in x.  As with any node of torch: a backward pass that is to be
 captured into a graph runs with leaves whose earlier eager graphs are gone.
 """
 from __future__ import annotations
@@ -164,3 +165,23 @@ def sequence_attention(q, k, v, heads: int, scale: float, table=None, buckets=No
     if _native_node(q, k, v, table, buckets, q_lengths, k_lengths, q_start):
         return binding._native().sequence_attention(q, k, v, int(heads), float(scale), table, buckets, q_lengths, k_lengths, q_start, bool(causal))
     return _SequenceAttention.apply(q, k, v, table, buckets, q_lengths, k_lengths, q_start, int(heads), float(scale), bool(causal))
+
+
+class _Rotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, positions, frequencies, axis_of, heads, interleaved, inverse):
+        ctx.save_for_backward(positions, frequencies, axis_of)
+        ctx.heads, ctx.interleaved, ctx.inverse = heads, interleaved, inverse
+        return binding.fwa_rotary(x, heads, positions, frequencies, axis_of, interleaved, inverse)
+
+    @staticmethod
+    def backward(ctx, dy):
+        positions, frequencies, axis_of = (None if t is None else t.contiguous() for t in ctx.saved_tensors)
+        return (binding.fwa_rotary(_aligned(dy), ctx.heads, positions, frequencies, axis_of, ctx.interleaved, not ctx.inverse),) + (None,) * 6
+
+
+def rotary(x, heads: int, positions, frequencies, axis_of=None, interleaved: bool = False, inverse: bool = False):
+    """Rotary positions (``binding.fwa_rotary``), differentiable in x: its gradient is the rotation back."""
+    if _native_node(x, positions, frequencies, axis_of):
+        return binding._native().rotary_node(x, int(heads), positions, frequencies, axis_of, bool(interleaved), bool(inverse))
+    return _Rotary.apply(x, positions, frequencies, axis_of, int(heads), bool(interleaved), bool(inverse))

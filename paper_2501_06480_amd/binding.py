@@ -36,7 +36,8 @@ EXPORTS = ("fwa_forward", "fwa_forward_strided", "fwa_forward_labels", "fwa_back
            "fwa_backward_labels", "fwa_backward_noalloc",
            "fwa_backward_workspace_bytes", "fwa_bias_gather", "fwa_bias_scatter", "fwa_status_string",
            "fwa_bucket_gather", "fwa_bucket_scatter", "fwa_bucket_scatter_workspace_bytes", "fwa_sequence_forward",
-           "fwa_sequence_forward_workspace_bytes", "fwa_sequence_backward", "fwa_sequence_backward_workspace_bytes")
+           "fwa_sequence_forward_workspace_bytes", "fwa_sequence_backward", "fwa_sequence_backward_workspace_bytes",
+           "fwa_rotary", "fwa_page_append", "fwa_page_forward", "fwa_page_forward_workspace_bytes")
 
 
 class FwaError(RuntimeError):
@@ -104,6 +105,16 @@ def load_library():
                                           vp, vp, ci, ci, vp, vp, vp, ci, ci, vp, sz, vp]
     lib.fwa_sequence_backward_workspace_bytes.restype = sz
     lib.fwa_sequence_backward_workspace_bytes.argtypes = [i64, ci, ci, ci, ci, ci, ci, ci, ci]
+    lib.fwa_rotary.restype = ci
+    lib.fwa_rotary.argtypes = [vp, vp, i64, ci, ci, i64, i64, vp, i64, ci, vp, vp, ci, ci, ci, ci, vp]
+    lib.fwa_page_append.restype = ci
+    lib.fwa_page_append.argtypes = [vp, vp, vp, vp, i64, i64, ci, ci, i64, i64, i64, ci, i64, i64, i64, vp, ci, vp, vp, vp, ci, vp, vp, ci, ci, vp, vp,
+                                    ci, i64, i64, ci, vp]
+    lib.fwa_page_forward.restype = ci
+    lib.fwa_page_forward.argtypes = [vp, vp, vp, vp, vp, i64, i64, ci, ci, ci, cf, i64, i64, i64, ci, i64, i64, i64, vp, ci, vp, vp, ci, ci, ci,
+                                     vp, sz, vp]
+    lib.fwa_page_forward_workspace_bytes.restype = sz
+    lib.fwa_page_forward_workspace_bytes.argtypes = [i64, i64, ci, ci, ci, ci, ci, ci, ci]
     lib.fwa_status_string.restype = ctypes.c_char_p
     lib.fwa_status_string.argtypes = [ci]
     _lib = lib
@@ -440,3 +451,76 @@ def fwa_sequence_backward(q, k, v, o, stats, d_o, heads: int, scale: float, tabl
 def fwa_sequence_backward_workspace_bytes(N: int, Lq: int, Lk: int, heads: int, kv_heads: int, d: int, far: int, dtype: int,
                                           want_dtable: bool) -> int:
     return int(load_library().fwa_sequence_backward_workspace_bytes(N, Lq, Lk, heads, kv_heads, d, far, dtype, int(bool(want_dtable))))
+
+
+def rotary_frequencies(sections, theta: float = 10000.0, joint: bool = False, device=None):
+    """(frequencies [pairs] fp32, axis_of [pairs] int32) for ``fwa_rotary``: `sections` has the number of pairs of each axis.  Each axis has a ladder
+    theta^(-i / n) of its own (images, video), or (`joint`) all share one over all pairs, cut into sections (text beside images)."""
+    sections = [int(n) for n in sections]
+    if not sections or min(sections) < 0 or not theta > 0:
+        raise ValueError("rotary_frequencies needs sections of no negative length and a positive theta")
+    pairs, f, axis = sum(sections), [], []
+    for a, n in enumerate(sections):
+        f += [theta ** (-(len(f) + i) / pairs if joint else -i / n) for i in range(n)]
+        axis += [a] * n
+    torch = _torch()
+    return torch.tensor(f, dtype=torch.float32, device=device), torch.tensor(axis, dtype=torch.int32, device=device)
+
+
+def fwa_rotary(x, heads: int, positions, frequencies, axis_of=None, interleaved: bool = False, inverse: bool = False, out=None, stream=None):
+    """Rotary positions: pair p of each head's channels of x ([N, L, heads * d] or packed [T, heads * d], rows of larger ones as well) turned by
+    positions[..., axis_of[p]] * frequencies[p] (``rotary_frequencies``).  `positions` is int32 [L, axes], the same for all N, or [N, L, axes]; [T, axes] of
+    packed rows.  A pair is channels p and p + pairs, or 2 p and 2 p + 1 (`interleaved`); channels behind the pairs stay.  `inverse` turns back,
+    which is also the gradient.  `out` may be x itself."""
+    args = (x, int(heads), positions, frequencies, axis_of, bool(interleaved), bool(inverse), out)
+    call = (_native_mod or _native()).rotary
+    if stream is None:
+        r = call(*args, None)
+    else:
+        with _alloc_on(stream, x.device):
+            r = call(*args, _stream_handle(stream, x.device))
+    if type(r) is int:
+        raise FwaError(r, "fwa_rotary")
+    return r
+
+
+def fwa_page_append(k, v, k_pages, v_pages, page_table, offsets, lengths, frequencies=None, positions=None, axis_of=None, interleaved: bool = False,
+                    q=None, q_out=None, stream=None):
+    """Store new tokens in a paged cache: k and v are packed [T, kv_heads * d] (rows of a fused projection as well), sequence n having rows
+    offsets[n] .. offsets[n + 1] - 1; k_pages and v_pages [pages, page_size, kv_heads, d] of any strides (one set) with contiguous channels; page_table int32
+    [N, width]; lengths int32 [N], the tokens in front of the new ones.  With `frequencies` keys are rotated (``fwa_rotary``) by `positions`
+    int32 [T, axes], or by their places in the sequences.  Returns the rotated queries if `q` [T, heads * d] is given (written to `q_out`, which may be q), else None;
+    rows of q outside the offsets are not written."""
+    args = (k, v, k_pages, v_pages, page_table, offsets, lengths, frequencies, positions, axis_of, bool(interleaved), q, q_out)
+    call = (_native_mod or _native()).page_append
+    if stream is None:
+        r = call(*args, None)
+    else:
+        with _alloc_on(stream, k.device):
+            r = call(*args, _stream_handle(stream, k.device))
+    if type(r) is int:
+        raise FwaError(r, "fwa_page_append")
+    return r
+
+
+def fwa_page_forward(q, k_pages, v_pages, page_table, offsets, lengths, heads: int, scale: float, most_new: Optional[int] = None, causal: bool = True,
+                     want_stats: bool = False, out=None, workspace=None, stream=None):
+    """Attention of packed new tokens q [T, heads * d] over a paged cache that holds their keys and values already (``fwa_page_append``, with the
+    same tables): token i of sequence n sees the keys at places up to lengths[n] + i, or (not `causal`) all of its sequence.  Prompts, chunks of prompts
+    and single tokens go in one call.  `most_new`: no sequence has more new tokens (default: T); tokens beyond are not computed.  Returns o, or (o, stats)
+    with the row statistics [T, heads, 2] as of ``fwa_sequence_forward``; rows outside the offsets are not written."""
+    args = (q, k_pages, v_pages, page_table, offsets, lengths, int(heads), float(scale), -1 if most_new is None else int(most_new), bool(causal),
+            bool(want_stats), out, workspace)
+    call = (_native_mod or _native()).page_forward
+    if stream is None:
+        r = call(*args, None)
+    else:
+        with _alloc_on(stream, q.device):
+            r = call(*args, _stream_handle(stream, q.device))
+    if type(r) is int:
+        raise FwaError(r, "fwa_page_forward")
+    return r
+
+
+def fwa_page_forward_workspace_bytes(rows: int, N: int, heads: int, kv_heads: int, d: int, page_size: int, width: int, most_new: int, dtype: int) -> int:
+    return int(load_library().fwa_page_forward_workspace_bytes(rows, N, heads, kv_heads, d, page_size, width, most_new, dtype))

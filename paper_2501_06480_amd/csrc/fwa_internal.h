@@ -157,4 +157,57 @@ size_t bucket_scatter_workspace(int heads, int far, int Lq);
 hipError_t launch_bucket_scatter(const float* dbias, const int32_t* buckets, float* dtable, int heads, int nb, int far, int Lq, int Lk, int q_start,
                                  float* workspace, hipStream_t s);
 
+// Rotary positions (fwa_rotary.hip).
+struct RotaryArgs {
+    const void* x;       // [rows, heads * d]
+    void* y;
+    long long rows;
+    int heads, d, dtype;
+    long long ldx, ldy;
+    const int32_t* positions;  // [period, axes]: row r has those of r mod period
+    long long period;
+    int axes;
+    const float* frequencies;  // [pairs], radians a position
+    const int32_t* axis_of;    // [pairs] or nullptr: all the first
+    int pairs;
+    int interleaved, inverse;
+};
+bool rotary_fits(long long rows, int heads, int d, int pairs, int dtype);
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t s);
+
+// A paged cache and the new tokens of a call, packed one sequence behind the other (fwa_page_*.hip).
+struct PageArgs {
+    void* k;             // row t % page_size of page p of head h: k + p page_stride + (t % page_size) token_stride + h head_stride elements
+    void* v;
+    long long pages, page_stride, token_stride, head_stride;
+    int page_size, width;
+    const int32_t* table;    // [N, width]
+    const int32_t* offsets;  // [N + 1]
+    const int32_t* lengths;  // [N]: tokens in the cache in front of the new ones
+    int N, rows;             // sequences, new tokens in all
+    int H, KV, D, dtype;
+    const void* q;           // [rows, H * D]
+    void* o;
+    long long ldq, ldo;
+    // attention
+    float* stats;        // [rows, H, 2] or nullptr
+    int most;            // new tokens of a sequence that count
+    int causal;
+    float scale;
+    // append: o is the rotated q
+    const void* new_k;   // [rows, KV * D]
+    const void* new_v;
+    long long ldk, ldv;
+    const int32_t* positions;  // [rows, axes], or nullptr: the place in the sequence
+    int axes;
+    const float* frequencies;
+    const int32_t* axis_of;
+    int pairs, interleaved;
+};
+bool page_append_fits(const PageArgs& a);
+hipError_t launch_page_append(const PageArgs& a, hipStream_t s);
+bool page_forward_fits(const PageArgs& a);
+size_t page_forward_workspace(const PageArgs& a);
+hipError_t launch_page_forward(const PageArgs& a, void* workspace, hipStream_t s);
+
 }  // namespace fwa

@@ -1,0 +1,150 @@
+// Append of new tokens to a paged cache: each token's keys, rotated by its position, and values go to their rows of the pages, and its queries are rotated
+// besides.  Tokens of several sequences stand one behind the other; a token's sequence is found from the offsets.
+#include "fwa_page.h"
+#include "fwa_rotary.h"
+
+namespace fwa {
+namespace {
+
+struct AppendPlan {
+    FastDiv by_each, by_units, by_pairs, by_page;
+    int heads, units, rows;  // heads of queries, keys and values together; units of a head; rows in LDS
+    int sample;              // one of so many offsets is looked at first
+    long long total;
+};
+
+// What a workgroup knows of a row that its units touch.
+struct AppendRow {
+    int place;        // in the sequence; the default position
+    uint32_t page;    // of the cache, ~0: nowhere
+};
+
+// Units as in the rotary kernel, a token's heads of queries, keys and values one behind the other, with their vectors on the way while the
+// places are looked up: sequence (a search in a sample of the offsets in LDS), length, page: three loads one behind the other.
+template <class T, int V>
+__global__ void __launch_bounds__(256) page_append_kernel(PageArgs a, AppendPlan plan) {
+    constexpr int E = SeqSize<T>::value, U = kRotaryUnits / 256;
+    extern __shared__ __attribute__((aligned(16))) f32x2 turns[];
+    __shared__ int samples[256];
+    AppendRow* const known = reinterpret_cast<AppendRow*>(turns + (size_t)plan.rows * a.pairs);
+    const uint32_t u0 = blockIdx.x * (uint32_t)kRotaryUnits, end = plan.total - u0 < kRotaryUnits ? (uint32_t)plan.total : u0 + kRotaryUnits;
+    const uint32_t row0 = fastdiv(u0, plan.by_each), rows = fastdiv(end - 1u, plan.by_each) - row0 + 1u;
+    {
+        const long long n = (long long)threadIdx.x * plan.sample;
+        samples[threadIdx.x] = n < a.N ? a.offsets[n] : 0x7fffffff;
+    }
+    RotaryVector<T, V> x[U], y[U];
+    RotaryUnit at[U];
+    uint32_t row[U], head[U], unit[U];
+    bool on[U], turned[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const uint32_t u = u0 + 256u * i + threadIdx.x;
+        on[i] = u < end;
+        if (!on[i]) continue;
+        row[i] = fastdiv(u, plan.by_each);
+        const uint32_t rest = u - row[i] * plan.by_each.d;
+        head[i] = fastdiv(rest, plan.by_units);
+        unit[i] = rest - head[i] * plan.by_units.d;
+        // values are not turned, and their channels go by the same units
+        at[i] = rotary_unit<V>((int)unit[i], a.pairs, a.D, a.interleaved);
+        turned[i] = at[i].turned && head[i] < (uint32_t)(a.H + a.KV);
+        const char* from;
+        if (head[i] < (uint32_t)a.H) from = static_cast<const char*>(a.q) + ((size_t)row[i] * a.ldq + (size_t)head[i] * a.D) * E;
+        else if (head[i] < (uint32_t)(a.H + a.KV)) from = static_cast<const char*>(a.new_k) + ((size_t)row[i] * a.ldk + (size_t)(head[i] - a.H) * a.D) * E;
+        else from = static_cast<const char*>(a.new_v) + ((size_t)row[i] * a.ldv + (size_t)(head[i] - a.H - a.KV) * a.D) * E;
+        x[i].load(from + (size_t)at[i].first * E);
+        if (at[i].both) y[i].load(from + (size_t)at[i].second * E);
+    }
+    __syncthreads();
+    for (uint32_t r = threadIdx.x; r < rows; r += 256u) {
+        const int t = (int)(row0 + r);
+        AppendRow k = {-1, ~0u};
+        // the last sequence that begins at or in front of t: of the samples, then of the offsets behind it
+        int lo = 0, hi = 256;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (samples[mid] <= t) lo = mid;
+            else hi = mid;
+        }
+        long long n = (long long)lo * plan.sample, to = n + plan.sample < a.N ? n + plan.sample : a.N;
+        while (to - n > 1) {
+            const long long mid = (n + to) / 2;
+            if (a.offsets[mid] <= t) n = mid;
+            else to = mid;
+        }
+        const int begin = page_offset_of(a, (int)n), finish = a.offsets[n + 1];
+        if (a.offsets[n] <= t && t < finish) {
+            k.place = page_length_of(a, (int)n) + (t - begin);
+            const uint32_t index = fastdiv((uint32_t)k.place, plan.by_page);
+            if (index < (uint32_t)a.width) {
+                const int page = a.table[(size_t)n * a.width + index];
+                if (page_exists(page, a.pages)) k.page = (uint32_t)page;
+            }
+        }
+        known[r] = k;
+    }
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < rows * (uint32_t)a.pairs; e += 256u) {
+        const uint32_t r = fastdiv(e, plan.by_pairs), p = e - r * (uint32_t)a.pairs;
+        const int place = known[r].place;
+        if (place < 0) continue;  // behind the last sequence
+        turns[e] = a.positions ? rotary_pair(a.positions + (size_t)(row0 + r) * a.axes, a.axes, a.frequencies, a.axis_of, (int)p, false)
+                               : rotary_pair(&place, 1, a.frequencies, a.axis_of, (int)p, false);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        if (!on[i]) continue;
+        const AppendRow k = known[row[i] - row0];
+        if (k.place < 0) continue;
+        if (turned[i]) rotary_apply<T, V>(x[i], y[i], turns + (size_t)(row[i] - row0) * a.pairs + unit[i] * V, a.interleaved);
+        char* to;
+        if (head[i] < (uint32_t)a.H) {
+            to = static_cast<char*>(a.o) + ((size_t)row[i] * a.ldo + (size_t)head[i] * a.D) * E;
+        } else {
+            if (k.page == ~0u) continue;
+            const bool key = head[i] < (uint32_t)(a.H + a.KV);
+            const uint32_t h = head[i] - a.H - (key ? 0 : a.KV), slot = (uint32_t)k.place - fastdiv((uint32_t)k.place, plan.by_page) * plan.by_page.d;
+            to = static_cast<char*>(key ? a.k : a.v) + (size_t)h * a.head_stride * E + page_place(k.page, slot, (uint64_t)a.page_stride * E, (uint32_t)(a.token_stride * E));
+        }
+        x[i].store(to + (size_t)at[i].first * E);
+        if (at[i].both) y[i].store(to + (size_t)at[i].second * E);
+    }
+}
+
+template <class T, int V>
+hipError_t launch(const PageArgs& a, const AppendPlan& plan, hipStream_t s) {
+    const size_t lds = (sizeof(f32x2) * a.pairs + sizeof(AppendRow)) * (size_t)plan.rows;
+    auto* const kernel = &page_append_kernel<T, V>;
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((plan.total + kRotaryUnits - 1) / kRotaryUnits)), dim3(256), lds, s, a, plan);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+bool page_append_fits(const PageArgs& a) {
+    return (double)a.rows * (a.H + 2 * a.KV) * rotary_units(a.D, a.pairs, rotary_vector(a.dtype, a.D, a.pairs)) < 2.0e9;
+}
+
+hipError_t launch_page_append(const PageArgs& a, hipStream_t s) {
+    const int V = rotary_vector(a.dtype, a.D, a.pairs);
+    AppendPlan plan;
+    plan.heads = a.H + 2 * a.KV;
+    plan.units = rotary_units(a.D, a.pairs, V);
+    const long long each = (long long)plan.heads * plan.units;
+    plan.total = a.rows * each;
+    plan.rows = rotary_rows(each);
+    plan.sample = (a.N + 255) / 256;
+    plan.by_each = make_fastdiv((uint32_t)each);
+    plan.by_units = make_fastdiv((uint32_t)plan.units);
+    plan.by_pairs = make_fastdiv(a.pairs > 0 ? (uint32_t)a.pairs : 1u);
+    plan.by_page = make_fastdiv((uint32_t)a.page_size);
+    if (a.dtype == 0) return V == 4 ? launch<SeqF32, 4>(a, plan, s) : launch<SeqF32, 1>(a, plan, s);
+    if (a.dtype == 1) return V == 8 ? launch<SeqBf16, 8>(a, plan, s) : V == 4 ? launch<SeqBf16, 4>(a, plan, s) : launch<SeqBf16, 1>(a, plan, s);
+    return V == 8 ? launch<SeqF16, 8>(a, plan, s) : V == 4 ? launch<SeqF16, 4>(a, plan, s) : launch<SeqF16, 1>(a, plan, s);
+}
+
+}  // namespace fwa

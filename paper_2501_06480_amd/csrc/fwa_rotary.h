@@ -1,0 +1,141 @@
+// Rotation of pairs of channels by their positions, as fwa_rotary.hip and fwa_page_append.hip have it.
+//
+// Pair p of a head is turned by the angle position[axis of p] * frequency[p]: (a, b) -> (a c - b s, b c + a s).  A unit of work is V pairs of
+// one head of one row: two vectors of V elements, V channels from each half of the rotated part, or (interleaved) 2 V neighbouring channels.  Channels behind
+// the pairs are copied, 2 V a unit.  Cosine and sine are formed once for all heads of a row and read from LDS, V pairs as 8 V bytes in a row.
+#pragma once
+
+#include "fwa_internal.h"
+#include "fwa_sequence.h"
+
+namespace fwa {
+
+// V neighbouring elements as they stand in memory: 16, 8 or, an element at a time, 4 or 2 bytes.
+template <class T, int V>
+struct RotaryVector {
+    static constexpr int kBytes = V * SeqSize<T>::value, kWords = kBytes >= 4 ? kBytes / 4 : 1;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const char* p) {
+        if constexpr (kBytes == 16) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = x[i];
+        } else if constexpr (kBytes == 8) {
+            const uint2 x = *reinterpret_cast<const uint2*>(p);
+            w[0] = x.x;
+            w[1] = x.y;
+        } else if constexpr (kBytes == 4) {
+            w[0] = *reinterpret_cast<const uint32_t*>(p);
+        } else {
+            w[0] = *reinterpret_cast<const uint16_t*>(p);
+        }
+    }
+    __device__ __forceinline__ void store(char* p) const {
+        if constexpr (kBytes == 16) *reinterpret_cast<u32x4*>(p) = u32x4{w[0], w[1], w[2], w[3]};
+        else if constexpr (kBytes == 8) *reinterpret_cast<uint2*>(p) = uint2{w[0], w[1]};
+        else if constexpr (kBytes == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
+        else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+    }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (__is_same(T, SeqF32)) {
+            const uint32_t x = w[i];
+            return __builtin_bit_cast(float, x);
+        } else {
+            const uint32_t x = i % 2 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu;
+            if constexpr (__is_same(T, SeqBf16)) return __builtin_bit_cast(float, x << 16);
+            else return (float)__builtin_bit_cast(_Float16, (uint16_t)x);
+        }
+    }
+    // all elements, rounded to the type
+    __device__ __forceinline__ void set(const float* x) {
+        if constexpr (__is_same(T, SeqF32)) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) w[i] = __builtin_bit_cast(uint32_t, x[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = pack_e<__is_same(T, SeqF16)>(x[2 * i], V == 1 ? 0.f : x[2 * i + 1]);
+        }
+    }
+};
+
+// Cosine and sine of position * frequency.  The product is formed in 64 bits and reduced to a part of one turn there: a position of 2^20 times a
+// frequency of 1 has 20 bits of whole turns in front of the angle, of which 32 bits would leave 4; what is left of the reduction's error is 2^-25
+// turns, from the fraction's rounding.
+__device__ __forceinline__ f32x2 rotary_turn(int position, float frequency, bool inverse) {
+    constexpr double kPerTurn = 0.15915494309189533577;  // 1 / (2 pi)
+    double turns = (double)position * ((double)frequency * kPerTurn);
+    turns -= __builtin_rint(turns);
+    float s, c;
+    sincospif(2.f * (float)turns, &s, &c);
+    return f32x2{c, inverse ? -s : s};
+}
+// that of pair p of a row with the given positions; an axis outside the row's leaves the pair as it is
+__device__ __forceinline__ f32x2 rotary_pair(const int32_t* positions, int axes, const float* frequencies, const int32_t* axis_of, int p, bool inverse) {
+    const uint32_t axis = axis_of ? (uint32_t)axis_of[p] : 0u;
+    if (axis >= (uint32_t)axes) return f32x2{1.f, 0.f};
+    return rotary_turn(positions[axis], frequencies[p], inverse);
+}
+
+// Where the two vectors of unit `u` of a head begin, in channels; the second may not exist for channels that are copied.
+struct RotaryUnit {
+    int first, second;
+    bool turned, both;
+};
+template <int V>
+__device__ __forceinline__ RotaryUnit rotary_unit(int u, int pairs, int d, bool interleaved) {
+    RotaryUnit r;
+    r.turned = u * V < pairs;
+    if (r.turned && !interleaved) {
+        r.first = u * V;
+        r.second = pairs + u * V;
+    } else {
+        r.first = r.turned ? 2 * V * u : 2 * pairs + 2 * V * (u - pairs / V);
+        r.second = r.first + V;
+    }
+    r.both = r.second < d;
+    return r;
+}
+
+// The V pairs of two vectors, `table` = cosine and sine of the first of them in LDS.
+template <class T, int V>
+__device__ __forceinline__ void rotary_apply(RotaryVector<T, V>& x, RotaryVector<T, V>& y, const f32x2* table, bool interleaved) {
+    float a[2 * V], z[2 * V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        a[i] = x.get(i);
+        a[V + i] = y.get(i);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const f32x2 t = table[i];
+        const float c = t[0], s = t[1];
+        const float h0 = a[i], h1 = a[V + i], n0 = a[2 * i], n1 = a[2 * i + 1];
+        const float p = interleaved ? n0 : h0, q = interleaved ? n1 : h1;
+        const float first = fmaf(p, c, -(q * s)), second = fmaf(q, c, p * s);
+        if (interleaved) {
+            z[2 * i] = first;
+            z[2 * i + 1] = second;
+        } else {
+            z[i] = first;
+            z[V + i] = second;
+        }
+    }
+    x.set(z);
+    y.set(z + V);
+}
+
+// Elements of a vector: 16 bytes where widths and pairs are whole vectors, half of that (16-bit data, heads of 72 channels for
+// instance), or single elements.  16-byte vectors against single ones, 2 x 6272 rows of 16 heads of 128, bf16: see fwa_rotary.hip.
+inline int rotary_vector(int dtype, int d, int pairs) {
+    const int most = dtype == 0 ? 4 : 8;
+    if (d % most == 0 && pairs % most == 0) return most;
+    return dtype != 0 && d % 4 == 0 && pairs % 4 == 0 ? 4 : 1;
+}
+// units of a head
+inline int rotary_units(int d, int pairs, int V) { return pairs / V + (d - 2 * pairs + 2 * V - 1) / (2 * V); }
+
+constexpr int kRotaryUnits = 512;  // of a workgroup of 256 threads
+// Rows that a workgroup's units may touch, of `each` units a row.
+inline int rotary_rows(long long each) { return (int)((kRotaryUnits - 1) / each) + 2; }
+
+}  // namespace fwa

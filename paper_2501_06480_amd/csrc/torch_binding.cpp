@@ -508,6 +508,194 @@ py::object sequence_backward(const at::Tensor& q, const at::Tensor& k, const at:
     return py::make_tuple(d.q, d.k, d.v, or_none(d.bias));
 }
 
+// ------------------------------------------------------------------ rotary positions, paged cache
+
+// Rows of [N, L, C], or of packed [T, C]
+Rows any_rows_of(const at::Tensor& t, const char* name, const at::Tensor* like) {
+    need_gpu(t, name);
+    if (t.dim() == 3) return rows_of(t, name, like);
+    if (t.dim() != 2) value_error(std::string(name) + " must be [N, L, C] or [T, C]");
+    if (like) need_like(t, name, *like);
+    const int64_t T = t.size(0), C = t.size(1);
+    if (t.is_contiguous()) return {t.data_ptr(), C};
+    if ((C > 1 && t.stride(1) != 1) || (T > 1 && t.stride(0) < C)) value_error(std::string(name) + ": channels must be contiguous and token rows evenly spaced");
+    return {t.data_ptr(), T > 1 ? t.stride(0) : C};
+}
+
+// The rotation's tables
+struct Rotation {
+    const int32_t* positions = nullptr;
+    const float* frequencies = nullptr;
+    const int32_t* axis_of = nullptr;
+    int axes = 1, pairs = 0;
+};
+Rotation rotation_of(const OptTensor& positions, const OptTensor& frequencies, const OptTensor& axis_of, const at::Tensor& like) {
+    Rotation r;
+    if (!frequencies) {
+        if (positions || axis_of) value_error("positions and axis_of go with frequencies");
+        return r;
+    }
+    need_same_device(*frequencies, "frequencies", like);
+    if (frequencies->scalar_type() != at::kFloat || frequencies->dim() != 1 || !frequencies->is_contiguous())
+        value_error("frequencies must be a contiguous float32 tensor [pairs]");
+    r.frequencies = frequencies->data_ptr<float>();
+    r.pairs = to_int(frequencies->size(0), "pairs");
+    if (positions) {
+        need_same_device(*positions, "positions", like);
+        if (positions->scalar_type() != at::kInt || positions->dim() < 2 || !positions->is_contiguous())
+            value_error("positions must be a contiguous int32 tensor with the axes last");
+        r.positions = positions->data_ptr<int32_t>();
+        r.axes = to_int(positions->size(-1), "axes");
+    }
+    if (axis_of) {
+        need_same_device(*axis_of, "axis_of", like);
+        if (axis_of->scalar_type() != at::kInt || axis_of->dim() != 1 || axis_of->size(0) != frequencies->size(0) || !axis_of->is_contiguous())
+            value_error("axis_of must be a contiguous int32 tensor [pairs]");
+        r.axis_of = axis_of->data_ptr<int32_t>();
+    }
+    return r;
+}
+
+int run_rotary(at::Tensor& y, const at::Tensor& x, int64_t heads, const at::Tensor& positions, const at::Tensor& frequencies, const OptTensor& axis_of, bool interleaved,
+               bool inverse, const OptTensor& out, std::optional<uintptr_t> stream) {
+    need_gpu(x, "x");
+    if (x.dim() != 2 && x.dim() != 3) value_error("x must be [N, L, heads * d] or [T, heads * d]");
+    if (heads < 1 || x.size(-1) == 0 || x.size(-1) % heads != 0) value_error("the channels of x must be a multiple of heads");
+    const Rotation r = rotation_of(positions, frequencies, axis_of, x);
+    const bool shared = positions.dim() == 2;
+    if (positions.dim() > x.dim() || positions.size(-2) != x.size(-2) || (!shared && positions.size(0) != x.size(0)))
+        value_error("positions must be [L, axes] or [N, L, axes], of packed rows [T, axes]");
+    const int64_t rows = x.dim() == 3 ? x.size(0) * x.size(1) : x.size(0);
+    const Rows rx = any_rows_of(x, "x", nullptr);
+    y = out ? *out : at::empty(x.sizes(), x.options());
+    const Rows ry = any_rows_of(y, "out", &x);
+    if (rows == 0) return FWA_OK;
+    const int dtype = dtype_code(x);
+    void* const st = stream_of(stream, x);
+    const c10::DeviceGuard guard(x.device());
+    const Nogil nogil;
+    return fwa_rotary(rx.p, ry.p, rows, to_int(heads, "heads"), to_int(x.size(-1) / heads, "d"), rx.ld, ry.ld, r.positions, shared ? positions.size(0) : rows, r.axes,
+                      r.frequencies, r.axis_of, r.pairs, interleaved, inverse, dtype, st);
+}
+py::object rotary(const at::Tensor& x, int64_t heads, const at::Tensor& positions, const at::Tensor& frequencies, const OptTensor& axis_of, bool interleaved, bool inverse,
+                  const OptTensor& out, std::optional<uintptr_t> stream) {
+    at::Tensor y;
+    const int rc = run_rotary(y, x, heads, positions, frequencies, axis_of, interleaved, inverse, out, stream);
+    return rc == FWA_OK ? py::cast(y) : py::cast(rc);
+}
+
+// Cache and tables of a call with packed rows
+struct Pages {
+    void *k, *v;
+    int64_t N, rows, pages, page_stride, token_stride, head_stride;
+    int kv_heads, d, page_size, width;
+    const int32_t *table, *offsets, *lengths;
+};
+Pages pages_of(const at::Tensor& like, const char* name, const at::Tensor& k_pages, const at::Tensor& v_pages, const at::Tensor& page_table, const at::Tensor& offsets,
+               const at::Tensor& lengths) {
+    need_gpu(like, name);
+    if (like.dim() != 2) value_error(std::string(name) + " must be packed rows [T, channels]");
+    for (const auto& t : {std::make_pair(&k_pages, "k_pages"), std::make_pair(&v_pages, "v_pages")}) {
+        need_same_device(*t.first, t.second, like);
+        if (t.first->dim() != 4 || t.first->scalar_type() != like.scalar_type())
+            value_error(std::string(t.second) + " must be [pages, page_size, kv_heads, d] of the type of " + name);
+        if (t.first->size(3) > 1 && t.first->stride(3) != 1) value_error(std::string(t.second) + ": channels must be contiguous");
+    }
+    if (k_pages.sizes() != v_pages.sizes()) value_error("k_pages and v_pages must have one shape");
+    for (int i = 0; i < 3; ++i)
+        if (k_pages.size(i) > 1 && k_pages.stride(i) != v_pages.stride(i)) value_error("k_pages and v_pages must share their strides");
+    for (const auto& t : {std::make_pair(&page_table, "page_table"), std::make_pair(&offsets, "offsets"), std::make_pair(&lengths, "lengths")}) {
+        need_same_device(*t.first, t.second, like);
+        if (t.first->scalar_type() != at::kInt || !t.first->is_contiguous()) value_error(std::string(t.second) + " must be a contiguous int32 tensor");
+    }
+    if (lengths.dim() != 1) value_error("lengths must be [N]");
+    Pages p;
+    p.N = lengths.size(0);
+    if (offsets.dim() != 1 || offsets.size(0) != p.N + 1) value_error("offsets must be [N + 1]");
+    if (page_table.dim() != 2 || page_table.size(0) != p.N) value_error("page_table must be [N, width]");
+    p.rows = like.size(0);
+    p.pages = k_pages.size(0);
+    p.page_size = to_int(k_pages.size(1), "page_size");
+    p.kv_heads = to_int(k_pages.size(2), "kv_heads");
+    p.d = to_int(k_pages.size(3), "d");
+    p.width = to_int(page_table.size(1), "width");
+    // a stride that no element needs may be anything
+    p.head_stride = p.kv_heads > 1 ? k_pages.stride(2) : p.d;
+    p.token_stride = p.page_size > 1 ? k_pages.stride(1) : p.d;
+    p.page_stride = p.pages > 1 ? k_pages.stride(0) : 0;
+    p.k = k_pages.data_ptr();
+    p.v = v_pages.data_ptr();
+    p.table = page_table.data_ptr<int32_t>();
+    p.offsets = offsets.data_ptr<int32_t>();
+    p.lengths = lengths.data_ptr<int32_t>();
+    return p;
+}
+
+py::object page_append(const at::Tensor& k, const at::Tensor& v, const at::Tensor& k_pages, const at::Tensor& v_pages, const at::Tensor& page_table,
+                       const at::Tensor& offsets, const at::Tensor& lengths, const OptTensor& frequencies, const OptTensor& positions, const OptTensor& axis_of,
+                       bool interleaved, const OptTensor& q, const OptTensor& q_out, std::optional<uintptr_t> stream) {
+    const Pages p = pages_of(k, "k", k_pages, v_pages, page_table, offsets, lengths);
+    const Rows rk = any_rows_of(k, "k", nullptr), rv = any_rows_of(v, "v", &k);
+    if (p.d < 1 || k.size(1) != (int64_t)p.kv_heads * p.d) value_error("the channels of k must be kv_heads * d");
+    const Rotation r = rotation_of(positions, frequencies, axis_of, k);
+    if (positions && (positions->dim() != 2 || positions->size(0) != p.rows)) value_error("positions must be [T, axes]");
+    if (q_out && !q) value_error("q_out goes with q");
+    at::Tensor y;
+    Rows rq = {nullptr, 0}, ry = {nullptr, 0};
+    int64_t heads = 0;
+    if (q) {
+        need_same_device(*q, "q", k);
+        if (q->dim() != 2 || q->size(0) != p.rows || q->scalar_type() != k.scalar_type() || q->size(1) == 0 || q->size(1) % p.d != 0)
+            value_error("q must be [T, heads * d] of the type of k");
+        heads = q->size(1) / p.d;
+        rq = any_rows_of(*q, "q", nullptr);
+        y = q_out ? *q_out : at::empty(q->sizes(), q->options());
+        ry = any_rows_of(y, "q_out", &*q);
+    }
+    const int dtype = dtype_code(k);
+    void* const st = stream_of(stream, k);
+    int rc;
+    {
+        const c10::DeviceGuard guard(k.device());
+        const Nogil nogil;
+        rc = fwa_page_append(rk.p, rv.p, p.k, p.v, p.rows, p.N, p.kv_heads, p.d, rk.ld, rv.ld, p.pages, p.page_size, p.page_stride, p.token_stride, p.head_stride, p.table,
+                             p.width, p.offsets, p.lengths, r.positions, r.axes, r.frequencies, r.axis_of, r.pairs, interleaved, p.rows ? rq.p : nullptr, ry.p, (int)heads,
+                             rq.ld, ry.ld, dtype, st);
+    }
+    if (rc != FWA_OK) return py::cast(rc);
+    return or_none(y);
+}
+
+py::object page_forward(const at::Tensor& q, const at::Tensor& k_pages, const at::Tensor& v_pages, const at::Tensor& page_table, const at::Tensor& offsets,
+                        const at::Tensor& lengths, int64_t heads, double scale, int64_t most_new, bool causal, bool want_stats, const OptTensor& out,
+                        const OptTensor& workspace, std::optional<uintptr_t> stream) {
+    const Pages p = pages_of(q, "q", k_pages, v_pages, page_table, offsets, lengths);
+    if (heads < 1 || p.kv_heads < 1 || heads % p.kv_heads != 0 || q.size(1) != heads * p.d)
+        value_error("the channels of q must be heads * d, heads a multiple of kv_heads");
+    const Rows rq = any_rows_of(q, "q", nullptr);
+    const at::Tensor o = out ? *out : at::empty(q.sizes(), q.options());
+    const Rows ro = any_rows_of(o, "out", &q);
+    at::Tensor stats;
+    if (want_stats) stats = at::empty({p.rows, heads, 2}, q.options().dtype(at::kFloat));
+    const int dtype = dtype_code(q), H = to_int(heads, "heads"), most = to_int(most_new < 0 || most_new > p.rows ? p.rows : most_new, "most_new");
+    if (workspace) need_same_device(*workspace, "workspace", q);
+    const at::Tensor ws = workspace ? *workspace : scratch(fwa_page_forward_workspace_bytes(p.rows, p.N, H, p.kv_heads, p.d, p.page_size, p.width, most, dtype), q);
+    float* const sp = stats.defined() ? stats.data_ptr<float>() : nullptr;
+    void* const wp = ws.defined() ? ws.data_ptr() : nullptr;
+    const size_t wb = ws.defined() ? (size_t)ws.nbytes() : 0;
+    void* const st = stream_of(stream, q);
+    int rc;
+    {
+        const c10::DeviceGuard guard(q.device());
+        const Nogil nogil;
+        rc = fwa_page_forward(rq.p, p.k, p.v, ro.p, sp, p.rows, p.N, H, p.kv_heads, p.d, (float)scale, rq.ld, ro.ld, p.pages, p.page_size, p.page_stride, p.token_stride,
+                              p.head_stride, p.table, p.width, p.offsets, p.lengths, most, causal, dtype, wp, wb, st);
+    }
+    if (rc != FWA_OK) return py::cast(rc);
+    if (want_stats) return py::make_tuple(o, stats);
+    return py::cast(o);
+}
+
 // ------------------------------------------------------------------ autograd
 // The two differentiable calls as native nodes.  What they save goes through the engine's saved variables (version counters,
 // saved-tensor hooks); an error in the backward reaches Python as the exception that the direct call raises.
@@ -684,6 +872,35 @@ at::Tensor sequence_attention(const at::Tensor& q, const at::Tensor& k, const at
     return SequenceAttention::apply(q, k, v, table, buckets, q_lengths, k_lengths, q_start, heads, scale, causal);
 }
 
+struct Rotary : torch::autograd::Function<Rotary> {
+    static at::Tensor forward(AutogradContext* ctx, const at::Tensor& x, const at::Tensor& positions, const at::Tensor& frequencies, const OptTensor& axis_of, int64_t heads,
+                              bool interleaved, bool inverse) {
+        ctx->save_for_backward({positions, frequencies, or_undefined(axis_of)});
+        ctx->saved_data["heads"] = heads;
+        ctx->saved_data["interleaved"] = interleaved;
+        ctx->saved_data["inverse"] = inverse;
+        at::Tensor y;
+        const int rc = run_rotary(y, x, heads, positions, frequencies, axis_of, interleaved, inverse, std::nullopt, std::nullopt);
+        if (rc != FWA_OK) raise_status(rc, "fwa_rotary");
+        return y;
+    }
+    static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
+        return with_python_errors([&]() -> variable_list {
+            const variable_list s = ctx->get_saved_variables();
+            at::Tensor dx;
+            const int rc = run_rotary(dx, aligned(grads[0]), ctx->saved_data["heads"].toInt(), s[0].contiguous(), s[1].contiguous(),
+                                      s[2].defined() ? OptTensor(s[2].contiguous()) : OptTensor(), ctx->saved_data["interleaved"].toBool(),
+                                      !ctx->saved_data["inverse"].toBool(), std::nullopt, std::nullopt);
+            if (rc != FWA_OK) raise_status(rc, "fwa_rotary");
+            return {dx, at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()};
+        });
+    }
+};
+at::Tensor rotary_node(const at::Tensor& x, int64_t heads, const at::Tensor& positions, const at::Tensor& frequencies, const OptTensor& axis_of, bool interleaved,
+                       bool inverse) {
+    return Rotary::apply(x, positions, frequencies, axis_of, heads, interleaved, inverse);
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_fwa_torch, m) {
@@ -701,4 +918,8 @@ PYBIND11_MODULE(_fwa_torch, m) {
     m.def("sequence_backward", &sequence_backward);
     m.def("bucket_bias", torch::wrap_pybind_function(&bucket_bias));
     m.def("sequence_attention", torch::wrap_pybind_function(&sequence_attention));
+    m.def("rotary", &rotary);
+    m.def("page_append", &page_append);
+    m.def("page_forward", &page_forward);
+    m.def("rotary_node", torch::wrap_pybind_function(&rotary_node));
 }

@@ -1,0 +1,69 @@
+"""Where the operators on a paged cache read and write, on the CPU: the functions that the kernels take their addresses from (csrc/fwa_page_index.h), walked the way the
+kernels walk them, over tables that hold anything: no access outside the page that was allotted, none of a page that is not there."""
+import os
+import subprocess
+
+from paper_2501_06480_amd import build
+
+DRIVER = r'''
+#include "fwa_page_index.h"
+#include <climits>
+#include <cstdio>
+#include <cstdlib>
+#include <random>
+using namespace fwa;
+static void need(bool ok, const char* what) { if (!ok) { std::printf("FAILED %s\n", what); std::exit(1); } }
+int main() {
+    std::mt19937 g(1);
+    auto pick = [&](int lo, int hi) { return (int)(lo + (long long)(g() % (uint64_t)((long long)hi - lo + 1))); };
+    const int odd[] = {INT_MIN, -1, 0, 1, INT_MAX, 1 << 29, (1 << 29) + 1, 17};
+    long long loads = 0;
+    for (int round = 0; round < 4000; ++round) {
+        const int size = 16 * pick(1, 8), width = pick(0, 6), pages = pick(0, 7), rows = pick(1, 200), most = pick(0, 220), heads = pick(1, 3);
+        const uint32_t row_bytes = 64u << pick(0, 3), token_bytes = row_bytes * (uint32_t)heads, group = pick(0, 1) ? 16 : 8;
+        const uint64_t page_bytes = (uint64_t)token_bytes * size + (pick(0, 1) ? 0 : 16u * pick(0, 5));
+        int table[8], offsets[2], length;
+        for (int& e : table) e = pick(0, 3) ? pick(-1, pages) : odd[pick(0, 7)];
+        for (int& e : offsets) e = pick(0, 3) ? pick(-5, rows + 5) : odd[pick(0, 7)];
+        length = pick(0, 3) ? pick(-5, width * size + 20) : odd[pick(0, 7)];
+        const int begin = page_offset(offsets[0], rows), count = page_count(begin, page_offset(offsets[1], rows), most), start = page_length(length);
+        need(begin >= 0 && count >= 0 && begin + count <= rows && count <= most, "new tokens");
+        const int keys = page_keys(start, count, width, size);
+        need(keys >= 0 && keys <= width * size, "keys");
+        // attention: groups of 16 (or 8) keys from the first to one behind the last
+        for (int key = 0; key < keys + 64 && keys > 0; key += (int)group) {
+            const int last = (keys - 1) / kPageRows, at = key / kPageRows, sub = at < last ? at : last, index = sub / (size / kPageRows);
+            need(index >= 0 && index < width, "entry of the table");
+            const int page = table[index], n = page_group(key, keys, (int)group, page_exists(page, pages));
+            need(n >= 0 && n <= (int)group && (n == 0 || key + n <= keys), "rows of a group");
+            if (n == 0) { need(page_bytes_of(n, token_bytes, row_bytes) == 0, "no bytes"); continue; }
+            const uint32_t of = (uint32_t)key / kPageRows / (uint32_t)(size / kPageRows), slot = (uint32_t)key - of * (uint32_t)size;
+            need(of == (uint32_t)index, "one page");
+            const uint64_t from = page_place((uint32_t)page, slot, page_bytes, token_bytes), bytes = page_bytes_of(n, token_bytes, row_bytes);
+            need(page >= 0 && page < pages && slot + (uint32_t)n <= (uint32_t)size, "rows of the page");
+            need(from >= (uint64_t)page * page_bytes && from + bytes + (uint64_t)(heads - 1) * row_bytes <= (uint64_t)page * page_bytes + (uint64_t)token_bytes * size, "bytes");
+            ++loads;
+        }
+        // append: the places of the new tokens
+        for (int i = 0; i < count; ++i) {
+            const uint32_t place = (uint32_t)(start + i), index = place / (uint32_t)size;
+            if (index >= (uint32_t)width || !page_exists(table[index], pages)) continue;
+            const uint64_t to = page_place((uint32_t)table[index], place - index * (uint32_t)size, page_bytes, token_bytes);
+            need(to + token_bytes <= (uint64_t)table[index] * page_bytes + (uint64_t)token_bytes * size, "stores");
+            ++loads;
+        }
+    }
+    // far into a large cache
+    need(page_place(70000u, 255u, 1ull << 31, 1u << 22) == 70000ull * (1ull << 31) + 255ull * (1u << 22), "64 bits");
+    std::printf("%lld accesses\n", loads);
+    return loads > 10000 ? 0 : 1;
+}
+'''
+
+
+def test_no_table_leads_outside(tmp_path):
+    src, exe = tmp_path / "driver.cpp", tmp_path / "driver"
+    src.write_text(DRIVER)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True, env={**os.environ, "UBSAN_OPTIONS": "print_stacktrace=1"})
+    assert r.returncode == 0, r.stdout + r.stderr
