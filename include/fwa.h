@@ -318,8 +318,8 @@ int fwa_rotary(const void* x, void* y, int64_t rows, int heads, int d, int64_t l
  * page page_table[n][t / page_size].
  *   k_pages, v_pages : [pages, page_size, kv_heads, d]; row r of page p of head h begins p * page_stride + r * token_stride + h * head_stride
  *                      elements behind the base, so pages with a head's rows together ([pages, kv_heads, page_size, d]) are meant as well.  The strides, one set
- *                      for both, are multiples of 16 bytes (FWA_ERR_ALIGN), reach no element twice (FWA_ERR_SHAPE), token_stride <= 2^20
- *                      elements.  Keys and values may interleave in one buffer.
+ *                      for both, are multiples of 16 bytes (FWA_ERR_ALIGN), reach no element twice (FWA_ERR_SHAPE), token_stride <= 2^20,
+ *                      page_stride <= 2^29 elements.  Keys and values may interleave in one buffer.
  *   page_size        : a multiple of 16, at most 65536; width * page_size <= 2^29; the whole cache of any size
  *   page_table       : [N, width] int32.  An entry outside [0, pages) is no page: nothing is stored there and its keys are not seen.
  *   offsets          : [N + 1] int32, not falling: the new tokens of sequence n are rows offsets[n] .. offsets[n + 1] - 1 of the packed tensors

@@ -89,9 +89,9 @@ int check_pages(fwa::PageArgs& a, int64_t rows, int64_t N, int heads, int kv_hea
     const int64_t per16 = dtype == FWA_F32 ? 4 : 8;
     if (page_stride < 0 || token_stride < 0 || head_stride < 0) return FWA_ERR_SHAPE;
     if (page_stride % per16 != 0 || token_stride % per16 != 0 || head_stride % per16 != 0) return FWA_ERR_ALIGN;
-    if (token_stride > (int64_t)1 << 20 || head_stride > (int64_t)1 << 40 || page_stride > (int64_t)1 << 40) return FWA_ERR_UNSUPPORTED;
+    if (token_stride > (int64_t)1 << 20 || page_stride > (int64_t)1 << 29 || head_stride > (int64_t)1 << 40) return FWA_ERR_UNSUPPORTED;
     a.rows = (int)rows; a.N = (int)N; a.H = heads; a.KV = kv_heads; a.D = d; a.dtype = dtype;
-    a.pages = pages; a.page_size = page_size; a.width = width;
+    a.pages = (int)pages; a.page_size = page_size; a.width = width;
     a.page_stride = page_stride; a.token_stride = token_stride; a.head_stride = head_stride;
     Dim dims[3];
     cache_dims(a, dims);

@@ -179,8 +179,8 @@ hipError_t launch_rotary(const RotaryArgs& a, hipStream_t s);
 struct PageArgs {
     void* k;             // row t % page_size of page p of head h: k + p page_stride + (t % page_size) token_stride + h head_stride elements
     void* v;
-    long long pages, page_stride, token_stride, head_stride;
-    int page_size, width;
+    long long page_stride, token_stride, head_stride;
+    int pages, page_size, width;
     const int32_t* table;    // [N, width]
     const int32_t* offsets;  // [N + 1]
     const int32_t* lengths;  // [N]: tokens in the cache in front of the new ones

@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(256) page_append_kernel(PageArgs a, AppendPlan
             if (k.page == ~0u) continue;
             const bool key = head[i] < (uint32_t)(a.H + a.KV);
             const uint32_t h = head[i] - a.H - (key ? 0 : a.KV), slot = (uint32_t)k.place - fastdiv((uint32_t)k.place, plan.by_page) * plan.by_page.d;
-            to = static_cast<char*>(key ? a.k : a.v) + (size_t)h * a.head_stride * E + page_place(k.page, slot, (uint64_t)a.page_stride * E, (uint32_t)(a.token_stride * E));
+            to = static_cast<char*>(key ? a.k : a.v) + (size_t)h * a.head_stride * E + page_place(k.page, slot, (uint32_t)(a.page_stride * E), (uint32_t)(a.token_stride * E));
         }
         x[i].store(to + (size_t)at[i].first * E);
         if (at[i].both) y[i].store(to + (size_t)at[i].second * E);

@@ -17,14 +17,15 @@ constexpr float kSlack = 6.f;
 constexpr int kFewRows = 32;  // rows (new tokens times heads of a group) up to which the waves of a workgroup share out the keys
 constexpr int kLeastTiles = 4;  // of a wave, where workgroups share out the keys
 
-// One form's share of a call.
+// How a call is laid out on the device.
 struct PagePlan {
+    int keys;         // the waves of a workgroup share out the keys, not the rows
     int rows;         // of a block
     int group;        // heads of queries per head of keys
     int each;         // blocks of each sequence, 0: as many as it has, found by a search
     int blocks, splits;
     int least;        // tiles that a part has at least
-    int only;         // 1: sequences of few rows are another form's, -1: those of more, 0: all are this one's
+    int rounds;       // workgroups in rounds of 256 go forwards and backwards in turn
     FastDiv by_kv, by_splits, by_each, by_group, by_sub;
     size_t slots;     // blocks * KV * splits * rows: rows of parts
     float* part_o;    // [block][kv][split][rows][D], not divided by the sum
@@ -71,7 +72,6 @@ __device__ __forceinline__ bool page_block(const PageArgs& a, const PagePlan& pl
     b.rows = count * plan.group;
     b.row0 = within * ROWS;
     if (within < 0 || b.row0 >= b.rows) return false;
-    if (plan.only != 0 && (b.rows <= kFewRows) != (plan.only < 0)) return false;
     b.start = page_length_of(a, n);
     b.klen = page_keys(b.start, count, a.width, a.page_size);
     const int last_row = b.rows - b.row0 < ROWS ? b.rows - 1 : b.row0 + ROWS - 1;
@@ -86,33 +86,31 @@ __device__ __forceinline__ int page_parts(const PagePlan& plan, int tiles, int& 
     return (tiles + per - 1) / per;
 }
 
-// acc[m][b] += V[rows of the block][channels 32 b ..]^T times w[m], for MB blocks of rows at once: the operand is read once for all.
-template <class T, int D, int MB>
-__device__ __forceinline__ void page_accumulate(const SeqColumnReader<T, D>& reader, f32x16 (&acc)[MB][D / 32], uint32_t tile, int block, const f32x16 (&w)[MB]) {
+// 16 rows of a tile of V (the `half`-th), as the operand of a product over them: 32 channels in each of v.
+template <class T, int D>
+__device__ __forceinline__ void page_values(const SeqColumnReader<T, D>& reader, u32x4 (&v)[D / 32], uint32_t tile, int half) {
     constexpr int RB = D * SeqSize<T>::value;
-    if constexpr (MB == 1) {
-        reader.accumulate(acc[0], tile, block, w[0]);
-    } else {
-        static_assert(!__is_same(T, SeqF32), "16-bit data");
-        constexpr bool F16 = __is_same(T, SeqF16);
-        tile += (uint32_t)(32 * RB * block);
+    tile += (uint32_t)(16 * RB * half);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            u32x4 x[MB];
-#pragma unroll
-            for (int m = 0; m < MB; ++m)
-                x[m] = u32x4{pack_e<F16>(w[m][8 * t], w[m][8 * t + 1]), pack_e<F16>(w[m][8 * t + 2], w[m][8 * t + 3]),
-                             pack_e<F16>(w[m][8 * t + 4], w[m][8 * t + 5]), pack_e<F16>(w[m][8 * t + 6], w[m][8 * t + 7])};
-#pragma unroll
-            for (int b = 0; b < D / 32; ++b) {
-                const uint32_t first = reader.at ^ (uint32_t)(64 * b), second = first ^ (seq_swizzle<RB>(8u) << 4);
-                const uint2 p = seq_lds_tr(tile + first + (uint32_t)(16 * t) * RB);
-                const uint2 q = seq_lds_tr(tile + second + (uint32_t)(16 * t + 8) * RB);
-#pragma unroll
-                for (int m = 0; m < MB; ++m) acc[m][b] = seq_dot<T>(u32x4{p.x, p.y, q.x, q.y}, x[m], acc[m][b]);
-            }
-        }
+    for (int b = 0; b < D / 32; ++b) {
+        const uint32_t first = reader.at ^ (uint32_t)(64 * b), second = first ^ (seq_swizzle<RB>(8u) << 4);
+        const uint2 p = seq_lds_tr(tile + first), q = seq_lds_tr(tile + second + 8u * RB);
+        v[b] = u32x4{p.x, p.y, q.x, q.y};
     }
+}
+// acc[m][b] += those rows' channels 32 b .. times their weights in half `h` of w[m], for MB blocks of rows at once.
+template <class T, int D, int MB>
+__device__ __forceinline__ void page_products(f32x16 (&acc)[MB][D / 32], const u32x4 (&v)[D / 32], const f32x16 (&w)[MB], int h) {
+    constexpr bool F16 = __is_same(T, SeqF16);
+    u32x4 x[MB];
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+        x[m] = u32x4{pack_e<F16>(w[m][8 * h], w[m][8 * h + 1]), pack_e<F16>(w[m][8 * h + 2], w[m][8 * h + 3]), pack_e<F16>(w[m][8 * h + 4], w[m][8 * h + 5]),
+                     pack_e<F16>(w[m][8 * h + 6], w[m][8 * h + 7])};
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int m = 0; m < MB; ++m) acc[m][b] = seq_dot<T>(v[b], x[m], acc[m][b]);
 }
 
 // A wave's loads of a tile: its rows in groups of 16 (or 8) that lie in one page each.
@@ -149,15 +147,19 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, KS = KT / 32, SUB = KT / kPageRows;
     constexpr int ROWS = KEYS ? 32 : 32 * MB * W, TURN = KEYS ? W : 1;  // of a workgroup; from a wave's tile to its next one
     constexpr uint32_t kTile = KT * RB;
-    static_assert(!KEYS || MB == 1, "one block of rows where the waves share out the keys");
+    static_assert(MB == 1 || !(KEYS || __is_same(T, SeqF32)), "one block of rows where the waves share out the keys, and of fp32");
     using Loader = PageLoader<RB, KT, KEYS ? 1 : W>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t hi = lane >> 5, c = lane & 31u;
     const uint32_t base = lds_offset(lds) + (KEYS ? wave * 4u * kTile : 0u);
 
-    // workgroup -> head of the keys (neighbours, so that each XCD has few of them), part of the keys, block of rows, the last ones of which have most keys
-    const uint32_t rest = fastdiv(blockIdx.x, plan.by_kv), hk = blockIdx.x - rest * plan.by_kv.d;
+    // workgroup -> head of the keys (neighbours, so that each XCD has few of them), part of the keys, block of rows, the last ones of which have most
+    // keys; rounds of as many workgroups as there are CUs go forwards and backwards in turn, so that a CU's come to one sum
+    uint32_t id = blockIdx.x;
+    const uint32_t round = id >> 8;
+    if ((round & 1u) && round < (uint32_t)plan.rounds) id = 512u * round + 248u - id + 2u * (id & 7u);
+    const uint32_t rest = fastdiv(id, plan.by_kv), hk = id - rest * plan.by_kv.d;
     const uint32_t turn = fastdiv(rest, plan.by_splits), split = rest - turn * plan.by_splits.d;
     const int block = plan.blocks - 1 - (int)turn;
     PageBlock b;
@@ -173,7 +175,7 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     const char* const kp = static_cast<const char*>(a.k) + head_at;
     const char* const vp = static_cast<const char*>(a.v) + head_at;
     const uint32_t token_bytes = (uint32_t)(a.token_stride * E);
-    const uint64_t page_bytes = (uint64_t)a.page_stride * E;
+    const uint32_t page_bytes = (uint32_t)(a.page_stride * E);
     const int32_t* const page_row = a.table + (size_t)b.n * a.width;
 
     Loader load;
@@ -183,35 +185,53 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     SeqColumnReader<T, D> column_reader;
     column_reader.init(hi, c);
 
-    // The pages of a tile: those of this wave's groups, and which of all have none.
-    struct Pages {
-        int own[Loader::kGroups];
-        uint32_t bad;
+    // Pages are looked up two tiles ahead of their use, so that nothing waits for the scalar loads, and in steps from group to group, without a
+    // division: a group's place is an entry of the table and a row of that page.
+    struct Place {
+        int index, slot;
     };
-    const int last_sub = klen > 0 ? (klen - 1) / kPageRows : 0;
-    auto look = [&](int t) {
-        Pages p;
-        p.bad = 0u;
-#pragma unroll
-        for (int j = 0; j < SUB; ++j) {
-            const int sub = t * SUB + j < last_sub ? t * SUB + j : last_sub;
-            const int page = seq_constant(page_row, fastdiv((uint32_t)sub, plan.by_sub));
-            p.bad |= page_exists(page, a.pages) ? 0u : 1u << j;
-            if (KEYS) p.own[j % Loader::kGroups] = page;
-        }
-        if constexpr (!KEYS) {
-            const int at = (t * KT + load.row) / kPageRows, sub = at < last_sub ? at : last_sub;
-            p.own[0] = seq_constant(page_row, fastdiv((uint32_t)sub, plan.by_sub));
-        }
-        return p;
+    const int page_size = a.page_size, last_index = klen > 0 ? (int)fastdiv((uint32_t)(klen - 1) / (uint32_t)kPageRows, plan.by_sub) : 0;
+    auto place_of = [&](int key) {
+        const int index = (int)fastdiv((uint32_t)key / (uint32_t)kPageRows, plan.by_sub);
+        return Place{index, key - index * page_size};
     };
-    auto issue = [&](int t, const Pages& p, uint32_t buf) {
+    auto find = [&](int index) { return seq_constant(page_row, index < last_index ? index : last_index); };
+    struct Group {
+        int page, slot;
+    };
+    struct Groups {
+        Group g[Loader::kGroups];
+    };
+    // what one wave's tiles are apart, and groups of a tile
+    constexpr int kStride = TURN * KT;
+    const Place stride = place_of(kStride);
+    auto advance = [&](Place& p, int index, int slot) {
+        p.index += index;
+        p.slot += slot;
+        if (p.slot >= page_size) {
+            p.slot -= page_size;
+            ++p.index;
+        }
+    };
+    const int mine0 = KEYS ? t0 + (int)wave : t0;
+    Place ahead = place_of(mine0 * KT + load.row);
+    auto look = [&]() {
+        Groups r;
+        Place p = ahead;
 #pragma unroll
         for (int g = 0; g < Loader::kGroups; ++g) {
-            const int key = t * KT + load.row + g * Loader::kGroup;
-            const int rows = page_group(key, klen, Loader::kGroup, page_exists(p.own[g], a.pages));
-            const uint32_t index = fastdiv((uint32_t)key / (uint32_t)kPageRows, plan.by_sub), slot = (uint32_t)key - index * (uint32_t)a.page_size;
-            const uint64_t at = rows > 0 ? page_place((uint32_t)p.own[g], slot, page_bytes, token_bytes) : 0u;
+            r.g[g] = Group{find(p.index), p.slot};
+            if (g + 1 < Loader::kGroups) advance(p, 0, Loader::kGroup);
+        }
+        advance(ahead, stride.index, stride.slot);
+        return r;
+    };
+    int left = klen - mine0 * KT - load.row;  // keys from the next tile's first row on
+    auto issue = [&](const Groups& r, uint32_t buf) {
+#pragma unroll
+        for (int g = 0; g < Loader::kGroups; ++g) {
+            const int rows = page_group(g * Loader::kGroup, left, Loader::kGroup, page_exists(r.g[g].page, a.pages));
+            const uint64_t at = rows > 0 ? page_place((uint32_t)r.g[g].page, (uint32_t)r.g[g].slot, page_bytes, token_bytes) : 0u;
             const uint32_t bytes = page_bytes_of(rows, token_bytes, RB);
             const uint32_t kt = base + buf * 2u * kTile, vt = kt + kTile;
             // Rows that no load fills hold zeros: their weights are zero, and zero times whatever else LDS may hold need not be.
@@ -223,14 +243,30 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
             load.issue(lds_source(kp + at, bytes), kt, g);
             load.issue(lds_source(vp + at, bytes), vt, g);
         }
+        left -= kStride;
+    };
+    // Groups of a tile whose page is none, looked up only where the part has any.
+    auto missing = [&](int t) {
+        uint32_t bad = 0u;
+#pragma unroll
+        for (int j = 0; j < SUB; ++j) bad |= page_exists(find((int)fastdiv((uint32_t)(t * SUB + j), plan.by_sub)), a.pages) ? 0u : 1u << j;
+        return bad;
     };
 
-    const int mine0 = KEYS ? t0 + (int)wave : t0;
-    Pages here = {}, next = {}, after = {};
+    Groups next = {}, after = {};
     if (mine0 < t1) {
-        here = look(mine0);
-        issue(mine0, here, 0u);
-        next = look(mine0 + TURN);
+        next = look();
+        issue(next, 0u);
+        next = look();
+    }
+    bool holes = false;
+    if (t0 < t1) {
+        const int from = place_of(t0 * KT).index, to = place_of(t1 * KT - 1).index;
+        for (int x = from; x <= to && x <= last_index; x += 64) {
+            const int at = x + (int)lane;
+            holes = holes || !page_exists(page_row[at < last_index ? at : last_index], a.pages);
+        }
+        holes = __any(holes);
     }
 
     // the rows of this lane: token, head of the group, whether there is one
@@ -266,6 +302,14 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
         mask0 = to < mask0 ? to : mask0;
     }
 
+    // tiles from here on show the rows of this wave nothing
+    int wave_end = t1;
+    if constexpr (!KEYS) {
+        const int first_row = b.row0 + 32 * MB * (int)wave, last_row = first_row + 32 * MB - 1 < b.rows ? first_row + 32 * MB - 1 : b.rows - 1;
+        const int pos = b.start + (int)fastdiv((uint32_t)last_row, plan.by_group), end = a.causal && pos + 1 < klen ? pos + 1 : klen;
+        wave_end = first_row < b.rows ? (end + KT - 1) / KT : 0;
+    }
+
     f32x16 o[MB][NB];
     float top_at[MB], sum[MB];
 #pragma unroll
@@ -280,26 +324,53 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     auto step = [&](auto parity, int t) {
         const uint32_t B = parity;
         const uint32_t kt = base + B * 2u * kTile, vt = kt + kTile;
-        const uint32_t bad = here.bad;
         lds_loads_done();
         if constexpr (!KEYS) __syncthreads();
-        if (t + TURN < t1) {
-            issue(t + TURN, next, B ^ 1u);
-            if (t + 2 * TURN < t1) after = look(t + 2 * TURN);
+        if (t + TURN < t1) issue(next, B ^ 1u);
+        if (!KEYS && t >= wave_end) {
+            next = look();
+            return;
         }
 
+        // scores
         f32x16 s[KS][MB];
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
+        for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int m = 0; m < MB; ++m) seq_zero(s[k][m]);
+        if constexpr (__is_same(T, SeqF32)) {
 #pragma unroll
-            for (int x = 0; x < NC; ++x) {
-                const u32x4 f = row_reader.read(kt, x, k);
+            for (int k = 0; k < KS; ++k)
 #pragma unroll
-                for (int m = 0; m < MB; ++m) s[k][m] = seq_dot<T>(f, qf[m][x], s[k][m]);
-            }
+                for (int x = 0; x < NC; ++x) {
+                    const u32x4 f = row_reader.read(kt, x, k);
+#pragma unroll
+                    for (int m = 0; m < MB; ++m) s[k][m] = seq_dot<T>(f, qf[m][x], s[k][m]);
+                }
+        } else {
+            u32x4 f[KS][NC];
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int x = 0; x < NC; ++x) f[k][x] = row_reader.read(kt, x, k);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int x = 0; x < NC; ++x)
+#pragma unroll
+                    for (int m = 0; m < MB; ++m) s[k][m] = seq_dot<T>(f[k][x], qf[m][x], s[k][m]);
         }
+        u32x4 v[2][NB];
+        if constexpr (!__is_same(T, SeqF32)) {
+            page_values<T, D>(column_reader, v[0], vt, 0);
+            page_values<T, D>(column_reader, v[1], vt, 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        after = look();
+
+        const uint32_t bad = holes ? missing(t) : 0u;
+        float minus[MB];
 #pragma unroll
         for (int m = 0; m < MB; ++m) {
             if (t >= mask0 || bad != 0u) {
@@ -328,18 +399,36 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
 #pragma unroll
                     for (int r = 0; r < 16; ++r) o[m][x][r] *= f;
             }
-            const float minus = top_at[m] == -__builtin_inff() ? 0.f : -top_at[m];
+            minus[m] = top_at[m] == -__builtin_inff() ? 0.f : -top_at[m];
+        }
+        auto weights = [&](int k) {
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
+            for (int m = 0; m < MB; ++m)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    s[k][m][r] = __builtin_amdgcn_exp2f(fmaf(s[k][m][r], scale, minus));
+                    s[k][m][r] = __builtin_amdgcn_exp2f(fmaf(s[k][m][r], scale, minus[m]));
                     sum[m] += s[k][m][r];
                 }
-        }
+        };
+        if constexpr (__is_same(T, SeqF32)) {
 #pragma unroll
-        for (int k = 0; k < KS; ++k) page_accumulate<T, D, MB>(column_reader, o, vt, k, s[k]);
-        here = next;
+            for (int k = 0; k < KS; ++k) {
+                weights(k);
+                column_reader.accumulate(o[0], vt, k, s[k][0]);
+            }
+        } else {
+            weights(0);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    page_products<T, D, MB>(o, v[h], s[k], h);
+                    if (k + 1 < KS) page_values<T, D>(column_reader, v[h], vt, 2 * (k + 1) + h);
+                }
+                if (k + 1 < KS) weights(k + 1);
+            }
+        }
         next = after;
     };
     if constexpr (KEYS) {
@@ -444,19 +533,35 @@ __global__ void __launch_bounds__(256) page_join_kernel(PageArgs a, PagePlan pla
     const int slot = (int)(turn * kRows + threadIdx.x / kThreads), r = b.row0 + slot, channel = 4 * (int)(threadIdx.x % kThreads);
     if (parts <= 1 || r >= b.rows) return;
     const size_t first = ((size_t)block * a.KV + hk) * plan.splits * ROWS + slot;
-    float top = -__builtin_inff();
-    for (int s = 0; s < parts; ++s) top = fmaxf(top, plan.part_ml[2 * (first + (size_t)s * ROWS)]);
-    float l = 0.f;
+    float top = -__builtin_inff(), l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < parts; ++s) {
-        const size_t part = first + (size_t)s * ROWS;
-        const f32x2 ml = *reinterpret_cast<const f32x2*>(plan.part_ml + 2 * part);
-        if (ml[1] == 0.f) continue;
-        const float f = __builtin_amdgcn_exp2f(ml[0] - top);
-        const f32x4 x = *reinterpret_cast<const f32x4*>(plan.part_o + part * D + channel);
-        l += f * ml[1];
+    // a few parts at a time, all of their loads on the way together; a part without weight was not written, and whatever is in its place is not used
+    constexpr int kAtOnce = 4;
+    for (int s0 = 0; s0 < parts; s0 += kAtOnce) {
+        f32x2 ml[kAtOnce];
+        f32x4 x[kAtOnce];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += f * x[e];
+        for (int s = 0; s < kAtOnce; ++s) {
+            const size_t part = first + (size_t)(s0 + s < parts ? s0 + s : s0) * ROWS;
+            ml[s] = *reinterpret_cast<const f32x2*>(plan.part_ml + 2 * part);
+            x[s] = *reinterpret_cast<const f32x4*>(plan.part_o + part * D + channel);
+        }
+        float to = top;
+#pragma unroll
+        for (int s = 0; s < kAtOnce; ++s) to = fmaxf(to, ml[s][0]);
+        const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - to);
+        top = to;
+        l *= f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= f;
+#pragma unroll
+        for (int s = 0; s < kAtOnce; ++s) {
+            if (s0 + s >= parts || ml[s][1] == 0.f) continue;
+            const float w = __builtin_amdgcn_exp2f(ml[s][0] - top);
+            l += w * ml[s][1];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += w * x[s][e];
+        }
     }
     const int token = (int)fastdiv((uint32_t)r, plan.by_group);
     const size_t row = (size_t)(b.begin + token), head = hk * plan.group + (r - token * plan.group);
@@ -488,55 +593,45 @@ hipError_t launch(const PageArgs& a, const PagePlan& plan, hipStream_t s) {
     return hipGetLastError();
 }
 
-// The forms that a call takes, and how much of each: keys[0] rows, keys[1] keys; blocks 0: not this one.
-struct PagePlans {
-    PagePlan form[2];
-};
-bool page_plans(const PageArgs& a, PagePlans& p) {
+// How a call is laid out, from what the host knows: the waves share out the keys where no sequence has more than a few rows.
+bool page_plan(const PageArgs& a, PagePlan& f) {
     const int size = a.dtype == 0 ? 4 : 2, RB = a.D * size, G = a.H / a.KV, cus = cu_count();
     const long long most_rows = (long long)a.most * G, capacity = (long long)a.width * a.page_size;
-    const bool few = most_rows <= kFewRows, same = (long long)a.N * a.most == a.rows;  // all sequences have few rows; all have the same number
-    for (int keys = 0; keys < 2; ++keys) {
-        PagePlan& f = p.form[keys];
-        f = PagePlan{};
-        if (keys ? !few && same : few) continue;
-        const int KT = page_tile_keys(RB, keys), W = page_waves(RB, keys);
-        f.rows = keys ? 32 : 32 * page_row_blocks(RB, keys) * W;
-        f.group = G;
-        f.only = few || same ? 0 : keys ? -1 : 1;
-        // blocks: a number for each sequence, or as many as the rows fill and one more for each sequence
-        const long long each = keys ? 1 : (most_rows + f.rows - 1) / f.rows, all = (long long)a.rows * G / f.rows + a.N;
-        f.each = each * a.N <= all ? (int)each : 0;
-        const long long blocks = f.each ? each * a.N : all;
-        const double base = (double)blocks * a.KV;
-        if (base * 64.0 * W > 4.0e9 || base * (f.rows / 8.0) * 256.0 > 4.0e9) return false;  // threads of a launch
-        f.blocks = (int)blocks;
-        const long long tiles = (capacity + KT - 1) / KT;
-        f.least = kLeastTiles * (keys ? W : 1);
-        long long splits = (long long)(2.0 * cus / base);
-        if (splits > tiles / f.least) splits = tiles / f.least;
-        if (splits > 64) splits = 64;
-        f.splits = splits < 1 ? 1 : (int)splits;
-        if (f.splits == 1) f.least = 1;
-        f.by_kv = make_fastdiv((uint32_t)a.KV);
-        f.by_splits = make_fastdiv((uint32_t)f.splits);
-        f.by_each = make_fastdiv(f.each > 0 ? (uint32_t)f.each : 1u);
-        f.by_group = make_fastdiv((uint32_t)G);
-        f.by_sub = make_fastdiv((uint32_t)(a.page_size / kPageRows));
-        f.slots = f.splits > 1 ? (size_t)f.blocks * a.KV * f.splits * f.rows : 0;
-    }
+    f = PagePlan{};
+    f.keys = most_rows <= kFewRows;
+    const int KT = page_tile_keys(RB, f.keys), W = page_waves(RB, f.keys);
+    f.rows = f.keys ? 32 : 32 * page_row_blocks(RB, false) * W;
+    f.group = G;
+    // blocks: a number for each sequence, or as many as the rows fill and one more for each sequence
+    const long long each = (most_rows + f.rows - 1) / f.rows, all = (long long)a.rows * G / f.rows + a.N;
+    f.each = each * a.N <= all ? (int)each : 0;
+    const long long blocks = f.each ? each * a.N : all;
+    const double base = (double)blocks * a.KV;
+    if (base * 64.0 * W > 4.0e9 || base * (f.rows / 8.0) * 256.0 > 4.0e9) return false;  // threads of a launch
+    f.blocks = (int)blocks;
+    const long long tiles = (capacity + KT - 1) / KT;
+    f.least = kLeastTiles * (f.keys ? W : 1);
+    long long splits = (long long)(2.0 * cus / base);
+    if (splits > tiles / f.least) splits = tiles / f.least;
+    if (splits > 64) splits = 64;
+    f.splits = splits < 1 ? 1 : (int)splits;
+    if (f.splits == 1) f.least = 1;
+    f.rounds = (int)(blocks * a.KV * f.splits / 256);
+    f.by_kv = make_fastdiv((uint32_t)a.KV);
+    f.by_splits = make_fastdiv((uint32_t)f.splits);
+    f.by_each = make_fastdiv(f.each > 0 ? (uint32_t)f.each : 1u);
+    f.by_group = make_fastdiv((uint32_t)G);
+    f.by_sub = make_fastdiv((uint32_t)(a.page_size / kPageRows));
+    f.slots = f.splits > 1 ? (size_t)f.blocks * a.KV * f.splits * f.rows : 0;
     return true;
 }
 
 template <class T, int D>
-hipError_t launch(const PageArgs& a, const PagePlans& p, hipStream_t s) {
-    hipError_t e = hipSuccess;
-    if (p.form[0].blocks > 0) e = launch<T, D, false>(a, p.form[0], s);
-    if (e == hipSuccess && p.form[1].blocks > 0) e = launch<T, D, true>(a, p.form[1], s);
-    return e;
+hipError_t launch(const PageArgs& a, const PagePlan& p, hipStream_t s) {
+    return p.keys ? launch<T, D, true>(a, p, s) : launch<T, D, false>(a, p, s);
 }
 template <class T>
-hipError_t launch(const PageArgs& a, const PagePlans& p, hipStream_t s) {
+hipError_t launch(const PageArgs& a, const PagePlan& p, hipStream_t s) {
     if (a.D == 32) return launch<T, 32>(a, p, s);
     if (a.D == 64) return launch<T, 64>(a, p, s);
     return launch<T, 128>(a, p, s);
@@ -545,26 +640,20 @@ hipError_t launch(const PageArgs& a, const PagePlans& p, hipStream_t s) {
 }  // namespace
 
 bool page_forward_fits(const PageArgs& a) {
-    PagePlans p;
-    return page_plans(a, p);
+    PagePlan p;
+    return page_plan(a, p);
 }
 
 size_t page_forward_workspace(const PageArgs& a) {
-    PagePlans p;
-    if (!page_plans(a, p)) return 0;
-    return (p.form[0].slots + p.form[1].slots) * (size_t)(a.D + 2) * sizeof(float);
+    PagePlan p;
+    return page_plan(a, p) ? p.slots * (size_t)(a.D + 2) * sizeof(float) : 0;
 }
 
 hipError_t launch_page_forward(const PageArgs& a, void* workspace, hipStream_t s) {
-    PagePlans p;
-    if (!page_plans(a, p)) return hipErrorInvalidValue;
-    float* at = static_cast<float*>(workspace);
-    for (PagePlan& f : p.form) {
-        if (f.slots == 0) continue;
-        f.part_o = at;
-        f.part_ml = at + f.slots * (size_t)a.D;
-        at = f.part_ml + 2 * f.slots;
-    }
+    PagePlan p;
+    if (!page_plan(a, p)) return hipErrorInvalidValue;
+    p.part_o = static_cast<float*>(workspace);
+    p.part_ml = p.part_o ? p.part_o + p.slots * (size_t)a.D : nullptr;
     if (a.dtype == 0) return launch<SeqF32>(a, p, s);
     return a.dtype == 1 ? launch<SeqBf16>(a, p, s) : launch<SeqF16>(a, p, s);
 }

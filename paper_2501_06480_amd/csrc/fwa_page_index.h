@@ -26,14 +26,14 @@ FWA_PAGE_FN int page_keys(int length, int count, int width, int page_size) {
     const int room = width * page_size;
     return length + count < room ? length + count : room;
 }
-FWA_PAGE_FN bool page_exists(int page, long long pages) { return page >= 0 && page < pages; }
+FWA_PAGE_FN bool page_exists(int page, int pages) { return (uint32_t)page < (uint32_t)pages; }
 // Rows of the cache that a group of `group` keys from `key` on has: 0 where the page is none.
 FWA_PAGE_FN int page_group(int key, int keys, int group, bool exists) {
     const int left = keys - key;
     return !exists || left <= 0 ? 0 : (left < group ? left : group);
 }
 // Bytes from the base of a head to a row of a page.
-FWA_PAGE_FN uint64_t page_place(uint32_t page, uint32_t slot, uint64_t page_bytes, uint32_t token_bytes) { return page * page_bytes + (uint64_t)slot * token_bytes; }
+FWA_PAGE_FN uint64_t page_place(uint32_t page, uint32_t slot, uint32_t page_bytes, uint32_t token_bytes) { return (uint64_t)page * page_bytes + (uint64_t)slot * token_bytes; }
 // Bytes from there that the loads of `rows` rows may touch.
 FWA_PAGE_FN uint32_t page_bytes_of(int rows, uint32_t token_bytes, uint32_t row_bytes) { return rows > 0 ? (uint32_t)(rows - 1) * token_bytes + row_bytes : 0u; }
 

@@ -80,6 +80,7 @@ def test_paged_calls_refuse_bad_arguments(lib, call):  # noqa: F811
     assert call(lib, rows=(1 << 24) + 1) == b.FWA_ERR_UNSUPPORTED
     assert call(lib, N=(1 << 20) + 1) == b.FWA_ERR_UNSUPPORTED
     assert call(lib, ts=(1 << 20) + 8, ps=1 << 30) == b.FWA_ERR_UNSUPPORTED
+    assert call(lib, ps=(1 << 29) + 8) == b.FWA_ERR_UNSUPPORTED
     # strides: multiples of 16 bytes that reach no element twice, in any order
     assert call(lib, ts=132) == b.FWA_ERR_ALIGN
     assert call(lib, ps=-16) == b.FWA_ERR_SHAPE

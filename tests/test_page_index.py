@@ -21,7 +21,7 @@ int main() {
     for (int round = 0; round < 4000; ++round) {
         const int size = 16 * pick(1, 8), width = pick(0, 6), pages = pick(0, 7), rows = pick(1, 200), most = pick(0, 220), heads = pick(1, 3);
         const uint32_t row_bytes = 64u << pick(0, 3), token_bytes = row_bytes * (uint32_t)heads, group = pick(0, 1) ? 16 : 8;
-        const uint64_t page_bytes = (uint64_t)token_bytes * size + (pick(0, 1) ? 0 : 16u * pick(0, 5));
+        const uint32_t page_bytes = token_bytes * size + (pick(0, 1) ? 0 : 16u * pick(0, 5));
         int table[8], offsets[2], length;
         for (int& e : table) e = pick(0, 3) ? pick(-1, pages) : odd[pick(0, 7)];
         for (int& e : offsets) e = pick(0, 3) ? pick(-5, rows + 5) : odd[pick(0, 7)];
@@ -54,7 +54,7 @@ int main() {
         }
     }
     // far into a large cache
-    need(page_place(70000u, 255u, 1ull << 31, 1u << 22) == 70000ull * (1ull << 31) + 255ull * (1u << 22), "64 bits");
+    need(page_place(70000u, 255u, 1u << 31, 1u << 22) == 70000ull * (1ull << 31) + 255ull * (1u << 22), "64 bits");
     std::printf("%lld accesses\n", loads);
     return loads > 10000 ? 0 : 1;
 }
