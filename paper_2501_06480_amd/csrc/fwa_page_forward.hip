@@ -15,7 +15,8 @@ namespace {
 // A row's reference moves when a score exceeds it by more than this, as in the attention of whole sequences.
 constexpr float kSlack = 6.f;
 constexpr int kFewRows = 32;  // rows (new tokens times heads of a group) up to which the waves of a workgroup share out the keys
-constexpr int kLeastTiles = 4;  // of a wave, where workgroups share out the keys
+constexpr double kWorth = 8.0;  // tiles of a wave from which an even share of all keys is worth finding
+constexpr int kMostShared = 1024;  // sequences up to which workgroups share out all keys evenly
 
 // How a call is laid out on the device.
 struct PagePlan {
@@ -23,13 +24,20 @@ struct PagePlan {
     int rows;         // of a block
     int group;        // heads of queries per head of keys
     int each;         // blocks of each sequence, 0: as many as it has, found by a search
-    int blocks, splits;
-    int least;        // tiles that a part has at least
-    int rounds;       // workgroups in rounds of 256 go forwards and backwards in turn
+    int blocks;
+    // The keys of a block may be shared out among workgroups: `splits` of them for each block, or `workers` for each head of the keys, evenly over all
+    // sequences.  1 and 0 otherwise.
+    int splits, workers;
+    int alone, least; // tiles up to which a block is not shared out, and that a part has at least
+    int lane_sequences;  // that a lane adds up for the workers
+    unsigned grid;
     FastDiv by_kv, by_splits, by_each, by_group, by_sub;
-    size_t slots;     // blocks * KV * splits * rows: rows of parts
-    float* part_o;    // [block][kv][split][rows][D], not divided by the sum
-    float* part_ml;   // [block][kv][split][rows][2]
+    size_t slots;     // rows of parts: [block][kv][split][rows] or [worker][kv][2][rows]
+    float* part_o;    // [D] each, not divided by the sum
+    float* part_ml;   // [2] each
+    int* joins;       // [block or worker][kv][8]: parts (0: nothing to join), first token, row of the block's first, rows of the sequence, rows of
+                      // parts: the first part's, the second's, from one to the next
+    int joined;       // blocks or workers
 };
 
 // A block of a sequence's rows (token-major: row r is token r / group, head r % group of the group).
@@ -40,7 +48,27 @@ struct PageBlock {
     int kend;           // keys up to this one are seen by a row of the block
 };
 
-// false: nothing to do
+// What is known of a sequence, its blocks left open
+__device__ __forceinline__ void page_sequence(const PageArgs& a, const PagePlan& plan, int n, PageBlock& b) {
+    b.n = n;
+    b.begin = page_offset_of(a, n);
+    const int count = page_count(b.begin, page_offset_of(a, n + 1), a.most);
+    b.rows = count * plan.group;
+    b.start = page_length_of(a, n);
+    b.klen = page_keys(b.start, count, a.width, a.page_size);
+}
+__device__ __forceinline__ void page_place_block(const PageArgs& a, const PagePlan& plan, int within, int rows, PageBlock& b) {
+    b.row0 = within * rows;
+    const int last_row = b.rows - b.row0 < rows ? b.rows - 1 : b.row0 + rows - 1;
+    const int last = b.start + (int)fastdiv((uint32_t)last_row, plan.by_group);
+    b.kend = a.causal && last + 1 < b.klen ? last + 1 : b.klen;
+}
+// Sequence n begins at block offsets[n] group / ROWS + n, so that none shares a block with another and a few blocks have no rows.
+template <int ROWS>
+__device__ __forceinline__ int page_first_block(const PagePlan& plan, int offset, int n) {
+    return (int)((uint32_t)offset * (uint32_t)plan.group / (uint32_t)ROWS) + n;
+}
+// The block with this number; false: it has no rows
 template <int ROWS>
 __device__ __forceinline__ bool page_block(const PageArgs& a, const PagePlan& plan, int block, PageBlock& b) {
     int n, within;
@@ -48,14 +76,12 @@ __device__ __forceinline__ bool page_block(const PageArgs& a, const PagePlan& pl
         n = (int)fastdiv((uint32_t)block, plan.by_each);
         within = block - n * plan.each;
     } else {
-        // Sequence n begins at block offsets[n] group / ROWS + n, so that none shares a block with another and a few blocks have no rows.  The last one
-        // that begins at or in front of this block, 64 candidates at a time.
+        // the last sequence that begins at or in front of this block, 64 candidates at a time
         const int lane = (int)(threadIdx.x & 63u);
         int lo = 0, size = a.N, first = 0;
         for (;;) {
             const int step = (size + 63) / 64, at = lo + lane * step;
-            const int offset = page_offset(a.offsets[at < a.N ? at : a.N - 1], a.rows);
-            const int f = (int)((uint32_t)offset * (uint32_t)plan.group / (uint32_t)ROWS) + at;
+            const int f = page_first_block<ROWS>(plan, page_offset(a.offsets[at < a.N ? at : a.N - 1], a.rows), at);
             const int count = __popcll(__ballot(at < lo + size && f <= block));
             if (count == 0) return false;
             first = __builtin_amdgcn_readlane(f, count - 1);
@@ -66,25 +92,59 @@ __device__ __forceinline__ bool page_block(const PageArgs& a, const PagePlan& pl
         n = lo;
         within = block - first;
     }
-    b.n = n;
-    b.begin = page_offset_of(a, n);
-    const int count = page_count(b.begin, page_offset_of(a, n + 1), a.most);
-    b.rows = count * plan.group;
-    b.row0 = within * ROWS;
-    if (within < 0 || b.row0 >= b.rows) return false;
-    b.start = page_length_of(a, n);
-    b.klen = page_keys(b.start, count, a.width, a.page_size);
-    const int last_row = b.rows - b.row0 < ROWS ? b.rows - 1 : b.row0 + ROWS - 1;
-    const int last = b.start + (int)fastdiv((uint32_t)last_row, plan.by_group);
-    b.kend = a.causal && last + 1 < b.klen ? last + 1 : b.klen;
+    page_sequence(a, plan, n, b);
+    if (within < 0 || (long long)within * ROWS >= b.rows) return false;
+    page_place_block(a, plan, within, ROWS, b);
     return true;
 }
-// Parts of a block's tiles that have any.
-__device__ __forceinline__ int page_parts(const PagePlan& plan, int tiles, int& per) {
-    per = (tiles + plan.splits - 1) / plan.splits;
-    if (per < plan.least) per = plan.least;
-    return (tiles + per - 1) / per;
+
+// Sum of x over the lanes up to this one
+template <int CONTROL, int ROW_MASK>
+__device__ __forceinline__ int page_scan_step(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CONTROL, ROW_MASK, 0xf, false); }
+__device__ __forceinline__ int page_scan(int x) {
+    // from 1, 2, 4 and 8 lanes back within a row of 16; from the last lane of rows 0 and 2 to rows 1 and 3; of row 1 to rows 2 and 3
+    return page_scan_step<0x143, 0xc>(page_scan_step<0x142, 0xa>(page_scan_step<0x118, 0xf>(page_scan_step<0x114, 0xf>(page_scan_step<0x112, 0xf>(page_scan_step<0x111, 0xf>(x))))));
 }
+// A worker's way through its range of the keys of all sequences.
+template <int ROWS, int KT, int TURN>
+struct PageWalk {
+    int lo, per, total, at, units;  // its range; first unit of the sequence that it is in, and its units
+    // to the sequence that its range begins in; false: it has nothing to do.  Each wave finds this by itself, a lane adding up a few sequences.
+    __device__ __forceinline__ bool begin(const PageArgs& a, const PagePlan& plan, int worker, PageBlock& b) {
+        const int first = (int)(threadIdx.x & 63u) * plan.lane_sequences;
+        int mine = 0;
+        for (int n = first; n < first + plan.lane_sequences && n < a.N; ++n) {
+            const int from = page_offset(a.offsets[n], a.rows), count = page_count(from, page_offset(a.offsets[n + 1], a.rows), a.most);
+            mine += page_units(count, (page_keys(page_length(a.lengths[n]), count, a.width, a.page_size) + KT - 1) / KT);
+        }
+        const int upto = page_scan(mine);
+        total = __builtin_amdgcn_readlane(upto, 63);
+        per = page_share(total, plan.workers, plan.least, TURN);
+        if ((long long)worker * per >= total) return false;
+        lo = worker * per;
+        const int owner = (int)__builtin_ctzll(__ballot(upto > lo));
+        at = __builtin_amdgcn_readlane(upto, owner) - __builtin_amdgcn_readlane(mine, owner);
+        units = 0;
+        for (int n = owner * plan.lane_sequences;; ++n) {
+            enter(a, plan, n, b);
+            if (at + units > lo) return true;
+        }
+    }
+    __device__ __forceinline__ void enter(const PageArgs& a, const PagePlan& plan, int n, PageBlock& b) {
+        at += units;
+        page_sequence(a, plan, n, b);
+        page_place_block(a, plan, 0, ROWS, b);
+        units = page_units(b.rows, (b.klen + KT - 1) / KT);
+    }
+    // to the next sequence of its range; false: there is none
+    __device__ __forceinline__ bool next(const PageArgs& a, const PagePlan& plan, PageBlock& b) {
+        if (at + units >= lo + per || at + units >= total) return false;
+        int n = b.n;
+        do enter(a, plan, ++n, b);
+        while (units == 0);
+        return true;
+    }
+};
 
 // 16 rows of a tile of V (the `half`-th), as the operand of a product over them: 32 channels in each of v.
 template <class T, int D>
@@ -154,21 +214,53 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     const uint32_t hi = lane >> 5, c = lane & 31u;
     const uint32_t base = lds_offset(lds) + (KEYS ? wave * 4u * kTile : 0u);
 
-    // workgroup -> head of the keys (neighbours, so that each XCD has few of them), part of the keys, block of rows, the last ones of which have most
-    // keys; rounds of as many workgroups as there are CUs go forwards and backwards in turn, so that a CU's come to one sum
+    // workgroup -> head of the keys (neighbours, so that each XCD has few of them), and a part of a block of rows, the last ones of which have most
+    // keys, or a share of all sequences.  Rounds of as many workgroups as there are CUs go forwards and backwards in turn, so that a CU's come to one sum.
     uint32_t id = blockIdx.x;
     const uint32_t round = id >> 8;
-    if ((round & 1u) && round < (uint32_t)plan.rounds) id = 512u * round + 248u - id + 2u * (id & 7u);
+    if (!KEYS && (round & 1u) && 256u * round + 256u <= gridDim.x) id = 512u * round + 248u - id + 2u * (id & 7u);
     const uint32_t rest = fastdiv(id, plan.by_kv), hk = id - rest * plan.by_kv.d;
     const uint32_t turn = fastdiv(rest, plan.by_splits), split = rest - turn * plan.by_splits.d;
-    const int block = plan.blocks - 1 - (int)turn;
+    const bool walks = KEYS && plan.workers > 0;
+    const uint32_t block = walks ? turn : (uint32_t)plan.blocks - 1u - turn, unit = block * (uint32_t)a.KV + hk;
     PageBlock b;
-    if (!page_block<ROWS>(a, plan, block, b)) return;
+    PageWalk<ROWS, KT, TURN> walk;
+    if (walks ? !walk.begin(a, plan, (int)block, b) : !page_block<ROWS>(a, plan, (int)block, b)) {
+        if (plan.joined > 0 && split == 0 && threadIdx.x == 0) plan.joins[8 * (size_t)unit] = 0;
+        return;
+    }
+    Loader load;
+    load.init(KEYS ? 0u : wave, lane, (uint32_t)(a.token_stride * E));
+    SeqRowReader<RB> row_reader;
+    row_reader.init(hi, c);
+    SeqColumnReader<T, D> column_reader;
+    column_reader.init(hi, c);
+
+    for (;;) {
     const int tiles = (b.kend + KT - 1) / KT;
-    int per;
-    const int parts = page_parts(plan, tiles, per);
-    if ((int)split >= (parts > 0 ? parts : 1)) return;
-    const int t0 = (int)split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
+    int t0 = 0, t1 = tiles, several = 0;
+    uint32_t slot0 = 0u, second = 0u;  // rows of parts: where this one goes, and the second one of a block whose first it is
+    bool whole = true;
+    if (walks) {
+        const PagePart p = page_part(walk.at, walk.units, walk.lo, walk.per);
+        t0 = p.from;
+        t1 = p.to < tiles ? p.to : tiles;
+        whole = p.place < 0;
+        several = p.parts;
+        slot0 = (2u * unit + (p.place > 0 ? 1u : 0u)) * ROWS;
+        second = 2u * (unit + (uint32_t)a.KV) * ROWS;
+    } else if (plan.splits > 1) {
+        int per = (int)fastdiv((uint32_t)(tiles + plan.splits - 1), plan.by_splits);
+        if (per < plan.least) per = plan.least;
+        const int parts = tiles <= plan.alone ? 1 : (tiles + per - 1) / per;
+        if ((int)split >= parts) return;
+        whole = parts == 1;
+        t0 = whole ? 0 : (int)split * per;
+        t1 = whole || t0 + per > tiles ? tiles : t0 + per;
+        several = split == 0 && !whole ? parts : 0;
+        slot0 = (unit * (uint32_t)plan.splits + split) * ROWS;
+        second = slot0 + ROWS;
+    }
 
     const int G = plan.group, klen = b.klen;
     const size_t head_at = (size_t)hk * (size_t)a.head_stride * E;
@@ -177,13 +269,6 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     const uint32_t token_bytes = (uint32_t)(a.token_stride * E);
     const uint32_t page_bytes = (uint32_t)(a.page_stride * E);
     const int32_t* const page_row = a.table + (size_t)b.n * a.width;
-
-    Loader load;
-    load.init(KEYS ? 0u : wave, lane, token_bytes);
-    SeqRowReader<RB> row_reader;
-    row_reader.init(hi, c);
-    SeqColumnReader<T, D> column_reader;
-    column_reader.init(hi, c);
 
     // Pages are looked up two tiles ahead of their use, so that nothing waits for the scalar loads, and in steps from group to group, without a
     // division: a group's place is an entry of the table and a row of that page.
@@ -350,21 +435,21 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
         } else {
             u32x4 f[KS][NC];
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
+            for (int x = 0; x < NC; ++x)
 #pragma unroll
-                for (int x = 0; x < NC; ++x) f[k][x] = row_reader.read(kt, x, k);
+                for (int k = 0; k < KS; ++k) f[k][x] = row_reader.read(kt, x, k);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
+            for (int x = 0; x < NC; ++x)
 #pragma unroll
-                for (int x = 0; x < NC; ++x)
+                for (int k = 0; k < KS; ++k)
 #pragma unroll
                     for (int m = 0; m < MB; ++m) s[k][m] = seq_dot<T>(f[k][x], qf[m][x], s[k][m]);
         }
-        u32x4 v[2][NB];
+        u32x4 v[2 * KS][NB];
         if constexpr (!__is_same(T, SeqF32)) {
-            page_values<T, D>(column_reader, v[0], vt, 0);
-            page_values<T, D>(column_reader, v[1], vt, 1);
+#pragma unroll
+            for (int h = 0; h < 2 * KS; ++h) page_values<T, D>(column_reader, v[h], vt, h);
         }
         __builtin_amdgcn_sched_barrier(0);
         after = look();
@@ -422,10 +507,7 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    page_products<T, D, MB>(o, v[h], s[k], h);
-                    if (k + 1 < KS) page_values<T, D>(column_reader, v[h], vt, 2 * (k + 1) + h);
-                }
+                for (int h = 0; h < 2; ++h) page_products<T, D, MB>(o, v[2 * k + h], s[k], h);
                 if (k + 1 < KS) weights(k + 1);
             }
         }
@@ -469,7 +551,7 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
                         f32x4{o[0][x][4 * q] * mine, o[0][x][4 * q + 1] * mine, o[0][x][4 * q + 2] * mine, o[0][x][4 * q + 3] * mine};
         }
         __syncthreads();
-        if (wave != W - 1) return;
+        if (wave == W - 1) {
 #pragma unroll
         for (int x = 0; x < NB; ++x)
 #pragma unroll
@@ -486,13 +568,14 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
                 }
         top_at[0] = top;
         sum[0] = total;
+        }
     }
 #pragma unroll
     for (int m = 0; m < MB; ++m) {
-        if (!exists[m]) continue;
+        if (!exists[m] || (KEYS && wave != W - 1)) continue;
         const float l = sum[m];
-        if (parts > 1) {
-            const size_t slot = (((size_t)block * a.KV + hk) * plan.splits + split) * ROWS + (KEYS ? 0 : 32 * (MB * wave + m)) + c;
+        if (!whole) {
+            const size_t slot = (size_t)slot0 + (KEYS ? 0 : 32 * (MB * wave + m)) + c;
             float* const to = plan.part_o + slot * D;
             if (l != 0.f)  // nothing reads a part without weight
 #pragma unroll
@@ -518,31 +601,39 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
             }
         if (a.stats && hi == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * (row * a.H + head)) = f32x2{any ? top_at[m] : -__builtin_inff(), any ? log2f(l) : 0.f};
     }
+    const bool more = walks && walk.next(a, plan, b);
+    if (!more) {  // a sequence of several parts that a worker begins is its last one
+        if (plan.joined > 0 && split == 0 && threadIdx.x == 0) {
+            int* const to = plan.joins + 8 * (size_t)unit;
+            *reinterpret_cast<i32x4*>(to) = i32x4{several, b.begin, b.row0, b.rows};
+            *reinterpret_cast<i32x4*>(to + 4) = i32x4{(int)slot0, (int)second, walks ? 2 * a.KV * ROWS : ROWS, 0};
+        }
+        return;
+    }
+    __syncthreads();  // the tiles and sums in LDS are done with
+    }
 }
 
 // Joins the parts of blocks whose keys are shared out: a thread has four channels of a row.
-template <class T, int D, int ROWS, int KT>
+template <class T, int D, int ROWS>
 __global__ void __launch_bounds__(256) page_join_kernel(PageArgs a, PagePlan plan) {
     constexpr int E = SeqSize<T>::value, kThreads = D / 4, kRows = 256 / kThreads, kTurns = ROWS / kRows;
-    const uint32_t unit = blockIdx.x / kTurns, turn = blockIdx.x - unit * kTurns;
-    const uint32_t block = fastdiv(unit, plan.by_kv), hk = unit - block * plan.by_kv.d;
-    PageBlock b;
-    if (!page_block<ROWS>(a, plan, (int)block, b)) return;
-    int per;
-    const int parts = page_parts(plan, (b.kend + KT - 1) / KT, per);
-    const int slot = (int)(turn * kRows + threadIdx.x / kThreads), r = b.row0 + slot, channel = 4 * (int)(threadIdx.x % kThreads);
-    if (parts <= 1 || r >= b.rows) return;
-    const size_t first = ((size_t)block * a.KV + hk) * plan.splits * ROWS + slot;
+    const uint32_t unit = blockIdx.x / kTurns, turn = blockIdx.x - unit * kTurns, hk = unit - fastdiv(unit, plan.by_kv) * plan.by_kv.d;
+    const i32x4 known = *reinterpret_cast<const i32x4*>(plan.joins + 8 * (size_t)unit), rows = *reinterpret_cast<const i32x4*>(plan.joins + 8 * (size_t)unit + 4);
+    const int parts = known[0], slot = (int)(turn * kRows + threadIdx.x / kThreads), r = known[2] + slot, channel = 4 * (int)(threadIdx.x % kThreads);
+    if (parts == 0 || r >= known[3]) return;
+    const size_t first = (size_t)(uint32_t)rows[0] + slot, second = (size_t)(uint32_t)rows[1] + slot, step = (size_t)(uint32_t)rows[2];
     float top = -__builtin_inff(), l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     // a few parts at a time, all of their loads on the way together; a part without weight was not written, and whatever is in its place is not used
-    constexpr int kAtOnce = 4;
+    constexpr int kAtOnce = 8;
     for (int s0 = 0; s0 < parts; s0 += kAtOnce) {
         f32x2 ml[kAtOnce];
         f32x4 x[kAtOnce];
 #pragma unroll
         for (int s = 0; s < kAtOnce; ++s) {
-            const size_t part = first + (size_t)(s0 + s < parts ? s0 + s : s0) * ROWS;
+            const int p = s0 + s < parts ? s0 + s : s0;
+            const size_t part = p == 0 ? first : second + (size_t)(p - 1) * step;
             ml[s] = *reinterpret_cast<const f32x2*>(plan.part_ml + 2 * part);
             x[s] = *reinterpret_cast<const f32x4*>(plan.part_o + part * D + channel);
         }
@@ -564,7 +655,7 @@ __global__ void __launch_bounds__(256) page_join_kernel(PageArgs a, PagePlan pla
         }
     }
     const int token = (int)fastdiv((uint32_t)r, plan.by_group);
-    const size_t row = (size_t)(b.begin + token), head = hk * plan.group + (r - token * plan.group);
+    const size_t row = (size_t)(known[1] + token), head = hk * plan.group + (r - token * plan.group);
     const bool any = l != 0.f;
     const float f = any ? 1.f / l : 0.f;
     char* const to = static_cast<char*>(a.o) + (row * a.ldo + head * D) * E;
@@ -572,7 +663,7 @@ __global__ void __launch_bounds__(256) page_join_kernel(PageArgs a, PagePlan pla
     if (a.stats && channel == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * (row * a.H + head)) = f32x2{any ? top : -__builtin_inff(), any ? log2f(l) : 0.f};
 }
 
-// Tile sizes and waves of the two forms.
+// Tiles and waves of the two forms.
 constexpr int page_tile_keys(int row_bytes, bool keys) { return row_bytes >= 512 || keys ? 32 : 64; }
 constexpr int page_waves(int row_bytes, bool keys) { return keys ? seq_keys_waves(row_bytes) : 4; }
 constexpr int page_row_blocks(int, bool) { return 1; }
@@ -585,15 +676,17 @@ hipError_t launch(const PageArgs& a, const PagePlan& plan, hipStream_t s) {
     auto* const kernel = &page_forward_kernel<T, D, W, KT, MB, KEYS, page_occupancy(RB, KEYS)>;
     hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)plan.blocks * (unsigned)a.KV * (unsigned)plan.splits), dim3(64 * W), lds, s, a, plan);
+    hipLaunchKernelGGL(kernel, dim3(plan.grid), dim3(64 * W), lds, s, a, plan);
     e = hipGetLastError();
-    if (e != hipSuccess || plan.splits == 1) return e;
+    if (e != hipSuccess || plan.joined == 0) return e;
     constexpr unsigned turns = ROWS / (256 / (D / 4));
-    hipLaunchKernelGGL((page_join_kernel<T, D, ROWS, KT>), dim3((unsigned)plan.blocks * (unsigned)a.KV * turns), dim3(256), 0, s, a, plan);
+    hipLaunchKernelGGL((page_join_kernel<T, D, ROWS>), dim3((unsigned)plan.joined * (unsigned)a.KV * turns), dim3(256), 0, s, a, plan);
     return hipGetLastError();
 }
 
-// How a call is laid out, from what the host knows: the waves share out the keys where no sequence has more than a few rows.
+// How a call is laid out, from what the host knows: the waves share out the keys where no sequence has more than a few rows.  Where there are too few
+// blocks for the device, its workgroups share out the keys besides, and a second launch joins the parts, but for caches that are too short to
+// be worth that (the join takes about as long as `alone` tiles).
 bool page_plan(const PageArgs& a, PagePlan& f) {
     const int size = a.dtype == 0 ? 4 : 2, RB = a.D * size, G = a.H / a.KV, cus = cu_count();
     const long long most_rows = (long long)a.most * G, capacity = (long long)a.width * a.page_size;
@@ -607,23 +700,35 @@ bool page_plan(const PageArgs& a, PagePlan& f) {
     f.each = each * a.N <= all ? (int)each : 0;
     const long long blocks = f.each ? each * a.N : all;
     const double base = (double)blocks * a.KV;
-    if (base * 64.0 * W > 4.0e9 || base * (f.rows / 8.0) * 256.0 > 4.0e9) return false;  // threads of a launch
+    if (base * 64.0 * W > 4.0e9) return false;  // threads of a launch
     f.blocks = (int)blocks;
+    f.splits = 1;
     const long long tiles = (capacity + KT - 1) / KT;
-    f.least = kLeastTiles * (f.keys ? W : 1);
-    long long splits = (long long)(2.0 * cus / base);
-    if (splits > tiles / f.least) splits = tiles / f.least;
-    if (splits > 64) splits = 64;
-    f.splits = splits < 1 ? 1 : (int)splits;
-    if (f.splits == 1) f.least = 1;
-    f.rounds = (int)(blocks * a.KV * f.splits / 256);
+    f.alone = f.keys ? 6 * W : a.dtype == 0 ? 1 : 4;
+    f.least = f.keys ? 2 * W : a.dtype == 0 ? 1 : 2;
+    if (tiles > f.alone) {
+        const bool same = (long long)a.N * a.most == a.rows;  // all sequences have the same number of new tokens
+        if (f.keys && a.N <= kMostShared && base < 4.0 * cus && 2 * cus / a.KV >= 2 && base * (double)tiles >= kWorth * W * 2.0 * cus && (double)a.N * (double)tiles < 1.0e9) {
+            f.workers = 2 * cus / a.KV;
+            f.lane_sequences = (a.N + 63) / 64;
+        } else {
+            long long splits = (long long)((f.keys || !same ? 4.0 : 2.0) * cus / base);
+            if (splits > tiles / f.least) splits = tiles / f.least;
+            f.splits = splits < 1 ? 1 : splits > 64 ? 64 : (int)splits;
+        }
+    }
+    f.joined = f.workers > 0 ? f.workers : f.splits > 1 ? f.blocks : 0;
+    f.grid = (unsigned)(f.workers > 0 ? f.workers : f.blocks * f.splits) * (unsigned)a.KV;
+    f.slots = f.workers > 0 ? (size_t)f.workers * a.KV * 2 * f.rows : f.splits > 1 ? (size_t)f.blocks * a.KV * f.splits * f.rows : 0;
     f.by_kv = make_fastdiv((uint32_t)a.KV);
     f.by_splits = make_fastdiv((uint32_t)f.splits);
     f.by_each = make_fastdiv(f.each > 0 ? (uint32_t)f.each : 1u);
     f.by_group = make_fastdiv((uint32_t)G);
     f.by_sub = make_fastdiv((uint32_t)(a.page_size / kPageRows));
-    f.slots = f.splits > 1 ? (size_t)f.blocks * a.KV * f.splits * f.rows : 0;
     return true;
+}
+size_t page_workspace(const PagePlan& p, const PageArgs& a) {
+    return p.slots * (size_t)(a.D + 2) * sizeof(float) + (size_t)p.joined * a.KV * 8 * sizeof(int);
 }
 
 template <class T, int D>
@@ -646,14 +751,17 @@ bool page_forward_fits(const PageArgs& a) {
 
 size_t page_forward_workspace(const PageArgs& a) {
     PagePlan p;
-    return page_plan(a, p) ? p.slots * (size_t)(a.D + 2) * sizeof(float) : 0;
+    return page_plan(a, p) ? page_workspace(p, a) : 0;
 }
 
 hipError_t launch_page_forward(const PageArgs& a, void* workspace, hipStream_t s) {
     PagePlan p;
     if (!page_plan(a, p)) return hipErrorInvalidValue;
-    p.part_o = static_cast<float*>(workspace);
-    p.part_ml = p.part_o ? p.part_o + p.slots * (size_t)a.D : nullptr;
+    if (p.joined > 0) {
+        p.part_o = static_cast<float*>(workspace);
+        p.part_ml = p.part_o + p.slots * (size_t)a.D;
+        p.joins = reinterpret_cast<int*>(p.part_ml + 2 * p.slots);
+    }
     if (a.dtype == 0) return launch<SeqF32>(a, p, s);
     return a.dtype == 1 ? launch<SeqBf16>(a, p, s) : launch<SeqF16>(a, p, s);
 }

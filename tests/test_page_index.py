@@ -67,3 +67,77 @@ def test_no_table_leads_outside(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True, env={**os.environ, "UBSAN_OPTIONS": "print_stacktrace=1"})
     assert r.returncode == 0, r.stdout + r.stderr
+
+
+SHARE = r'''
+#include "fwa_page_index.h"
+#include <cstdio>
+#include <cstdlib>
+#include <map>
+#include <random>
+#include <vector>
+using namespace fwa;
+static void need(bool ok, const char* what) { if (!ok) { std::printf("FAILED %s\n", what); std::exit(1); } }
+int main() {
+    std::mt19937 g(2);
+    auto pick = [&](int lo, int hi) { return (int)(lo + (long long)(g() % (uint64_t)((long long)hi - lo + 1))); };
+    long long parts_seen = 0;
+    for (int round = 0; round < 20000; ++round) {
+        const int N = pick(1, 20), workers = pick(1, 300), least = pick(1, 16), turn = 1 << pick(0, 2), most = pick(0, 1) ? 20 : 2000;
+        std::vector<int> units, starts;
+        int total = 0;
+        for (int n = 0; n < N; ++n) {
+            const int rows = pick(0, 3), tiles = pick(0, 5) ? pick(0, most) : 0;
+            units.push_back(page_units(rows, tiles));
+            need(units[n] == (rows == 0 ? 0 : tiles == 0 ? 1 : tiles), "units");
+            starts.push_back(total);
+            total += units[n];
+        }
+        if (total == 0) continue;
+        const int per = page_share(total, workers, least, turn);
+        need(per >= least && per % turn == 0 && (long long)per * workers >= total, "share");
+        struct Part { int worker, place, from, to; };
+        std::vector<std::vector<Part>> got(N);
+        std::map<std::pair<int, int>, int> places;
+        std::vector<std::vector<int>> joins(N);  // worker, place, parts
+        for (int w = 0; w < workers && (long long)w * per < total; ++w) {
+            int begins = 0;
+            for (int n = 0; n < N; ++n) {
+                if (units[n] == 0 || starts[n] + units[n] <= w * per || starts[n] >= w * per + per) continue;
+                const PagePart p = page_part(starts[n], units[n], w * per, per);
+                need(p.from >= 0 && p.from < p.to && p.to <= units[n], "units of a part");
+                if (p.place < 0) need(p.from == 0 && p.to == units[n] && p.parts == 0, "all of it");
+                else need(++places[{w, p.place}] == 1, "a place has one part");
+                if (p.parts) {
+                    need(p.place >= 0 && p.from == 0 && ++begins == 1, "one block of several is begun");
+                    need(n == N - 1 || starts[n] + units[n] >= w * per + per, "the last of the range");
+                    joins[n] = {w, p.place, p.parts};
+                }
+                got[n].push_back({w, p.place, p.from, p.to});
+            }
+        }
+        for (int n = 0; n < N; ++n) {
+            int at = 0;
+            for (size_t k = 0; k < got[n].size(); ++k) {
+                need(got[n][k].from == at, "parts one behind the other");
+                at = got[n][k].to;
+                if (!joins[n].empty()) need(got[n][k].worker == joins[n][0] + (int)k && got[n][k].place == (k == 0 ? joins[n][1] : 0), "a part where the join looks for it");
+            }
+            need(at == units[n], "all units");
+            need(joins[n].empty() ? got[n].size() <= 1 : (int)got[n].size() == joins[n][2], "as many parts as the join reads");
+            parts_seen += got[n].size();
+        }
+    }
+    std::printf("%lld parts\n", parts_seen);
+    return parts_seen > 10000 ? 0 : 1;
+}
+'''
+
+
+def test_shares_cover_every_unit_once(tmp_path):
+    """The ranges of all workers over sequences of all kinds: every unit in one part, every part where the join looks for it, no place used twice."""
+    src, exe = tmp_path / "share.cpp", tmp_path / "share"
+    src.write_text(SHARE)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout + r.stderr
