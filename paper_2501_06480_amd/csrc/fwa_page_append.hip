@@ -7,31 +7,31 @@ namespace fwa {
 namespace {
 
 struct AppendPlan {
-    FastDiv by_each, by_units, by_pairs, by_page;
+    FastDiv by_each, by_units, by_page;
     int heads, units, rows;  // heads of queries, keys and values together; units of a head; rows in LDS
-    int sample;              // one of so many offsets is looked at first
+    int sample, samples;     // one of so many offsets is looked at first, and how many there are of these
     long long total;
 };
 
 // What a workgroup knows of a row that its units touch.
 struct AppendRow {
-    int place;        // in the sequence; the default position
-    uint32_t page;    // of the cache, ~0: nowhere
+    int place;        // in the sequence; the default position.  -1: a row of no sequence
+    int sequence;     // and then, in its place, the entry of the table
 };
+constexpr uint32_t kNowhere = 0xffffffffu;
 
 // Units as in the rotary kernel, a token's heads of queries, keys and values one behind the other, with their vectors on the way while the
-// places are looked up: sequence (a search in a sample of the offsets in LDS), length, page: three loads one behind the other.
-template <class T, int V>
-__global__ void __launch_bounds__(256) page_append_kernel(PageArgs a, AppendPlan plan) {
-    constexpr int E = SeqSize<T>::value, U = kRotaryUnits / 256;
+// places are looked up: sequence (a search in a sample of the offsets in LDS), length, page, three loads one behind the other, the last of them beside the cosines.
+template <class T, int V, int UNITS, int THREADS>
+__global__ void __launch_bounds__(THREADS) page_append_kernel(PageArgs a, AppendPlan plan) {
+    constexpr int E = SeqSize<T>::value, U = UNITS / THREADS;
     extern __shared__ __attribute__((aligned(16))) f32x2 turns[];
-    __shared__ int samples[256];
+    __shared__ int samples[THREADS];
     AppendRow* const known = reinterpret_cast<AppendRow*>(turns + (size_t)plan.rows * a.pairs);
-    const uint32_t u0 = blockIdx.x * (uint32_t)kRotaryUnits, end = plan.total - u0 < kRotaryUnits ? (uint32_t)plan.total : u0 + kRotaryUnits;
+    const uint32_t u0 = blockIdx.x * (uint32_t)UNITS, end = plan.total - u0 < UNITS ? (uint32_t)plan.total : u0 + UNITS;
     const uint32_t row0 = fastdiv(u0, plan.by_each), rows = fastdiv(end - 1u, plan.by_each) - row0 + 1u;
     {
-        const long long n = (long long)threadIdx.x * plan.sample;
-        samples[threadIdx.x] = n < a.N ? a.offsets[n] : 0x7fffffff;
+        if ((int)threadIdx.x < plan.samples) samples[threadIdx.x] = a.offsets[threadIdx.x * (uint32_t)plan.sample];
     }
     RotaryVector<T, V> x[U], y[U];
     RotaryUnit at[U];
@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(256) page_append_kernel(PageArgs a, AppendPlan
     bool on[U], turned[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        const uint32_t u = u0 + 256u * i + threadIdx.x;
+        const uint32_t u = u0 + (uint32_t)(THREADS * i) + threadIdx.x;
         on[i] = u < end;
         if (!on[i]) continue;
         row[i] = fastdiv(u, plan.by_each);
@@ -57,41 +57,40 @@ __global__ void __launch_bounds__(256) page_append_kernel(PageArgs a, AppendPlan
         if (at[i].both) y[i].load(from + (size_t)at[i].second * E);
     }
     __syncthreads();
-    for (uint32_t r = threadIdx.x; r < rows; r += 256u) {
+    for (uint32_t r = threadIdx.x; r < rows; r += THREADS) {
         const int t = (int)(row0 + r);
-        AppendRow k = {-1, ~0u};
         // the last sequence that begins at or in front of t: of the samples, then of the offsets behind it
-        int lo = 0, hi = 256;
+        int lo = 0, hi = plan.samples;
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
             if (samples[mid] <= t) lo = mid;
             else hi = mid;
         }
-        long long n = (long long)lo * plan.sample, to = n + plan.sample < a.N ? n + plan.sample : a.N;
+        int n = lo * plan.sample, to = n + plan.sample < a.N ? n + plan.sample : a.N;
         while (to - n > 1) {
-            const long long mid = (n + to) / 2;
+            const int mid = (n + to) / 2;
             if (a.offsets[mid] <= t) n = mid;
             else to = mid;
         }
-        const int begin = page_offset_of(a, (int)n), finish = a.offsets[n + 1];
-        if (a.offsets[n] <= t && t < finish) {
-            k.place = page_length_of(a, (int)n) + (t - begin);
-            const uint32_t index = fastdiv((uint32_t)k.place, plan.by_page);
-            if (index < (uint32_t)a.width) {
-                const int page = a.table[(size_t)n * a.width + index];
-                if (page_exists(page, a.pages)) k.page = (uint32_t)page;
-            }
-        }
-        known[r] = k;
+        const int begin = a.offsets[n], finish = a.offsets[n + 1], length = a.lengths[n];
+        known[r] = AppendRow{begin <= t && t < finish ? page_length(length) + (t - page_offset(begin, a.rows)) : -1, n};
     }
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < rows * (uint32_t)a.pairs; e += 256u) {
-        const uint32_t r = fastdiv(e, plan.by_pairs), p = e - r * (uint32_t)a.pairs;
-        const int place = known[r].place;
-        if (place < 0) continue;  // behind the last sequence
-        turns[e] = a.positions ? rotary_pair(a.positions + (size_t)(row0 + r) * a.axes, a.axes, a.frequencies, a.axis_of, (int)p, false)
-                               : rotary_pair(&place, 1, a.frequencies, a.axis_of, (int)p, false);
-    }
+    // the page of a row is on its way while the cosines are formed
+    uint32_t page = kNowhere;
+    const bool looks = threadIdx.x < rows;
+    auto look = [&](uint32_t r) {
+        const AppendRow k = known[r];
+        const uint32_t index = k.place < 0 ? ~0u : fastdiv((uint32_t)k.place, plan.by_page);
+        return index < (uint32_t)a.width ? (uint32_t)a.table[(size_t)k.sequence * a.width + index] : kNowhere;
+    };
+    if (looks) page = look(threadIdx.x);
+    rotary_turns<THREADS>(turns, rows, a.pairs, a.axes, a.frequencies, a.axis_of, false, [&](uint32_t r, uint32_t axis) {
+        return a.positions ? a.positions[(size_t)(row0 + r) * a.axes + axis] : known[r].place;
+    });
+    __syncthreads();
+    if (looks) known[threadIdx.x].sequence = (int)page;
+    for (uint32_t r = threadIdx.x + THREADS; r < rows; r += THREADS) known[r].sequence = (int)look(r);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -103,24 +102,31 @@ __global__ void __launch_bounds__(256) page_append_kernel(PageArgs a, AppendPlan
         if (head[i] < (uint32_t)a.H) {
             to = static_cast<char*>(a.o) + ((size_t)row[i] * a.ldo + (size_t)head[i] * a.D) * E;
         } else {
-            if (k.page == ~0u) continue;
+            if (!page_exists(k.sequence, a.pages)) continue;
             const bool key = head[i] < (uint32_t)(a.H + a.KV);
             const uint32_t h = head[i] - a.H - (key ? 0 : a.KV), slot = (uint32_t)k.place - fastdiv((uint32_t)k.place, plan.by_page) * plan.by_page.d;
-            to = static_cast<char*>(key ? a.k : a.v) + (size_t)h * a.head_stride * E + page_place(k.page, slot, (uint32_t)(a.page_stride * E), (uint32_t)(a.token_stride * E));
+            to = static_cast<char*>(key ? a.k : a.v) + (size_t)h * a.head_stride * E + page_place((uint32_t)k.sequence, slot, (uint32_t)(a.page_stride * E), (uint32_t)(a.token_stride * E));
         }
         x[i].store(to + (size_t)at[i].first * E);
         if (at[i].both) y[i].store(to + (size_t)at[i].second * E);
     }
 }
 
-template <class T, int V>
-hipError_t launch(const PageArgs& a, const AppendPlan& plan, hipStream_t s) {
+template <class T, int V, int UNITS, int THREADS>
+hipError_t launch(const PageArgs& a, AppendPlan plan, hipStream_t s) {
+    plan.rows = rotary_rows((long long)plan.heads * plan.units, UNITS);
+    plan.sample = (a.N + THREADS - 1) / THREADS;
+    plan.samples = (a.N + plan.sample - 1) / plan.sample;
     const size_t lds = (sizeof(f32x2) * a.pairs + sizeof(AppendRow)) * (size_t)plan.rows;
-    auto* const kernel = &page_append_kernel<T, V>;
+    auto* const kernel = &page_append_kernel<T, V, UNITS, THREADS>;
     const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((plan.total + kRotaryUnits - 1) / kRotaryUnits)), dim3(256), lds, s, a, plan);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((plan.total + UNITS - 1) / UNITS)), dim3(THREADS), lds, s, a, plan);
     return hipGetLastError();
+}
+template <class T, int V>
+hipError_t launch(const PageArgs& a, const AppendPlan& plan, hipStream_t s) {
+    return rotary_small(plan.total) ? launch<T, V, RotaryShape::kSmall, RotaryShape::kSmall>(a, plan, s) : launch<T, V, RotaryShape::kLarge, 256>(a, plan, s);
 }
 
 }  // namespace
@@ -136,11 +142,8 @@ hipError_t launch_page_append(const PageArgs& a, hipStream_t s) {
     plan.units = rotary_units(a.D, a.pairs, V);
     const long long each = (long long)plan.heads * plan.units;
     plan.total = a.rows * each;
-    plan.rows = rotary_rows(each);
-    plan.sample = (a.N + 255) / 256;
     plan.by_each = make_fastdiv((uint32_t)each);
     plan.by_units = make_fastdiv((uint32_t)plan.units);
-    plan.by_pairs = make_fastdiv(a.pairs > 0 ? (uint32_t)a.pairs : 1u);
     plan.by_page = make_fastdiv((uint32_t)a.page_size);
     if (a.dtype == 0) return V == 4 ? launch<SeqF32, 4>(a, plan, s) : launch<SeqF32, 1>(a, plan, s);
     if (a.dtype == 1) return V == 8 ? launch<SeqBf16, 8>(a, plan, s) : V == 4 ? launch<SeqBf16, 4>(a, plan, s) : launch<SeqBf16, 1>(a, plan, s);

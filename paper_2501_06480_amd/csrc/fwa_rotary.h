@@ -69,13 +69,6 @@ __device__ __forceinline__ f32x2 rotary_turn(int position, float frequency, bool
     sincospif(2.f * (float)turns, &s, &c);
     return f32x2{c, inverse ? -s : s};
 }
-// that of pair p of a row with the given positions; an axis outside the row's leaves the pair as it is
-__device__ __forceinline__ f32x2 rotary_pair(const int32_t* positions, int axes, const float* frequencies, const int32_t* axis_of, int p, bool inverse) {
-    const uint32_t axis = axis_of ? (uint32_t)axis_of[p] : 0u;
-    if (axis >= (uint32_t)axes) return f32x2{1.f, 0.f};
-    return rotary_turn(positions[axis], frequencies[p], inverse);
-}
-
 // Where the two vectors of unit `u` of a head begin, in channels; the second may not exist for channels that are copied.
 struct RotaryUnit {
     int first, second;
@@ -134,8 +127,40 @@ inline int rotary_vector(int dtype, int d, int pairs) {
 // units of a head
 inline int rotary_units(int d, int pairs, int V) { return pairs / V + (d - 2 * pairs + 2 * V - 1) / (2 * V); }
 
-constexpr int kRotaryUnits = 512;  // of a workgroup of 256 threads
+// Units and threads of a workgroup.  Large calls have two units a thread, small ones 128 threads with one each: more workgroups, and fewer cosines for each (64
+// windows of 49 rows of 3 heads of 32: 5.2 us with 512 units a workgroup, MEASURE with 128).
+struct RotaryShape {
+    static constexpr int kLarge = 512, kSmall = 128;
+};
+inline bool rotary_small(long long total) { return total <= 256 * RotaryShape::kLarge; }
 // Rows that a workgroup's units may touch, of `each` units a row.
-inline int rotary_rows(long long each) { return (int)((kRotaryUnits - 1) / each) + 2; }
+inline int rotary_rows(long long each, int units) { return (int)((units - 1) / each) + 2; }
+
+// Cosines and sines of `rows` rows into LDS, pairs of a row one behind the other.  A thread has one pair of every so many rows, so that its axis and frequency are loaded
+// once, and the positions of four rows at a time.  position(r, axis) is that of row r on an axis of the row's.
+template <int THREADS, class Position>
+__device__ __forceinline__ void rotary_turns(f32x2* turns, uint32_t rows, int pairs, int axes, const float* frequencies, const int32_t* axis_of, bool inverse, Position position) {
+    uint32_t wide = 1u;  // threads for a row's pairs: a power of two
+    while (wide < (uint32_t)pairs && wide < THREADS) wide *= 2u;
+    const uint32_t first = threadIdx.x & (wide - 1u), step = THREADS / wide;
+    for (uint32_t p = first; p < (uint32_t)pairs; p += wide) {
+        const uint32_t axis = axis_of ? (uint32_t)axis_of[p] : 0u;
+        const float f = frequencies[p];
+        const bool turned = axis < (uint32_t)axes;
+        for (uint32_t r0 = threadIdx.x / wide; r0 < rows; r0 += 4u * step) {
+            int at[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t r = r0 + k * step;
+                at[k] = turned && r < rows ? position(r, axis) : 0;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t r = r0 + k * step;
+                if (r < rows) turns[r * (uint32_t)pairs + p] = turned ? rotary_turn(at[k], f, inverse) : f32x2{1.f, 0.f};
+            }
+        }
+    }
+}
 
 }  // namespace fwa

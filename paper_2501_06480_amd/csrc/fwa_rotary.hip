@@ -5,18 +5,18 @@ namespace fwa {
 namespace {
 
 struct RotaryPlan {
-    FastDiv by_each, by_units, by_pairs, by_period;
+    FastDiv by_each, by_units, by_period;
     int units, rows;      // of a head; of cosines and sines in LDS
     long long total;
 };
 
-// A workgroup has 512 units one behind the other, whatever rows they belong to: memory is read and written in order, and each thread has its four vectors on the
+// A workgroup has its units one behind the other, whatever rows they belong to: memory is read and written in order, and each thread has its four vectors on the
 // way while the workgroup forms the cosines and sines of the rows they touch, each once.
-template <class T, int V>
-__global__ void __launch_bounds__(256) rotary_kernel(RotaryArgs a, RotaryPlan plan) {
-    constexpr int E = SeqSize<T>::value, U = kRotaryUnits / 256;
+template <class T, int V, int UNITS, int THREADS>
+__global__ void __launch_bounds__(THREADS) rotary_kernel(RotaryArgs a, RotaryPlan plan) {
+    constexpr int E = SeqSize<T>::value, U = UNITS / THREADS;
     extern __shared__ __attribute__((aligned(16))) f32x2 turns[];
-    const uint32_t u0 = blockIdx.x * (uint32_t)kRotaryUnits, end = plan.total - u0 < kRotaryUnits ? (uint32_t)plan.total : u0 + kRotaryUnits;
+    const uint32_t u0 = blockIdx.x * (uint32_t)UNITS, end = plan.total - u0 < UNITS ? (uint32_t)plan.total : u0 + UNITS;
     const uint32_t row0 = fastdiv(u0, plan.by_each), rows = fastdiv(end - 1u, plan.by_each) - row0 + 1u;
     RotaryVector<T, V> x[U], y[U];
     RotaryUnit at[U];
@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryArgs a, RotaryPlan pl
     bool on[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        const uint32_t u = u0 + 256u * i + threadIdx.x;
+        const uint32_t u = u0 + (uint32_t)(THREADS * i) + threadIdx.x;
         on[i] = u < end;
         if (!on[i]) continue;
         row[i] = fastdiv(u, plan.by_each);
@@ -36,11 +36,10 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryArgs a, RotaryPlan pl
         x[i].load(from + (size_t)at[i].first * E);
         if (at[i].both) y[i].load(from + (size_t)at[i].second * E);
     }
-    for (uint32_t e = threadIdx.x; e < rows * (uint32_t)a.pairs; e += 256u) {
-        const uint32_t r = fastdiv(e, plan.by_pairs), p = e - r * (uint32_t)a.pairs, global = row0 + r;
-        const uint32_t place = global - fastdiv(global, plan.by_period) * plan.by_period.d;
-        turns[e] = rotary_pair(a.positions + (size_t)place * a.axes, a.axes, a.frequencies, a.axis_of, (int)p, a.inverse);
-    }
+    rotary_turns<THREADS>(turns, rows, a.pairs, a.axes, a.frequencies, a.axis_of, a.inverse, [&](uint32_t r, uint32_t axis) {
+        const uint32_t global = row0 + r, place = global - fastdiv(global, plan.by_period) * plan.by_period.d;
+        return a.positions[(size_t)place * a.axes + axis];
+    });
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -52,14 +51,19 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryArgs a, RotaryPlan pl
     }
 }
 
-template <class T, int V>
+template <class T, int V, int UNITS, int THREADS>
 hipError_t launch(const RotaryArgs& a, RotaryPlan plan, hipStream_t s) {
+    plan.rows = rotary_rows((long long)a.heads * plan.units, UNITS);
     const size_t lds = sizeof(f32x2) * (size_t)plan.rows * a.pairs;
-    auto* const kernel = &rotary_kernel<T, V>;
+    auto* const kernel = &rotary_kernel<T, V, UNITS, THREADS>;
     const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((plan.total + kRotaryUnits - 1) / kRotaryUnits)), dim3(256), lds, s, a, plan);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((plan.total + UNITS - 1) / UNITS)), dim3(THREADS), lds, s, a, plan);
     return hipGetLastError();
+}
+template <class T, int V>
+hipError_t launch(const RotaryArgs& a, const RotaryPlan& plan, hipStream_t s) {
+    return rotary_small(plan.total) ? launch<T, V, RotaryShape::kSmall, RotaryShape::kSmall>(a, plan, s) : launch<T, V, RotaryShape::kLarge, 256>(a, plan, s);
 }
 
 }  // namespace
@@ -74,10 +78,8 @@ hipError_t launch_rotary(const RotaryArgs& a, hipStream_t s) {
     plan.units = rotary_units(a.d, a.pairs, V);
     const long long each = (long long)a.heads * plan.units;
     plan.total = a.rows * each;
-    plan.rows = rotary_rows(each);
     plan.by_each = make_fastdiv((uint32_t)each);
     plan.by_units = make_fastdiv((uint32_t)plan.units);
-    plan.by_pairs = make_fastdiv(a.pairs > 0 ? (uint32_t)a.pairs : 1u);
     plan.by_period = make_fastdiv((uint32_t)a.period);
     if (a.dtype == 0) return V == 4 ? launch<SeqF32, 4>(a, plan, s) : launch<SeqF32, 1>(a, plan, s);
     if (a.dtype == 1) return V == 8 ? launch<SeqBf16, 8>(a, plan, s) : V == 4 ? launch<SeqBf16, 4>(a, plan, s) : launch<SeqBf16, 1>(a, plan, s);
