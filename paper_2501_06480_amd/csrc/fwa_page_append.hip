@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(THREADS) page_append_kernel(PageArgs a, Append
         if (!on[i]) continue;
         const AppendRow k = known[row[i] - row0];
         if (k.place < 0) continue;
-        if (turned[i]) rotary_apply<T, V>(x[i], y[i], turns + (size_t)(row[i] - row0) * a.pairs + unit[i] * V, a.interleaved);
+        if (turned[i]) rotary_apply<T, V>(x[i], y[i], turns + (size_t)(row[i] - row0) * a.pairs, (int)unit[i], a.pairs, a.interleaved);
         char* to;
         if (head[i] < (uint32_t)a.H) {
             to = static_cast<char*>(a.o) + ((size_t)row[i] * a.ldo + (size_t)head[i] * a.D) * E;

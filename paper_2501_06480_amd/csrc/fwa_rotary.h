@@ -1,8 +1,7 @@
 // Rotation of pairs of channels by their positions, as fwa_rotary.hip and fwa_page_append.hip have it.
 //
 // Pair p of a head is turned by the angle position[axis of p] * frequency[p]: (a, b) -> (a c - b s, b c + a s).  A unit of work is V pairs of
-// one head of one row: two vectors of V elements, V channels from each half of the rotated part, or (interleaved) 2 V neighbouring channels.  Channels behind
-// the pairs are copied, 2 V a unit.  Cosine and sine are formed once for all heads of a row and read from LDS, V pairs as 8 V bytes in a row.
+// one head of one row: two vectors of V elements.  Channels behind the pairs are copied, 2 V a unit.  Cosine and sine are formed once for all heads of a row and read from LDS, V pairs as 8 V bytes in a row.
 #pragma once
 
 #include "fwa_internal.h"
@@ -69,7 +68,8 @@ __device__ __forceinline__ f32x2 rotary_turn(int position, float frequency, bool
     sincospif(2.f * (float)turns, &s, &c);
     return f32x2{c, inverse ? -s : s};
 }
-// Where the two vectors of unit `u` of a head begin, in channels; the second may not exist for channels that are copied.
+// Where the two vectors of unit `u` of a head begin, in channels; the second may not exist for channels that are copied.  Of either kind of pairs a unit has V channels of each half of
+// the rotated part, so that neighbouring threads have neighbouring vectors (a single element's interleaved pair has its two channels).
 struct RotaryUnit {
     int first, second;
     bool turned, both;
@@ -78,43 +78,45 @@ template <int V>
 __device__ __forceinline__ RotaryUnit rotary_unit(int u, int pairs, int d, bool interleaved) {
     RotaryUnit r;
     r.turned = u * V < pairs;
-    if (r.turned && !interleaved) {
+    if (r.turned && !(V == 1 && interleaved)) {
         r.first = u * V;
         r.second = pairs + u * V;
     } else {
-        r.first = r.turned ? 2 * V * u : 2 * pairs + 2 * V * (u - pairs / V);
+        r.first = r.turned ? 2 * u : 2 * pairs + 2 * V * (u - pairs / V);
         r.second = r.first + V;
     }
     r.both = r.second < d;
     return r;
 }
 
-// The V pairs of two vectors, `table` = cosine and sine of the first of them in LDS.
+// The V pairs of the two vectors of unit `u`, `table` = cosine and sine of the row's pairs in LDS.
 template <class T, int V>
-__device__ __forceinline__ void rotary_apply(RotaryVector<T, V>& x, RotaryVector<T, V>& y, const f32x2* table, bool interleaved) {
-    float a[2 * V], z[2 * V];
+__device__ __forceinline__ void rotary_apply(RotaryVector<T, V>& x, RotaryVector<T, V>& y, const f32x2* table, int u, int pairs, bool interleaved) {
+    float a[V], b[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         a[i] = x.get(i);
-        a[V + i] = y.get(i);
+        b[i] = y.get(i);
     }
+    auto turn = [](float& p, float& q, const f32x2& t) {
+        const float first = fmaf(p, t[0], -(q * t[1]));
+        q = fmaf(q, t[0], p * t[1]);
+        p = first;
+    };
+    if (V > 1 && interleaved) {
+        const f32x2* const low = table + u * (V / 2);
+        const f32x2* const high = low + pairs / 2;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const f32x2 t = table[i];
-        const float c = t[0], s = t[1];
-        const float h0 = a[i], h1 = a[V + i], n0 = a[2 * i], n1 = a[2 * i + 1];
-        const float p = interleaved ? n0 : h0, q = interleaved ? n1 : h1;
-        const float first = fmaf(p, c, -(q * s)), second = fmaf(q, c, p * s);
-        if (interleaved) {
-            z[2 * i] = first;
-            z[2 * i + 1] = second;
-        } else {
-            z[i] = first;
-            z[V + i] = second;
+        for (int i = 0; i < V / 2; ++i) {
+            turn(a[2 * i], a[2 * i + 1], low[i]);
+            turn(b[2 * i], b[2 * i + 1], high[i]);
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) turn(a[i], b[i], table[u * V + i]);
     }
-    x.set(z);
-    y.set(z + V);
+    x.set(a);
+    y.set(b);
 }
 
 // Elements of a vector: 16 bytes where widths and pairs are whole vectors, half of that (16-bit data, heads of 72 channels for

@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(THREADS) rotary_kernel(RotaryArgs a, RotaryPla
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         if (!on[i]) continue;
-        if (at[i].turned) rotary_apply<T, V>(x[i], y[i], turns + (size_t)(row[i] - row0) * a.pairs + unit[i] * V, a.interleaved);
+        if (at[i].turned) rotary_apply<T, V>(x[i], y[i], turns + (size_t)(row[i] - row0) * a.pairs, (int)unit[i], a.pairs, a.interleaved);
         char* const to = static_cast<char*>(a.y) + ((size_t)row[i] * a.ldy + (size_t)head[i] * a.d) * E;
         x[i].store(to + (size_t)at[i].first * E);
         if (at[i].both) y[i].store(to + (size_t)at[i].second * E);
