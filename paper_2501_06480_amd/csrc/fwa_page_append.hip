@@ -126,7 +126,10 @@ hipError_t launch(const PageArgs& a, AppendPlan plan, hipStream_t s) {
 }
 template <class T, int V>
 hipError_t launch(const PageArgs& a, const AppendPlan& plan, hipStream_t s) {
-    return rotary_small(plan.total) ? launch<T, V, RotaryShape::kSmall, RotaryShape::kSmall>(a, plan, s) : launch<T, V, RotaryShape::kLarge, 256>(a, plan, s);
+    // Four units a thread where that leaves two workgroups for each CU: half as many searches (6439 tokens of 36 heads of 64, 0.9 million units,
+    // bf16: 15.0 us with two, 13.3 with four; a rotation of 0.2 million units, 7.6 and 8.1).
+    if (rotary_small(plan.total)) return launch<T, V, RotaryShape::kSmall, RotaryShape::kSmall>(a, plan, s);
+    return plan.total <= 512 * 1024 ? launch<T, V, RotaryShape::kLarge, 256>(a, plan, s) : launch<T, V, 2 * RotaryShape::kLarge, 256>(a, plan, s);
 }
 
 }  // namespace

@@ -129,8 +129,8 @@ inline int rotary_vector(int dtype, int d, int pairs) {
 // units of a head
 inline int rotary_units(int d, int pairs, int V) { return pairs / V + (d - 2 * pairs + 2 * V - 1) / (2 * V); }
 
-// Units and threads of a workgroup.  Large calls have two units a thread, small ones 128 threads with one each: more workgroups, and fewer cosines for each (64
-// windows of 49 rows of 3 heads of 32: 5.2 us with 512 units a workgroup, MEASURE with 128).
+// Units of a workgroup: 256 threads with two each, or for small calls 128 threads with one each, more workgroups with fewer cosines for each (64 windows of 49
+// rows of 3 heads of 32: kernel 5.6 us with 512 units, 3.7 with 128).
 struct RotaryShape {
     static constexpr int kLarge = 512, kSmall = 128;
 };
