@@ -158,19 +158,11 @@ __device__ __forceinline__ void page_values(const SeqColumnReader<T, D>& reader,
         v[b] = u32x4{p.x, p.y, q.x, q.y};
     }
 }
-// acc[m][b] += those rows' channels 32 b .. times their weights in half `h` of w[m], for MB blocks of rows at once.
-template <class T, int D, int MB>
-__device__ __forceinline__ void page_products(f32x16 (&acc)[MB][D / 32], const u32x4 (&v)[D / 32], const f32x16 (&w)[MB], int h) {
+// Half `h` of a tile of weights, rounded: the operand of a product over its 16 keys.
+template <class T>
+__device__ __forceinline__ u32x4 page_weights(const f32x16& w, int h) {
     constexpr bool F16 = __is_same(T, SeqF16);
-    u32x4 x[MB];
-#pragma unroll
-    for (int m = 0; m < MB; ++m)
-        x[m] = u32x4{pack_e<F16>(w[m][8 * h], w[m][8 * h + 1]), pack_e<F16>(w[m][8 * h + 2], w[m][8 * h + 3]), pack_e<F16>(w[m][8 * h + 4], w[m][8 * h + 5]),
-                     pack_e<F16>(w[m][8 * h + 6], w[m][8 * h + 7])};
-#pragma unroll
-    for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-        for (int m = 0; m < MB; ++m) acc[m][b] = seq_dot<T>(v[b], x[m], acc[m][b]);
+    return u32x4{pack_e<F16>(w[8 * h], w[8 * h + 1]), pack_e<F16>(w[8 * h + 2], w[8 * h + 3]), pack_e<F16>(w[8 * h + 4], w[8 * h + 5]), pack_e<F16>(w[8 * h + 6], w[8 * h + 7])};
 }
 
 // A wave's loads of a tile: its rows in groups of 16 (or 8) that lie in one page each.
@@ -200,14 +192,13 @@ struct PageLoader {
     }
 };
 
-// Two forms.  Rows: the W waves of a workgroup have 32 MB rows each and share the tiles.  KEYS: all have the same 32 rows and every W-th tile each, in
+// Two forms.  Rows: the W waves of a workgroup have 32 rows each and share the tiles.  KEYS: all have the same 32 rows and every W-th tile each, in
 // buffers of their own without a barrier, and join what they have at the end.  Workgroups share out the keys of a block besides where blocks are few.
-template <class T, int D, int W, int KT, int MB, bool KEYS, int OCC>
+template <class T, int D, int W, int KT, bool KEYS, bool WALKS, int OCC>
 __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, PagePlan plan) {
     constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, KS = KT / 32, SUB = KT / kPageRows;
-    constexpr int ROWS = KEYS ? 32 : 32 * MB * W, TURN = KEYS ? W : 1;  // of a workgroup; from a wave's tile to its next one
+    constexpr int ROWS = KEYS ? 32 : 32 * W, TURN = KEYS ? W : 1;  // of a workgroup; from a wave's tile to its next one
     constexpr uint32_t kTile = KT * RB;
-    static_assert(MB == 1 || !(KEYS || __is_same(T, SeqF32)), "one block of rows where the waves share out the keys, and of fp32");
     using Loader = PageLoader<RB, KT, KEYS ? 1 : W>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -221,11 +212,13 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     if (!KEYS && (round & 1u) && 256u * round + 256u <= gridDim.x) id = 512u * round + 248u - id + 2u * (id & 7u);
     const uint32_t rest = fastdiv(id, plan.by_kv), hk = id - rest * plan.by_kv.d;
     const uint32_t turn = fastdiv(rest, plan.by_splits), split = rest - turn * plan.by_splits.d;
-    const bool walks = KEYS && plan.workers > 0;
-    const uint32_t block = walks ? turn : (uint32_t)plan.blocks - 1u - turn, unit = block * (uint32_t)a.KV + hk;
+    const uint32_t block = WALKS ? turn : (uint32_t)plan.blocks - 1u - turn, unit = block * (uint32_t)a.KV + hk;
     PageBlock b;
     PageWalk<ROWS, KT, TURN> walk;
-    if (walks ? !walk.begin(a, plan, (int)block, b) : !page_block<ROWS>(a, plan, (int)block, b)) {
+    bool any;
+    if constexpr (WALKS) any = walk.begin(a, plan, (int)block, b);
+    else any = page_block<ROWS>(a, plan, (int)block, b);
+    if (!any) {
         if (plan.joined > 0 && split == 0 && threadIdx.x == 0) plan.joins[8 * (size_t)unit] = 0;
         return;
     }
@@ -241,7 +234,7 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     int t0 = 0, t1 = tiles, several = 0;
     uint32_t slot0 = 0u, second = 0u;  // rows of parts: where this one goes, and the second one of a block whose first it is
     bool whole = true;
-    if (walks) {
+    if constexpr (WALKS) {
         const PagePart p = page_part(walk.at, walk.units, walk.lo, walk.per);
         t0 = p.from;
         t1 = p.to < tiles ? p.to : tiles;
@@ -311,25 +304,22 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
         advance(ahead, stride.index, stride.slot);
         return r;
     };
-    int left = klen - mine0 * KT - load.row;  // keys from the next tile's first row on
-    auto issue = [&](const Groups& r, uint32_t buf) {
+    // rows of a tile of K or V from the first of this wave's on, of which there are `left`
+    auto issue = [&](const Groups& r, const char* from, int left, uint32_t to) {
 #pragma unroll
         for (int g = 0; g < Loader::kGroups; ++g) {
             const int rows = page_group(g * Loader::kGroup, left, Loader::kGroup, page_exists(r.g[g].page, a.pages));
             const uint64_t at = rows > 0 ? page_place((uint32_t)r.g[g].page, (uint32_t)r.g[g].slot, page_bytes, token_bytes) : 0u;
-            const uint32_t bytes = page_bytes_of(rows, token_bytes, RB);
-            const uint32_t kt = base + buf * 2u * kTile, vt = kt + kTile;
             // Rows that no load fills hold zeros: their weights are zero, and zero times whatever else LDS may hold need not be.
             if (rows < Loader::kGroup) {
-                load.zero(kt, g, lane);
-                load.zero(vt, g, lane);
+                load.zero(to, g, lane);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
-            load.issue(lds_source(kp + at, bytes), kt, g);
-            load.issue(lds_source(vp + at, bytes), vt, g);
+            load.issue(lds_source(from + at, page_bytes_of(rows, token_bytes, RB)), to, g);
         }
-        left -= kStride;
     };
+    int left = klen - mine0 * KT - load.row;  // in the tile that is asked for next
+    const uint32_t k_at = base, v_at = base + kTile;  // the first of two tiles each, 2 kTile apart
     // Groups of a tile whose page is none, looked up only where the part has any.
     auto missing = [&](int t) {
         uint32_t bad = 0u;
@@ -341,7 +331,9 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     Groups next = {}, after = {};
     if (mine0 < t1) {
         next = look();
-        issue(next, 0u);
+        issue(next, kp, left, k_at);
+        issue(next, vp, left, v_at);
+        left -= kStride;
         next = look();
     }
     bool holes = false;
@@ -354,30 +346,23 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
         holes = __any(holes);
     }
 
-    // the rows of this lane: token, head of the group, whether there is one
-    int limit[MB], token[MB], member[MB];
-    bool exists[MB];
-    u32x4 qf[MB][NC];
+    // the row of this lane: token, head of the group, whether there is one
+    const int row = b.row0 + (KEYS ? 0 : 32 * (int)wave) + (int)c;
+    const bool exists = row < b.rows;
+    const int token = exists ? (int)fastdiv((uint32_t)row, plan.by_group) : 0, member = exists ? row - token * G : 0;
+    const int pos = b.start + token, limit = a.causal && pos + 1 < klen ? pos + 1 : klen;
+    u32x4 qf[NC];
 #pragma unroll
-    for (int m = 0; m < MB; ++m) {
-        const int r = b.row0 + (KEYS ? 0 : 32 * (MB * (int)wave + m)) + (int)c;
-        exists[m] = r < b.rows;
-        token[m] = exists[m] ? (int)fastdiv((uint32_t)r, plan.by_group) : 0;
-        member[m] = exists[m] ? r - token[m] * G : 0;
-        const int pos = b.start + token[m];
-        limit[m] = a.causal && pos + 1 < klen ? pos + 1 : klen;
+    for (int s = 0; s < NC; ++s) qf[s] = u32x4{0u, 0u, 0u, 0u};
+    if (exists && a.scale != 0.f) {  // with a scale of zero the queries are zero: a shut out score times zero would be no score
+        const char* const qp = static_cast<const char*>(a.q) + ((size_t)(b.begin + token) * a.ldq + (size_t)(hk * G + member) * D) * E + 16u * hi;
 #pragma unroll
-        for (int s = 0; s < NC; ++s) qf[m][s] = u32x4{0u, 0u, 0u, 0u};
-        if (exists[m] && a.scale != 0.f) {  // with a scale of zero the queries are zero: a shut out score times zero would be no score
-            const char* const qp = static_cast<const char*>(a.q) + ((size_t)(b.begin + token[m]) * a.ldq + (size_t)(hk * G + member[m]) * D) * E + 16u * hi;
+        for (int s = 0; s < NC; ++s) qf[s] = *reinterpret_cast<const u32x4*>(qp + 32 * s);
+        // a negative scale goes into the queries, so that the largest product is the largest score
+        if (a.scale < 0.f) {
+            constexpr uint32_t kSign = __is_same(T, SeqF32) ? 0x80000000u : 0x80008000u;
 #pragma unroll
-            for (int s = 0; s < NC; ++s) qf[m][s] = *reinterpret_cast<const u32x4*>(qp + 32 * s);
-            // a negative scale goes into the queries, so that the largest product is the largest score
-            if (a.scale < 0.f) {
-                constexpr uint32_t kSign = __is_same(T, SeqF32) ? 0x80000000u : 0x80008000u;
-#pragma unroll
-                for (int s = 0; s < NC; ++s) qf[m][s] ^= kSign;
-            }
+            for (int s = 0; s < NC; ++s) qf[s] ^= kSign;
         }
     }
     // tiles with a key that a row of the block does not see: from mask0 on
@@ -390,48 +375,71 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     // tiles from here on show the rows of this wave nothing
     int wave_end = t1;
     if constexpr (!KEYS) {
-        const int first_row = b.row0 + 32 * MB * (int)wave, last_row = first_row + 32 * MB - 1 < b.rows ? first_row + 32 * MB - 1 : b.rows - 1;
-        const int pos = b.start + (int)fastdiv((uint32_t)last_row, plan.by_group), end = a.causal && pos + 1 < klen ? pos + 1 : klen;
+        const int first_row = b.row0 + 32 * (int)wave, last_row = first_row + 31 < b.rows ? first_row + 31 : b.rows - 1;
+        const int last = b.start + (int)fastdiv((uint32_t)last_row, plan.by_group), end = a.causal && last + 1 < klen ? last + 1 : klen;
         wave_end = first_row < b.rows ? (end + KT - 1) / KT : 0;
     }
 
-    f32x16 o[MB][NB];
-    float top_at[MB], sum[MB];
+    f32x16 o[NB];
 #pragma unroll
-    for (int m = 0; m < MB; ++m) {
-#pragma unroll
-        for (int x = 0; x < NB; ++x) seq_zero(o[m][x]);
-        top_at[m] = -__builtin_inff();
-        sum[m] = 0.f;
-    }
+    for (int x = 0; x < NB; ++x) seq_zero(o[x]);
+    float top_at = -__builtin_inff(), sum = 0.f;
     const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale) * kLog2e;
 
+    // The reference of a tile of scores: what no key has is shut out, and the reference follows the largest score so far.  Returns what is added to a score.
+    auto refer = [&](f32x16 (&s)[KS], int t) {
+        const uint32_t bad = holes ? missing(t) : 0u;
+        if (t >= mask0 || bad != 0u) {
+            const int room = limit - t * KT - 4 * (int)hi;
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const bool seen = 32 * k + 8 * (r / 4) + r % 4 < room && !((bad >> (2 * k + r / 8)) & 1u);
+                    s[k][r] = seen ? s[k][r] : -__builtin_inff();
+                }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[k][r]);
+        top = seq_max_halves(top) * scale;
+        if (__any(top > top_at + kSlack)) {
+            const float to = top > top_at + kSlack ? top : top_at, f = to == top_at ? 1.f : __builtin_amdgcn_exp2f(top_at - to);
+            top_at = to;
+            sum *= f;
+#pragma unroll
+            for (int x = 0; x < NB; ++x)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[x][r] *= f;
+        }
+        return top_at == -__builtin_inff() ? 0.f : -top_at;
+    };
     auto step = [&](auto parity, int t) {
         const uint32_t B = parity;
-        const uint32_t kt = base + B * 2u * kTile, vt = kt + kTile;
+        const uint32_t kt = k_at + B * 2u * kTile, vt = v_at + B * 2u * kTile;
         lds_loads_done();
         if constexpr (!KEYS) __syncthreads();
-        if (t + TURN < t1) issue(next, B ^ 1u);
+        if (t + TURN < t1) {
+            issue(next, kp, left, k_at + (B ^ 1u) * 2u * kTile);
+            issue(next, vp, left, v_at + (B ^ 1u) * 2u * kTile);
+        }
+        left -= kStride;
         if (!KEYS && t >= wave_end) {
             next = look();
             return;
         }
 
-        // scores
-        f32x16 s[KS][MB];
+        f32x16 s[KS];
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
-#pragma unroll
-            for (int m = 0; m < MB; ++m) seq_zero(s[k][m]);
+        for (int k = 0; k < KS; ++k) seq_zero(s[k]);
+        u32x4 v[2 * KS][NB];
         if constexpr (__is_same(T, SeqF32)) {
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
-                for (int x = 0; x < NC; ++x) {
-                    const u32x4 f = row_reader.read(kt, x, k);
-#pragma unroll
-                    for (int m = 0; m < MB; ++m) s[k][m] = seq_dot<T>(f, qf[m][x], s[k][m]);
-                }
+                for (int x = 0; x < NC; ++x) s[k] = seq_dot<T>(row_reader.read(kt, x, k), qf[x], s[k]);
         } else {
             u32x4 f[KS][NC];
 #pragma unroll
@@ -442,64 +450,25 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
 #pragma unroll
             for (int x = 0; x < NC; ++x)
 #pragma unroll
-                for (int k = 0; k < KS; ++k)
-#pragma unroll
-                    for (int m = 0; m < MB; ++m) s[k][m] = seq_dot<T>(f[k][x], qf[m][x], s[k][m]);
-        }
-        u32x4 v[2 * KS][NB];
-        if constexpr (!__is_same(T, SeqF32)) {
+                for (int k = 0; k < KS; ++k) s[k] = seq_dot<T>(f[k][x], qf[x], s[k]);
 #pragma unroll
             for (int h = 0; h < 2 * KS; ++h) page_values<T, D>(column_reader, v[h], vt, h);
         }
         __builtin_amdgcn_sched_barrier(0);
         after = look();
-
-        const uint32_t bad = holes ? missing(t) : 0u;
-        float minus[MB];
-#pragma unroll
-        for (int m = 0; m < MB; ++m) {
-            if (t >= mask0 || bad != 0u) {
-                const int room = limit[m] - t * KT - 4 * (int)hi;
-#pragma unroll
-                for (int k = 0; k < KS; ++k)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const bool seen = 32 * k + 8 * (r / 4) + r % 4 < room && !((bad >> (2 * k + r / 8)) & 1u);
-                        s[k][m][r] = seen ? s[k][m][r] : -__builtin_inff();
-                    }
-            }
-            float top = s[0][m][0];
-#pragma unroll
-            for (int k = 0; k < KS; ++k)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[k][m][r]);
-            top = seq_max_halves(top) * scale;
-            // the reference follows the largest score so far
-            if (__any(top > top_at[m] + kSlack)) {
-                const float to = top > top_at[m] + kSlack ? top : top_at[m], f = to == top_at[m] ? 1.f : __builtin_amdgcn_exp2f(top_at[m] - to);
-                top_at[m] = to;
-                sum[m] *= f;
-#pragma unroll
-                for (int x = 0; x < NB; ++x)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[m][x][r] *= f;
-            }
-            minus[m] = top_at[m] == -__builtin_inff() ? 0.f : -top_at[m];
-        }
+        const float minus = refer(s, t);
         auto weights = [&](int k) {
 #pragma unroll
-            for (int m = 0; m < MB; ++m)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[k][m][r] = __builtin_amdgcn_exp2f(fmaf(s[k][m][r], scale, minus[m]));
-                    sum[m] += s[k][m][r];
-                }
+            for (int r = 0; r < 16; ++r) {
+                s[k][r] = __builtin_amdgcn_exp2f(fmaf(s[k][r], scale, minus));
+                sum += s[k][r];
+            }
         };
         if constexpr (__is_same(T, SeqF32)) {
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 weights(k);
-                column_reader.accumulate(o[0], vt, k, s[k][0]);
+                column_reader.accumulate(o, vt, k, s[k]);
             }
         } else {
             weights(0);
@@ -507,7 +476,11 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) page_products<T, D, MB>(o, v[2 * k + h], s[k], h);
+                for (int h = 0; h < 2; ++h) {
+                    const u32x4 w = page_weights<T>(s[k], h);
+#pragma unroll
+                    for (int x = 0; x < NB; ++x) o[x] = seq_dot<T>(v[2 * k + h][x], w, o[x]);
+                }
                 if (k + 1 < KS) weights(k + 1);
             }
         }
@@ -523,14 +496,13 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
         }
     }
 
-#pragma unroll
-    for (int m = 0; m < MB; ++m) sum[m] = seq_sum_halves(sum[m]);
+    sum = seq_sum_halves(sum);
     if constexpr (KEYS && W > 1) {
         // sums of all waves through LDS, rows 4 floats apart from a multiple of the banks; the last wave has them, the others are done
         constexpr uint32_t kRow = 4u * (D + 4);
         const uint32_t all = lds_offset(lds), sums = all + W * 32u * kRow;
         __syncthreads();
-        if (hi == 0) *(__attribute__((address_space(3))) f32x2*)(uintptr_t)(sums + 8u * (32u * wave + c)) = f32x2{top_at[0], sum[0]};
+        if (hi == 0) *(__attribute__((address_space(3))) f32x2*)(uintptr_t)(sums + 8u * (32u * wave + c)) = f32x2{top_at, sum};
         __syncthreads();
         float top = -__builtin_inff(), total = 0.f, mine = 0.f;
 #pragma unroll
@@ -548,14 +520,14 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     *(__attribute__((address_space(3))) f32x4*)(uintptr_t)(all + kRow * (32u * wave + c) + 4u * (32 * x + 8 * q + 4 * hi)) =
-                        f32x4{o[0][x][4 * q] * mine, o[0][x][4 * q + 1] * mine, o[0][x][4 * q + 2] * mine, o[0][x][4 * q + 3] * mine};
+                        f32x4{o[x][4 * q] * mine, o[x][4 * q + 1] * mine, o[x][4 * q + 2] * mine, o[x][4 * q + 3] * mine};
         }
         __syncthreads();
         if (wave == W - 1) {
 #pragma unroll
         for (int x = 0; x < NB; ++x)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) o[0][x][r] *= mine;
+            for (int r = 0; r < 16; ++r) o[x][r] *= mine;
 #pragma unroll
         for (int w = 0; w < W - 1; ++w)
 #pragma unroll
@@ -564,53 +536,51 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
                 for (int q = 0; q < 4; ++q) {
                     const f32x4 y = seq_lds_f32x4(all + kRow * (32u * w + c) + 4u * (32 * x + 8 * q + 4 * hi));
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[0][x][4 * q + e] += y[e];
+                    for (int e = 0; e < 4; ++e) o[x][4 * q + e] += y[e];
                 }
-        top_at[0] = top;
-        sum[0] = total;
+        top_at = top;
+        sum = total;
         }
     }
-#pragma unroll
-    for (int m = 0; m < MB; ++m) {
-        if (!exists[m] || (KEYS && wave != W - 1)) continue;
-        const float l = sum[m];
+    if (exists && !(KEYS && wave != W - 1)) {
         if (!whole) {
-            const size_t slot = (size_t)slot0 + (KEYS ? 0 : 32 * (MB * wave + m)) + c;
+            const size_t slot = (size_t)slot0 + (KEYS ? 0 : 32 * wave) + c;
             float* const to = plan.part_o + slot * D;
-            if (l != 0.f)  // nothing reads a part without weight
+            if (sum != 0.f)  // nothing reads a part without weight
 #pragma unroll
                 for (int x = 0; x < NB; ++x)
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        *reinterpret_cast<f32x4*>(to + 32 * x + 8 * q + 4 * hi) = f32x4{o[m][x][4 * q], o[m][x][4 * q + 1], o[m][x][4 * q + 2], o[m][x][4 * q + 3]};
-            if (hi == 0) *reinterpret_cast<f32x2*>(plan.part_ml + 2 * slot) = f32x2{top_at[m], l};
-            continue;
+                        *reinterpret_cast<f32x4*>(to + 32 * x + 8 * q + 4 * hi) = f32x4{o[x][4 * q], o[x][4 * q + 1], o[x][4 * q + 2], o[x][4 * q + 3]};
+            if (hi == 0) *reinterpret_cast<f32x2*>(plan.part_ml + 2 * slot) = f32x2{top_at, sum};
+        } else {
+            const bool some = sum != 0.f;  // NaN too
+            const float f = some ? 1.f / sum : 0.f;
+            const size_t at = (size_t)(b.begin + token), head = hk * G + member;
+            char* const to = static_cast<char*>(a.o) + (at * a.ldo + head * D) * E;
+#pragma unroll
+            for (int x = 0; x < NB; ++x)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = some ? o[x][4 * q + e] * f : 0.f;
+                    seq_store4<T>(to, 32 * x + 8 * q + 4 * hi, y[0], y[1], y[2], y[3]);
+                }
+            if (a.stats && hi == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * (at * a.H + head)) = f32x2{some ? top_at : -__builtin_inff(), some ? log2f(sum) : 0.f};
         }
-        const bool any = l != 0.f;  // NaN too
-        const float f = any ? 1.f / l : 0.f;
-        const size_t row = (size_t)(b.begin + token[m]), head = hk * G + member[m];
-        char* const to = static_cast<char*>(a.o) + (row * a.ldo + head * D) * E;
-#pragma unroll
-        for (int x = 0; x < NB; ++x)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float y[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = any ? o[m][x][4 * q + e] * f : 0.f;
-                seq_store4<T>(to, 32 * x + 8 * q + 4 * hi, y[0], y[1], y[2], y[3]);
-            }
-        if (a.stats && hi == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * (row * a.H + head)) = f32x2{any ? top_at[m] : -__builtin_inff(), any ? log2f(l) : 0.f};
     }
-    const bool more = walks && walk.next(a, plan, b);
+    bool more = false;
+    if constexpr (WALKS) more = walk.next(a, plan, b);
     if (!more) {  // a sequence of several parts that a worker begins is its last one
         if (plan.joined > 0 && split == 0 && threadIdx.x == 0) {
             int* const to = plan.joins + 8 * (size_t)unit;
             *reinterpret_cast<i32x4*>(to) = i32x4{several, b.begin, b.row0, b.rows};
-            *reinterpret_cast<i32x4*>(to + 4) = i32x4{(int)slot0, (int)second, walks ? 2 * a.KV * ROWS : ROWS, 0};
+            *reinterpret_cast<i32x4*>(to + 4) = i32x4{(int)slot0, (int)second, WALKS ? 2 * a.KV * ROWS : ROWS, 0};
         }
         return;
     }
-    __syncthreads();  // the tiles and sums in LDS are done with
+    __syncthreads();  // the tiles and sums in LDS are done with, and the next sequence's may come
     }
 }
 
@@ -666,14 +636,13 @@ __global__ void __launch_bounds__(256) page_join_kernel(PageArgs a, PagePlan pla
 // Tiles and waves of the two forms.
 constexpr int page_tile_keys(int row_bytes, bool keys) { return row_bytes >= 512 || keys ? 32 : 64; }
 constexpr int page_waves(int row_bytes, bool keys) { return keys ? seq_keys_waves(row_bytes) : 4; }
-constexpr int page_row_blocks(int, bool) { return 1; }
 constexpr int page_occupancy(int row_bytes, bool keys) { return row_bytes == 128 && !keys ? 3 : 1; }
 
-template <class T, int D, bool KEYS>
+template <class T, int D, bool KEYS, bool WALKS>
 hipError_t launch(const PageArgs& a, const PagePlan& plan, hipStream_t s) {
-    constexpr int RB = D * SeqSize<T>::value, W = page_waves(RB, KEYS), KT = page_tile_keys(RB, KEYS), MB = page_row_blocks(RB, KEYS), ROWS = KEYS ? 32 : 32 * MB * W;
+    constexpr int RB = D * SeqSize<T>::value, W = page_waves(RB, KEYS), KT = page_tile_keys(RB, KEYS), ROWS = KEYS ? 32 : 32 * W;
     constexpr size_t tiles = 4 * (size_t)KT * RB * (KEYS ? W : 1), sums = KEYS && W > 1 ? (size_t)W * 32 * (4 * (D + 4) + 8) : 0, lds = tiles > sums ? tiles : sums;
-    auto* const kernel = &page_forward_kernel<T, D, W, KT, MB, KEYS, page_occupancy(RB, KEYS)>;
+    auto* const kernel = &page_forward_kernel<T, D, W, KT, KEYS, WALKS, page_occupancy(RB, KEYS)>;
     hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), lds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(plan.grid), dim3(64 * W), lds, s, a, plan);
@@ -693,7 +662,7 @@ bool page_plan(const PageArgs& a, PagePlan& f) {
     f = PagePlan{};
     f.keys = most_rows <= kFewRows;
     const int KT = page_tile_keys(RB, f.keys), W = page_waves(RB, f.keys);
-    f.rows = f.keys ? 32 : 32 * page_row_blocks(RB, false) * W;
+    f.rows = f.keys ? 32 : 32 * W;
     f.group = G;
     // blocks: a number for each sequence, or as many as the rows fill and one more for each sequence
     const long long each = (most_rows + f.rows - 1) / f.rows, all = (long long)a.rows * G / f.rows + a.N;
@@ -733,7 +702,8 @@ size_t page_workspace(const PagePlan& p, const PageArgs& a) {
 
 template <class T, int D>
 hipError_t launch(const PageArgs& a, const PagePlan& p, hipStream_t s) {
-    return p.keys ? launch<T, D, true>(a, p, s) : launch<T, D, false>(a, p, s);
+    if (p.workers > 0) return launch<T, D, true, true>(a, p, s);
+    return p.keys ? launch<T, D, true, false>(a, p, s) : launch<T, D, false, false>(a, p, s);
 }
 template <class T>
 hipError_t launch(const PageArgs& a, const PagePlan& p, hipStream_t s) {
