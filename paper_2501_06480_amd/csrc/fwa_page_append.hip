@@ -21,17 +21,22 @@ struct AppendRow {
 constexpr uint32_t kNowhere = 0xffffffffu;
 
 // Units as in the rotary kernel, a token's heads of queries, keys and values one behind the other, with their vectors on the way while the
-// places are looked up: sequence (a search in a sample of the offsets in LDS), length, page, three loads one behind the other, the last of them beside the cosines.
+// places are looked up: sequence and length in LDS (or, of more sequences than threads, from a sample of the offsets in LDS on), then the page, beside the cosines.
 template <class T, int V, int UNITS, int THREADS>
 __global__ void __launch_bounds__(THREADS) page_append_kernel(PageArgs a, AppendPlan plan) {
     constexpr int E = SeqSize<T>::value, U = UNITS / THREADS;
     extern __shared__ __attribute__((aligned(16))) f32x2 turns[];
-    __shared__ int samples[THREADS];
+    __shared__ int samples[THREADS + 1], lengths[THREADS];
     AppendRow* const known = reinterpret_cast<AppendRow*>(turns + (size_t)plan.rows * a.pairs);
     const uint32_t u0 = blockIdx.x * (uint32_t)UNITS, end = plan.total - u0 < UNITS ? (uint32_t)plan.total : u0 + UNITS;
     const uint32_t row0 = fastdiv(u0, plan.by_each), rows = fastdiv(end - 1u, plan.by_each) - row0 + 1u;
-    {
-        if ((int)threadIdx.x < plan.samples) samples[threadIdx.x] = a.offsets[threadIdx.x * (uint32_t)plan.sample];
+    if ((int)threadIdx.x < plan.samples) {
+        const uint32_t n = threadIdx.x * (uint32_t)plan.sample;
+        samples[threadIdx.x] = a.offsets[n];
+        if (plan.sample == 1) {
+            lengths[threadIdx.x] = a.lengths[n];
+            if ((int)threadIdx.x == plan.samples - 1) samples[plan.samples] = a.offsets[n + 1u];
+        }
     }
     RotaryVector<T, V> x[U], y[U];
     RotaryUnit at[U];
@@ -66,13 +71,22 @@ __global__ void __launch_bounds__(THREADS) page_append_kernel(PageArgs a, Append
             if (samples[mid] <= t) lo = mid;
             else hi = mid;
         }
-        int n = lo * plan.sample, to = n + plan.sample < a.N ? n + plan.sample : a.N;
-        while (to - n > 1) {
-            const int mid = (n + to) / 2;
-            if (a.offsets[mid] <= t) n = mid;
-            else to = mid;
+        int n = lo * plan.sample, begin, finish, length;
+        if (plan.sample == 1) {
+            begin = samples[n];
+            finish = samples[n + 1];
+            length = lengths[n];
+        } else {
+            int to = n + plan.sample < a.N ? n + plan.sample : a.N;
+            while (to - n > 1) {
+                const int mid = (n + to) / 2;
+                if (a.offsets[mid] <= t) n = mid;
+                else to = mid;
+            }
+            begin = a.offsets[n];
+            finish = a.offsets[n + 1];
+            length = a.lengths[n];
         }
-        const int begin = a.offsets[n], finish = a.offsets[n + 1], length = a.lengths[n];
         known[r] = AppendRow{begin <= t && t < finish ? page_length(length) + (t - page_offset(begin, a.rows)) : -1, n};
     }
     __syncthreads();

@@ -273,7 +273,8 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
         const int index = (int)fastdiv((uint32_t)key / (uint32_t)kPageRows, plan.by_sub);
         return Place{index, key - index * page_size};
     };
-    auto find = [&](int index) { return seq_constant(page_row, index < last_index ? index : last_index); };
+    // (entries behind the sequence's last are read and not used)
+    auto find = [&](int index) { return seq_constant(page_row, index < a.width ? index : a.width - 1); };
     struct Group {
         int page, slot;
     };
@@ -584,53 +585,71 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     }
 }
 
-// Joins the parts of blocks whose keys are shared out: a thread has four channels of a row.
+// Joins the parts of blocks whose keys are shared out: a workgroup has 32 rows, a thread four channels of some of them, with the loads of all on the way together.
 template <class T, int D, int ROWS>
 __global__ void __launch_bounds__(256) page_join_kernel(PageArgs a, PagePlan plan) {
-    constexpr int E = SeqSize<T>::value, kThreads = D / 4, kRows = 256 / kThreads, kTurns = ROWS / kRows;
+    constexpr int E = SeqSize<T>::value, kThreads = D / 4, kRows = 256 / kThreads, kMine = 32 / kRows, kTurns = ROWS / 32;
+    constexpr int kAtOnce = 8 / kMine;  // parts of a row
     const uint32_t unit = blockIdx.x / kTurns, turn = blockIdx.x - unit * kTurns, hk = unit - fastdiv(unit, plan.by_kv) * plan.by_kv.d;
     const i32x4 known = *reinterpret_cast<const i32x4*>(plan.joins + 8 * (size_t)unit), rows = *reinterpret_cast<const i32x4*>(plan.joins + 8 * (size_t)unit + 4);
-    const int parts = known[0], slot = (int)(turn * kRows + threadIdx.x / kThreads), r = known[2] + slot, channel = 4 * (int)(threadIdx.x % kThreads);
-    if (parts == 0 || r >= known[3]) return;
-    const size_t first = (size_t)(uint32_t)rows[0] + slot, second = (size_t)(uint32_t)rows[1] + slot, step = (size_t)(uint32_t)rows[2];
-    float top = -__builtin_inff(), l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    // a few parts at a time, all of their loads on the way together; a part without weight was not written, and whatever is in its place is not used
-    constexpr int kAtOnce = 8;
+    const int parts = known[0], channel = 4 * (int)(threadIdx.x % kThreads);
+    const uint32_t slot0 = 32u * turn + threadIdx.x / kThreads;
+    if (parts == 0 || known[2] + (int)slot0 >= known[3]) return;
+    const size_t first = (uint32_t)rows[0], second = (uint32_t)rows[1], step = (uint32_t)rows[2];
+    float top[kMine], l[kMine];
+    f32x4 o[kMine];
+#pragma unroll
+    for (int m = 0; m < kMine; ++m) {
+        top[m] = -__builtin_inff();
+        l[m] = 0.f;
+        o[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // rows that there are not are those of the first again; a part without weight was not written, and whatever is in its place is not used
     for (int s0 = 0; s0 < parts; s0 += kAtOnce) {
-        f32x2 ml[kAtOnce];
-        f32x4 x[kAtOnce];
+        f32x2 ml[kMine][kAtOnce];
+        f32x4 x[kMine][kAtOnce];
 #pragma unroll
-        for (int s = 0; s < kAtOnce; ++s) {
-            const int p = s0 + s < parts ? s0 + s : s0;
-            const size_t part = p == 0 ? first : second + (size_t)(p - 1) * step;
-            ml[s] = *reinterpret_cast<const f32x2*>(plan.part_ml + 2 * part);
-            x[s] = *reinterpret_cast<const f32x4*>(plan.part_o + part * D + channel);
-        }
-        float to = top;
+        for (int m = 0; m < kMine; ++m)
 #pragma unroll
-        for (int s = 0; s < kAtOnce; ++s) to = fmaxf(to, ml[s][0]);
-        const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - to);
-        top = to;
-        l *= f;
+            for (int s = 0; s < kAtOnce; ++s) {
+                const int p = s0 + s < parts ? s0 + s : s0;
+                const uint32_t slot = known[2] + (int)slot0 + m * kRows < known[3] ? slot0 + m * kRows : slot0;
+                const size_t part = (p == 0 ? first : second + (size_t)(p - 1) * step) + slot;
+                ml[m][s] = *reinterpret_cast<const f32x2*>(plan.part_ml + 2 * part);
+                x[m][s] = *reinterpret_cast<const f32x4*>(plan.part_o + part * D + channel);
+            }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] *= f;
+        for (int m = 0; m < kMine; ++m) {
+            float to = top[m];
 #pragma unroll
-        for (int s = 0; s < kAtOnce; ++s) {
-            if (s0 + s >= parts || ml[s][1] == 0.f) continue;
-            const float w = __builtin_amdgcn_exp2f(ml[s][0] - top);
-            l += w * ml[s][1];
+            for (int s = 0; s < kAtOnce; ++s) to = fmaxf(to, ml[m][s][0]);
+            const float f = l[m] == 0.f ? 0.f : __builtin_amdgcn_exp2f(top[m] - to);
+            top[m] = to;
+            l[m] *= f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += w * x[s][e];
+            for (int e = 0; e < 4; ++e) o[m][e] *= f;
+#pragma unroll
+            for (int s = 0; s < kAtOnce; ++s) {
+                if (s0 + s >= parts || ml[m][s][1] == 0.f) continue;
+                const float w = __builtin_amdgcn_exp2f(ml[m][s][0] - to);
+                l[m] += w * ml[m][s][1];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[m][e] += w * x[m][s][e];
+            }
         }
     }
-    const int token = (int)fastdiv((uint32_t)r, plan.by_group);
-    const size_t row = (size_t)(known[1] + token), head = hk * plan.group + (r - token * plan.group);
-    const bool any = l != 0.f;
-    const float f = any ? 1.f / l : 0.f;
-    char* const to = static_cast<char*>(a.o) + (row * a.ldo + head * D) * E;
-    seq_store4<T>(to, channel, o[0] * f, o[1] * f, o[2] * f, o[3] * f);
-    if (a.stats && channel == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * (row * a.H + head)) = f32x2{any ? top : -__builtin_inff(), any ? log2f(l) : 0.f};
+#pragma unroll
+    for (int m = 0; m < kMine; ++m) {
+        const int r = known[2] + (int)slot0 + m * kRows;
+        if (r >= known[3]) continue;
+        const int token = (int)fastdiv((uint32_t)r, plan.by_group);
+        const size_t row = (size_t)(known[1] + token), head = hk * plan.group + (r - token * plan.group);
+        const bool any = l[m] != 0.f;
+        const float f = any ? 1.f / l[m] : 0.f;
+        char* const to = static_cast<char*>(a.o) + (row * a.ldo + head * D) * E;
+        seq_store4<T>(to, channel, o[m][0] * f, o[m][1] * f, o[m][2] * f, o[m][3] * f);
+        if (a.stats && channel == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * (row * a.H + head)) = f32x2{any ? top[m] : -__builtin_inff(), any ? log2f(l[m]) : 0.f};
+    }
 }
 
 // Tiles and waves of the two forms.
@@ -648,8 +667,7 @@ hipError_t launch(const PageArgs& a, const PagePlan& plan, hipStream_t s) {
     hipLaunchKernelGGL(kernel, dim3(plan.grid), dim3(64 * W), lds, s, a, plan);
     e = hipGetLastError();
     if (e != hipSuccess || plan.joined == 0) return e;
-    constexpr unsigned turns = ROWS / (256 / (D / 4));
-    hipLaunchKernelGGL((page_join_kernel<T, D, ROWS>), dim3((unsigned)plan.joined * (unsigned)a.KV * turns), dim3(256), 0, s, a, plan);
+    hipLaunchKernelGGL((page_join_kernel<T, D, ROWS>), dim3((unsigned)plan.joined * (unsigned)a.KV * (unsigned)(ROWS / 32)), dim3(256), 0, s, a, plan);
     return hipGetLastError();
 }
 
