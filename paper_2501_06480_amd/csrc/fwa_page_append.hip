@@ -1,6 +1,7 @@
 // Append of new tokens to a paged cache: each token's keys, rotated by its position, and values go to their rows of the pages, and its queries are rotated
 // besides.  Tokens of several sequences stand one behind the other; a token's sequence is found from the offsets.
-#include "fwa_page.h"
+#include "fwa_internal.h"
+#include "fwa_page_index.h"
 #include "fwa_rotary.h"
 
 namespace fwa {

@@ -5,7 +5,9 @@
 // V through LDS, two of each.  What differs: the rows of a workgroup are those of all heads that share the keys, token by token, so that a tile is loaded once for
 // all of them and single tokens fill a block as far as they can; the loads of 16 rows of a tile go to one page, whose number is
 // looked up by the scalar unit two tiles ahead; how many rows and keys a sequence has is known on the device alone.
-#include "fwa_page.h"
+#include "fwa_internal.h"
+#include "fwa_page_index.h"
+#include "fwa_sequence.h"
 
 #include <type_traits>
 
@@ -48,14 +50,17 @@ struct PageBlock {
     int kend;           // keys up to this one are seen by a row of the block
 };
 
-// What is known of a sequence, its blocks left open
-__device__ __forceinline__ void page_sequence(const PageArgs& a, const PagePlan& plan, int n, PageBlock& b) {
+// What is known of a sequence from its entries in the tables, its blocks left open
+__device__ __forceinline__ void page_sequence(const PageArgs& a, const PagePlan& plan, int n, int offset, int next_offset, int length, PageBlock& b) {
     b.n = n;
-    b.begin = page_offset_of(a, n);
-    const int count = page_count(b.begin, page_offset_of(a, n + 1), a.most);
+    b.begin = page_offset(offset, a.rows);
+    const int count = page_count(b.begin, page_offset(next_offset, a.rows), a.most);
     b.rows = count * plan.group;
-    b.start = page_length_of(a, n);
+    b.start = page_length(length);
     b.klen = page_keys(b.start, count, a.width, a.page_size);
+}
+__device__ __forceinline__ void page_sequence(const PageArgs& a, const PagePlan& plan, int n, PageBlock& b) {
+    page_sequence(a, plan, n, seq_constant(a.offsets, n), seq_constant(a.offsets, n + 1), seq_constant(a.lengths, n), b);
 }
 __device__ __forceinline__ void page_place_block(const PageArgs& a, const PagePlan& plan, int within, int rows, PageBlock& b) {
     b.row0 = within * rows;
@@ -71,28 +76,31 @@ __device__ __forceinline__ int page_first_block(const PagePlan& plan, int offset
 // The block with this number; false: it has no rows
 template <int ROWS>
 __device__ __forceinline__ bool page_block(const PageArgs& a, const PagePlan& plan, int block, PageBlock& b) {
-    int n, within;
+    int within;
     if (plan.each > 0) {
-        n = (int)fastdiv((uint32_t)block, plan.by_each);
+        const int n = (int)fastdiv((uint32_t)block, plan.by_each);
         within = block - n * plan.each;
+        page_sequence(a, plan, n, b);
     } else {
-        // the last sequence that begins at or in front of this block, 64 candidates at a time
+        // the last sequence that begins at or in front of this block, 64 candidates at a time, each lane with all that is known of its own
         const int lane = (int)(threadIdx.x & 63u);
-        int lo = 0, size = a.N, first = 0;
+        int lo = 0, size = a.N;
         for (;;) {
-            const int step = (size + 63) / 64, at = lo + lane * step;
-            const int f = page_first_block<ROWS>(plan, page_offset(a.offsets[at < a.N ? at : a.N - 1], a.rows), at);
+            const int step = (size + 63) / 64, at = lo + lane * step, n = at < a.N ? at : a.N - 1;
+            const int offset = a.offsets[n], next_offset = a.offsets[n + 1], length = a.lengths[n];
+            const int f = page_first_block<ROWS>(plan, page_offset(offset, a.rows), at);
             const int count = __popcll(__ballot(at < lo + size && f <= block));
             if (count == 0) return false;
-            first = __builtin_amdgcn_readlane(f, count - 1);
             lo += (count - 1) * step;
-            if (step == 1) break;
+            if (step == 1) {
+                within = block - __builtin_amdgcn_readlane(f, count - 1);
+                page_sequence(a, plan, lo, __builtin_amdgcn_readlane(offset, count - 1), __builtin_amdgcn_readlane(next_offset, count - 1),
+                              __builtin_amdgcn_readlane(length, count - 1), b);
+                break;
+            }
             size = step < a.N - lo ? step : a.N - lo;
         }
-        n = lo;
-        within = block - first;
     }
-    page_sequence(a, plan, n, b);
     if (within < 0 || (long long)within * ROWS >= b.rows) return false;
     page_place_block(a, plan, within, ROWS, b);
     return true;
