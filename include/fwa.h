@@ -326,7 +326,7 @@ int fwa_rotary(const void* x, void* y, int64_t rows, int heads, int d, int64_t l
  *                      [rows, heads * d].  Rows in front of offsets[0] and from offsets[N] on are left as they were.
  *   lengths          : [N] int32: tokens of sequence n in front of the new ones; new token i has place lengths[n] + i.  Below 0 counts as 0.
  * Both calls of a step take the same tables.  d is 32, 64 or 128, dtype FWA_F32, FWA_BF16 or FWA_F16 for all tensors, rows <= 2^24,
- * N <= 2^20, rows * (heads + 2 kv_heads) <= 2^28.  The tables need 4-byte alignment only.
+ * N <= 2^20, rows * (heads + 2 kv_heads) <= 2^28, N * kv_heads up to about 15 million.  The tables need 4-byte alignment only.
  *
  * fwa_page_append stores the new tokens' keys, rotated, and values in their places, and rotates their queries besides.
  *   k, v       : [rows, kv_heads * d], rows ld_k resp. ld_v apart

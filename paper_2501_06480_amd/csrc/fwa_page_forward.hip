@@ -1,9 +1,9 @@
 // Attention of new tokens over a paged cache: O = softmax(scale Q K^T) V, the keys and values of a sequence in the rows of its pages, the new
 // tokens of all sequences one behind the other.
 //
-// As fwa_sequence_forward.hip: one pass over the keys with a running reference and sum per row, S^T = K Q^T and O^T += V^T P^T, tiles of K and
-// V through LDS, two of each.  What differs: the rows of a workgroup are those of all heads that share the keys, token by token, so that a tile is loaded once for
-// all of them and single tokens fill a block as far as they can; the loads of 16 rows of a tile go to one page, whose number is
+// As fwa_sequence_forward.hip: one pass over the keys with a running reference and sum per row, S^T = K Q^T and O^T += V^T P^T, tiles of K and V
+// through LDS, two of each.  What differs: the rows of a workgroup are those of all heads that share the keys, token by token, so that a tile is
+// loaded once for all of them and single tokens fill a block as far as they can; the loads of 16 rows of a tile go to one page, whose number is
 // looked up by the scalar unit two tiles ahead; how many rows and keys a sequence has is known on the device alone.
 #include "fwa_internal.h"
 #include "fwa_page_index.h"
@@ -17,8 +17,11 @@ namespace {
 // A row's reference moves when a score exceeds it by more than this, as in the attention of whole sequences.
 constexpr float kSlack = 6.f;
 constexpr int kFewRows = 32;  // rows (new tokens times heads of a group) up to which the waves of a workgroup share out the keys
-constexpr double kWorth = 8.0;  // tiles of a wave from which an even share of all keys is worth finding
-constexpr int kMostShared = 1024;  // sequences up to which workgroups share out all keys evenly
+// Tiles of a wave from which an even share of all keys is worth finding, which takes a workgroup about 3 us (32 sequences of 4096 to 8192 keys, 8
+// heads of 128, bf16, 250 tiles a wave: 158 us in parts of each sequence, 150 in even shares; 8 sequences of 1000 to 2000, 2 heads of 64, 2 tiles a
+// wave: 16.5 and 18.3), and sequences up to which it is: each lane adds up 16 of them at most.
+constexpr double kWorth = 8.0;
+constexpr int kMostShared = 1024;
 
 // How a call is laid out on the device.
 struct PagePlan {
@@ -111,7 +114,12 @@ template <int CONTROL, int ROW_MASK>
 __device__ __forceinline__ int page_scan_step(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CONTROL, ROW_MASK, 0xf, false); }
 __device__ __forceinline__ int page_scan(int x) {
     // from 1, 2, 4 and 8 lanes back within a row of 16; from the last lane of rows 0 and 2 to rows 1 and 3; of row 1 to rows 2 and 3
-    return page_scan_step<0x143, 0xc>(page_scan_step<0x142, 0xa>(page_scan_step<0x118, 0xf>(page_scan_step<0x114, 0xf>(page_scan_step<0x112, 0xf>(page_scan_step<0x111, 0xf>(x))))));
+    x = page_scan_step<0x111, 0xf>(x);
+    x = page_scan_step<0x112, 0xf>(x);
+    x = page_scan_step<0x114, 0xf>(x);
+    x = page_scan_step<0x118, 0xf>(x);
+    x = page_scan_step<0x142, 0xa>(x);
+    return page_scan_step<0x143, 0xc>(x);
 }
 // A worker's way through its range of the keys of all sequences.
 template <int ROWS, int KT, int TURN>
@@ -170,7 +178,8 @@ __device__ __forceinline__ void page_values(const SeqColumnReader<T, D>& reader,
 template <class T>
 __device__ __forceinline__ u32x4 page_weights(const f32x16& w, int h) {
     constexpr bool F16 = __is_same(T, SeqF16);
-    return u32x4{pack_e<F16>(w[8 * h], w[8 * h + 1]), pack_e<F16>(w[8 * h + 2], w[8 * h + 3]), pack_e<F16>(w[8 * h + 4], w[8 * h + 5]), pack_e<F16>(w[8 * h + 6], w[8 * h + 7])};
+    return u32x4{pack_e<F16>(w[8 * h], w[8 * h + 1]), pack_e<F16>(w[8 * h + 2], w[8 * h + 3]),
+                 pack_e<F16>(w[8 * h + 4], w[8 * h + 5]), pack_e<F16>(w[8 * h + 6], w[8 * h + 7])};
 }
 
 // A wave's loads of a tile: its rows in groups of 16 (or 8) that lie in one page each.
@@ -202,6 +211,12 @@ struct PageLoader {
 
 // Two forms.  Rows: the W waves of a workgroup have 32 rows each and share the tiles.  KEYS: all have the same 32 rows and every W-th tile each, in
 // buffers of their own without a barrier, and join what they have at the end.  Workgroups share out the keys of a block besides where blocks are few.
+// Rows: bound by the power of the card and by what a tile takes of all units: 2048 tokens on 6001, 16 heads of 128 on 4, bf16: 122 us, 970 TFLOP/s,
+// matrix units 42 per cent busy at the 1.6 GHz that the clock falls to (a product of 8192^3 reaches 1260).  Leaving out the loads, or the
+// exponentials, gains a tenth each, and no order of instructions gains any (scores a tile ahead of the weights: the same; 64 rows a wave, 8 waves,
+// tiles of 32 keys: slower).  Of tokens beside chunks (16 sequences, two of them with 500 new tokens: 60 us): the ends of parts of different lengths,
+// 41 us if all were one. Keys: bound by the reads of the cache (814 MB in 140 to 148 us, 5.5 TB/s) or, for short ones, by a chain of loads, tables,
+// pages, keys, of about 1 us each, behind the launch (4 tokens on 700, 12 heads of 64: 8.5 us).
 template <class T, int D, int W, int KT, bool KEYS, bool WALKS, int OCC>
 __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, PagePlan plan) {
     constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, KS = KT / 32, SUB = KT / kPageRows;
@@ -593,7 +608,9 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     }
 }
 
-// Joins the parts of blocks whose keys are shared out: a workgroup has 32 rows, a thread four channels of some of them, with the loads of all on the way together.
+// Joins the parts of blocks whose keys are shared out: a workgroup has 32 rows, a thread four channels of some of them, with the loads of all on the
+// way together (512 blocks of 128 rows of 128 channels, 33 MB: 8.9 us, 10.4 with 8 rows a workgroup; few rows: 4, a launch and two loads one behind
+// the other).
 template <class T, int D, int ROWS>
 __global__ void __launch_bounds__(256) page_join_kernel(PageArgs a, PagePlan plan) {
     constexpr int E = SeqSize<T>::value, kThreads = D / 4, kRows = 256 / kThreads, kMine = 32 / kRows, kTurns = ROWS / 32;
@@ -660,7 +677,7 @@ __global__ void __launch_bounds__(256) page_join_kernel(PageArgs a, PagePlan pla
     }
 }
 
-// Tiles and waves of the two forms.
+// Tiles, waves, and waves of a SIMD that the registers are held to, as in the attention of whole sequences.
 constexpr int page_tile_keys(int row_bytes, bool keys) { return row_bytes >= 512 || keys ? 32 : 64; }
 constexpr int page_waves(int row_bytes, bool keys) { return keys ? seq_keys_waves(row_bytes) : 4; }
 constexpr int page_occupancy(int row_bytes, bool keys) { return row_bytes == 128 && !keys ? 3 : 1; }
@@ -680,8 +697,11 @@ hipError_t launch(const PageArgs& a, const PagePlan& plan, hipStream_t s) {
 }
 
 // How a call is laid out, from what the host knows: the waves share out the keys where no sequence has more than a few rows.  Where there are too few
-// blocks for the device, its workgroups share out the keys besides, and a second launch joins the parts, but for caches that are too short to
-// be worth that (the join takes about as long as `alone` tiles).
+// blocks for the device, its workgroups share out the keys besides, and a second launch joins the parts, but for caches that are too short to be
+// worth that: the join takes as long as about `alone` tiles (704 keys, 6 tiles a wave: 9.0 us whole, 10.4 in parts of two).  Parts are no shorter
+// than `least` tiles of a wave (8 sequences of up to 2000 keys: two tiles 16.5 us, four 18.1; fp32 rows, whose tiles take four times as long, one
+// tile 14.5 us, four 20.1), and as many as two workgroups for each CU where all sequences bring the same rows, four where not or where the keys are
+// all there is to do (2048 tokens: two 131 us, four 142; tokens beside chunks: 77 and 72).
 bool page_plan(const PageArgs& a, PagePlan& f) {
     const int size = a.dtype == 0 ? 4 : 2, RB = a.D * size, G = a.H / a.KV, cus = cu_count();
     const long long most_rows = (long long)a.most * G, capacity = (long long)a.width * a.page_size;

@@ -37,10 +37,10 @@ FWA_PAGE_FN uint64_t page_place(uint32_t page, uint32_t slot, uint32_t page_byte
 // Bytes from there that the loads of `rows` rows may touch.
 FWA_PAGE_FN uint32_t page_bytes_of(int rows, uint32_t token_bytes, uint32_t row_bytes) { return rows > 0 ? (uint32_t)(rows - 1) * token_bytes + row_bytes : 0u; }
 
-// Sharing out the keys of sequences with a block of rows each.  A sequence is as many units as its keys have tiles, or one if it has none; all sequences, one
-// behind the other, are cut into ranges of `per` units, one for each worker.  A worker leaves its part of a sequence in one of two places, 0 for
-// the sequence that its range begins in, 1 for a later one that it begins and does not finish, of which there is one at most, the last of its range.  A sequence of
-// several parts has those of the worker that begins it, and of place 0 of the workers behind it.
+// Sharing out the keys of sequences with a block of rows each.  A sequence is as many units as its keys have tiles, or one if it has none; all
+// sequences, one behind the other, are cut into ranges of `per` units, one for each worker.  A worker leaves its part of a sequence in one of two
+// places, 0 for the sequence that its range begins in, 1 for a later one that it begins and does not finish, of which there is one at most, the last
+// of its range.  A sequence of several parts has those of the worker that begins it, and of place 0 of the workers behind it.
 FWA_PAGE_FN int page_units(int rows, int tiles) { return rows == 0 ? 0 : (tiles > 0 ? tiles : 1); }
 // units of a worker, a multiple of `turn` (the waves that share out a worker's tiles)
 FWA_PAGE_FN int page_share(int total, int workers, int least, int turn) {

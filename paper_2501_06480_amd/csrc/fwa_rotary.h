@@ -1,7 +1,8 @@
 // Rotation of pairs of channels by their positions, as fwa_rotary.hip and fwa_page_append.hip have it.
 //
-// Pair p of a head is turned by the angle position[axis of p] * frequency[p]: (a, b) -> (a c - b s, b c + a s).  A unit of work is V pairs of
-// one head of one row: two vectors of V elements.  Channels behind the pairs are copied, 2 V a unit.  Cosine and sine are formed once for all heads of a row and read from LDS, V pairs as 8 V bytes in a row.
+// Pair p of a head is turned by the angle position[axis of p] * frequency[p]: (a, b) -> (a c - b s, b c + a s).  A unit of work is V pairs of one
+// head of one row: two vectors of V elements.  Channels behind the pairs are copied, 2 V a unit.  Cosine and sine are formed once for all heads of a
+// row and read from LDS, V pairs as 8 V bytes in a row.
 #pragma once
 
 #include "fwa_internal.h"
@@ -68,8 +69,9 @@ __device__ __forceinline__ f32x2 rotary_turn(int position, float frequency, bool
     sincospif(2.f * (float)turns, &s, &c);
     return f32x2{c, inverse ? -s : s};
 }
-// Where the two vectors of unit `u` of a head begin, in channels; the second may not exist for channels that are copied.  Of either kind of pairs a unit has V channels of each half of
-// the rotated part, so that neighbouring threads have neighbouring vectors (a single element's interleaved pair has its two channels).
+// Where the two vectors of unit `u` of a head begin, in channels; the second may not exist for channels that are copied.  Of either kind of pairs a
+// unit has V channels of each half of the rotated part, so that neighbouring threads have neighbouring vectors (a single element's interleaved pair
+// has its two channels).
 struct RotaryUnit {
     int first, second;
     bool turned, both;
@@ -120,7 +122,7 @@ __device__ __forceinline__ void rotary_apply(RotaryVector<T, V>& x, RotaryVector
 }
 
 // Elements of a vector: 16 bytes where widths and pairs are whole vectors, half of that (16-bit data, heads of 72 channels for
-// instance), or single elements.  16-byte vectors against single ones, 2 x 6272 rows of 16 heads of 128, bf16: see fwa_rotary.hip.
+// instance), or single elements.
 inline int rotary_vector(int dtype, int d, int pairs) {
     const int most = dtype == 0 ? 4 : 8;
     if (d % most == 0 && pairs % most == 0) return most;
@@ -138,10 +140,11 @@ inline bool rotary_small(long long total) { return total <= 256 * RotaryShape::k
 // Rows that a workgroup's units may touch, of `each` units a row.
 inline int rotary_rows(long long each, int units) { return (int)((units - 1) / each) + 2; }
 
-// Cosines and sines of `rows` rows into LDS, pairs of a row one behind the other.  A thread has one pair of every so many rows, so that its axis and frequency are loaded
-// once, and the positions of four rows at a time.  position(r, axis) is that of row r on an axis of the row's.
+// Cosines and sines of `rows` rows into LDS, pairs of a row one behind the other.  A thread has one pair of every so many rows, so that its axis and
+// frequency are loaded once, and the positions of four rows at a time.  position(r, axis) is that of row r on an axis of the row's.
 template <int THREADS, class Position>
-__device__ __forceinline__ void rotary_turns(f32x2* turns, uint32_t rows, int pairs, int axes, const float* frequencies, const int32_t* axis_of, bool inverse, Position position) {
+__device__ __forceinline__ void rotary_turns(f32x2* turns, uint32_t rows, int pairs, int axes, const float* frequencies, const int32_t* axis_of, bool inverse,
+                                             Position position) {
     uint32_t wide = 1u;  // threads for a row's pairs: a power of two
     while (wide < (uint32_t)pairs && wide < THREADS) wide *= 2u;
     const uint32_t first = threadIdx.x & (wide - 1u), step = THREADS / wide;

@@ -678,6 +678,7 @@ py::object page_forward(const at::Tensor& q, const at::Tensor& k_pages, const at
     at::Tensor stats;
     if (want_stats) stats = at::empty({p.rows, heads, 2}, q.options().dtype(at::kFloat));
     const int dtype = dtype_code(q), H = to_int(heads, "heads"), most = to_int(most_new < 0 || most_new > p.rows ? p.rows : most_new, "most_new");
+    const c10::DeviceGuard guard(q.device());
     if (workspace) need_same_device(*workspace, "workspace", q);
     const at::Tensor ws = workspace ? *workspace : scratch(fwa_page_forward_workspace_bytes(p.rows, p.N, H, p.kv_heads, p.d, p.page_size, p.width, most, dtype), q);
     float* const sp = stats.defined() ? stats.data_ptr<float>() : nullptr;
@@ -686,7 +687,6 @@ py::object page_forward(const at::Tensor& q, const at::Tensor& k_pages, const at
     void* const st = stream_of(stream, q);
     int rc;
     {
-        const c10::DeviceGuard guard(q.device());
         const Nogil nogil;
         rc = fwa_page_forward(rq.p, p.k, p.v, ro.p, sp, p.rows, p.N, H, p.kv_heads, p.d, (float)scale, rq.ld, ro.ld, p.pages, p.page_size, p.page_stride, p.token_stride,
                               p.head_stride, p.table, p.width, p.offsets, p.lengths, most, causal, dtype, wp, wb, st);
@@ -876,9 +876,7 @@ struct Rotary : torch::autograd::Function<Rotary> {
     static at::Tensor forward(AutogradContext* ctx, const at::Tensor& x, const at::Tensor& positions, const at::Tensor& frequencies, const OptTensor& axis_of, int64_t heads,
                               bool interleaved, bool inverse) {
         ctx->save_for_backward({positions, frequencies, or_undefined(axis_of)});
-        ctx->saved_data["heads"] = heads;
-        ctx->saved_data["interleaved"] = interleaved;
-        ctx->saved_data["inverse"] = inverse;
+        ctx->saved_data["call"] = 4 * heads + 2 * interleaved + inverse;
         at::Tensor y;
         const int rc = run_rotary(y, x, heads, positions, frequencies, axis_of, interleaved, inverse, std::nullopt, std::nullopt);
         if (rc != FWA_OK) raise_status(rc, "fwa_rotary");
@@ -887,10 +885,10 @@ struct Rotary : torch::autograd::Function<Rotary> {
     static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
         return with_python_errors([&]() -> variable_list {
             const variable_list s = ctx->get_saved_variables();
+            const int64_t call = ctx->saved_data["call"].toInt();
             at::Tensor dx;
-            const int rc = run_rotary(dx, aligned(grads[0]), ctx->saved_data["heads"].toInt(), s[0].contiguous(), s[1].contiguous(),
-                                      s[2].defined() ? OptTensor(s[2].contiguous()) : OptTensor(), ctx->saved_data["interleaved"].toBool(),
-                                      !ctx->saved_data["inverse"].toBool(), std::nullopt, std::nullopt);
+            const int rc = run_rotary(dx, aligned(grads[0]), call / 4, s[0].contiguous(), s[1].contiguous(), s[2].defined() ? OptTensor(s[2].contiguous()) : OptTensor(),
+                                      (call & 2) != 0, (call & 1) == 0, std::nullopt, std::nullopt);
             if (rc != FWA_OK) raise_status(rc, "fwa_rotary");
             return {dx, at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()};
         });
