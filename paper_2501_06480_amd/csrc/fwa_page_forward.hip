@@ -217,16 +217,17 @@ struct PageLoader {
 // tiles of 32 keys: slower).  Of tokens beside chunks (16 sequences, two of them with 500 new tokens: 60 us): the ends of parts of different lengths,
 // 41 us if all were one. Keys: bound by the reads of the cache (814 MB in 140 to 148 us, 5.5 TB/s) or, for short ones, by a chain of loads, tables,
 // pages, keys, of about 1 us each, behind the launch (4 tokens on 700, 12 heads of 64: 8.5 us).
-template <class T, int D, int W, int KT, bool KEYS, bool WALKS, int OCC>
+template <class T, int D, int W, int KT, int BUFS, bool KEYS, bool WALKS, int OCC>
 __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, PagePlan plan) {
     constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, KS = KT / 32, SUB = KT / kPageRows;
     constexpr int ROWS = KEYS ? 32 : 32 * W, TURN = KEYS ? W : 1;  // of a workgroup; from a wave's tile to its next one
     constexpr uint32_t kTile = KT * RB;
+    static_assert(KEYS || BUFS == 2, "a tile is on its way while the one in front of it is read");
     using Loader = PageLoader<RB, KT, KEYS ? 1 : W>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t hi = lane >> 5, c = lane & 31u;
-    const uint32_t base = lds_offset(lds) + (KEYS ? wave * 4u * kTile : 0u);
+    const uint32_t base = lds_offset(lds) + (KEYS ? wave * 2u * BUFS * kTile : 0u);
 
     // workgroup -> head of the keys (neighbours, so that each XCD has few of them), and a part of a block of rows, the last ones of which have most
     // keys, or a share of all sequences.  Rounds of as many workgroups as there are CUs go forwards and backwards in turn, so that a CU's come to one sum.
@@ -445,11 +446,11 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
         const uint32_t kt = k_at + B * 2u * kTile, vt = v_at + B * 2u * kTile;
         lds_loads_done();
         if constexpr (!KEYS) __syncthreads();
-        if (t + TURN < t1) {
+        if (BUFS == 2 && t + TURN < t1) {
             issue(next, kp, left, k_at + (B ^ 1u) * 2u * kTile);
             issue(next, vp, left, v_at + (B ^ 1u) * 2u * kTile);
         }
-        left -= kStride;
+        if (BUFS == 2) left -= kStride;
         if (!KEYS && t >= wave_end) {
             next = look();
             return;
@@ -508,11 +509,18 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
                 if (k + 1 < KS) weights(k + 1);
             }
         }
+        if constexpr (BUFS == 1) {  // all reads of the tile are done with
+            if (t + TURN < t1) {
+                issue(next, kp, left, k_at);
+                issue(next, vp, left, v_at);
+            }
+            left -= kStride;
+        }
         next = after;
     };
     if constexpr (KEYS) {
         uint32_t parity = 0;
-        for (int t = mine0; t < t1; t += TURN, parity ^= 1u) step(parity, t);
+        for (int t = mine0; t < t1; t += TURN, parity ^= BUFS - 1u) step(parity, t);
     } else {
         for (int t = mine0; t < t1; t += 2) {
             step(std::integral_constant<uint32_t, 0>{}, t);
@@ -608,17 +616,18 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     }
 }
 
-// Joins the parts of blocks whose keys are shared out: a workgroup has 32 rows, a thread four channels of some of them, with the loads of all on the
-// way together (512 blocks of 128 rows of 128 channels, 33 MB: 8.9 us, 10.4 with 8 rows a workgroup; few rows: 4, a launch and two loads one behind
-// the other).
+// Joins the parts of blocks whose keys are shared out: a thread has four channels of a row, 16 parts at a time, of blocks of few rows (and as many as
+// 64 parts: one sequence of 32768 keys, 39 us in all, 58 with two at a time), or of some of a workgroup's 32 rows, with the loads of all on the way
+// together (512 blocks of 128 rows of 128 channels, 33 MB: 8.9 us, 10.4 with a row).  Few rows: 4 us, a launch and two loads one behind the other.
 template <class T, int D, int ROWS>
 __global__ void __launch_bounds__(256) page_join_kernel(PageArgs a, PagePlan plan) {
-    constexpr int E = SeqSize<T>::value, kThreads = D / 4, kRows = 256 / kThreads, kMine = 32 / kRows, kTurns = ROWS / 32;
-    constexpr int kAtOnce = 8 / kMine;  // parts of a row
+    constexpr bool KEYS = ROWS == 32;
+    constexpr int E = SeqSize<T>::value, kThreads = D / 4, kRows = 256 / kThreads, kMine = KEYS ? 1 : 32 / kRows, kTurns = ROWS / (kRows * kMine);
+    constexpr int kAtOnce = KEYS ? 16 : 8 / kMine;  // parts of a row
     const uint32_t unit = blockIdx.x / kTurns, turn = blockIdx.x - unit * kTurns, hk = unit - fastdiv(unit, plan.by_kv) * plan.by_kv.d;
     const i32x4 known = *reinterpret_cast<const i32x4*>(plan.joins + 8 * (size_t)unit), rows = *reinterpret_cast<const i32x4*>(plan.joins + 8 * (size_t)unit + 4);
     const int parts = known[0], channel = 4 * (int)(threadIdx.x % kThreads);
-    const uint32_t slot0 = 32u * turn + threadIdx.x / kThreads;
+    const uint32_t slot0 = (uint32_t)(kRows * kMine) * turn + threadIdx.x / kThreads;
     if (parts == 0 || known[2] + (int)slot0 >= known[3]) return;
     const size_t first = (uint32_t)rows[0], second = (uint32_t)rows[1], step = (uint32_t)rows[2];
     float top[kMine], l[kMine];
@@ -680,19 +689,22 @@ __global__ void __launch_bounds__(256) page_join_kernel(PageArgs a, PagePlan pla
 // Tiles, waves, and waves of a SIMD that the registers are held to, as in the attention of whole sequences.
 constexpr int page_tile_keys(int row_bytes, bool keys) { return row_bytes >= 512 || keys ? 32 : 64; }
 constexpr int page_waves(int row_bytes, bool keys) { return keys ? seq_keys_waves(row_bytes) : 4; }
+// Tiles of K and of V that a wave (workgroup) has room for: two, so that one is on its way while the other is read, or one where two leave a CU no
+// more than two waves (fp32 heads of 128, 16 sequences of up to 4000 keys, 8 heads: 138 us with one, 172 with two).
+constexpr int page_bufs(int row_bytes, bool keys) { return keys && row_bytes >= 512 ? 1 : 2; }
 constexpr int page_occupancy(int row_bytes, bool keys) { return row_bytes == 128 && !keys ? 3 : 1; }
 
 template <class T, int D, bool KEYS, bool WALKS>
 hipError_t launch(const PageArgs& a, const PagePlan& plan, hipStream_t s) {
     constexpr int RB = D * SeqSize<T>::value, W = page_waves(RB, KEYS), KT = page_tile_keys(RB, KEYS), ROWS = KEYS ? 32 : 32 * W;
-    constexpr size_t tiles = 4 * (size_t)KT * RB * (KEYS ? W : 1), sums = KEYS && W > 1 ? (size_t)W * 32 * (4 * (D + 4) + 8) : 0, lds = tiles > sums ? tiles : sums;
-    auto* const kernel = &page_forward_kernel<T, D, W, KT, KEYS, WALKS, page_occupancy(RB, KEYS)>;
+    constexpr size_t tiles = 2 * (size_t)page_bufs(RB, KEYS) * KT * RB * (KEYS ? W : 1), sums = KEYS && W > 1 ? (size_t)W * 32 * (4 * (D + 4) + 8) : 0, lds = tiles > sums ? tiles : sums;
+    auto* const kernel = &page_forward_kernel<T, D, W, KT, page_bufs(RB, KEYS), KEYS, WALKS, page_occupancy(RB, KEYS)>;
     hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), lds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(plan.grid), dim3(64 * W), lds, s, a, plan);
     e = hipGetLastError();
     if (e != hipSuccess || plan.joined == 0) return e;
-    hipLaunchKernelGGL((page_join_kernel<T, D, ROWS>), dim3((unsigned)plan.joined * (unsigned)a.KV * (unsigned)(ROWS / 32)), dim3(256), 0, s, a, plan);
+    hipLaunchKernelGGL((page_join_kernel<T, D, ROWS>), dim3((unsigned)plan.joined * (unsigned)a.KV * (unsigned)(KEYS ? 32 / (256 / (D / 4)) : ROWS / 32)), dim3(256), 0, s, a, plan);
     return hipGetLastError();
 }
 
