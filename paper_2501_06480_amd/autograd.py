@@ -177,11 +177,11 @@ class _Rotary(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         positions, frequencies, axis_of = (None if t is None else t.contiguous() for t in ctx.saved_tensors)
-        return (binding.fwa_rotary(_aligned(dy), ctx.heads, positions, frequencies, axis_of, ctx.interleaved, not ctx.inverse),) + (None,) * 6
+        return (_Rotary.apply(_aligned(dy), positions, frequencies, axis_of, ctx.heads, ctx.interleaved, not ctx.inverse),) + (None,) * 6
 
 
 def rotary(x, heads: int, positions, frequencies, axis_of=None, interleaved: bool = False, inverse: bool = False):
-    """Rotary positions (``binding.fwa_rotary``), differentiable in x: its gradient is the rotation back."""
+    """Rotary positions (``binding.fwa_rotary``), differentiable in x, any number of times: its gradient is the rotation back."""
     if _native_node(x, positions, frequencies, axis_of):
         return binding._native().rotary_node(x, int(heads), positions, frequencies, axis_of, bool(interleaved), bool(inverse))
     return _Rotary.apply(x, positions, frequencies, axis_of, int(heads), bool(interleaved), bool(inverse))

@@ -446,6 +446,7 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
         const uint32_t kt = k_at + B * 2u * kTile, vt = v_at + B * 2u * kTile;
         lds_loads_done();
         if constexpr (!KEYS) __syncthreads();
+        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads of the tile in front, before the loads of the next one write there
         if (BUFS == 2 && t + TURN < t1) {
             issue(next, kp, left, k_at + (B ^ 1u) * 2u * kTile);
             issue(next, vp, left, v_at + (B ^ 1u) * 2u * kTile);
@@ -509,7 +510,8 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
                 if (k + 1 < KS) weights(k + 1);
             }
         }
-        if constexpr (BUFS == 1) {  // all reads of the tile are done with
+        if constexpr (BUFS == 1) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             if (t + TURN < t1) {
                 issue(next, kp, left, k_at);
                 issue(next, vp, left, v_at);

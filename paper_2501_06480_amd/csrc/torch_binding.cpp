@@ -886,10 +886,15 @@ struct Rotary : torch::autograd::Function<Rotary> {
         return with_python_errors([&]() -> variable_list {
             const variable_list s = ctx->get_saved_variables();
             const int64_t call = ctx->saved_data["call"].toInt();
+            const at::Tensor dy = aligned(grads[0]), positions = s[0].contiguous(), frequencies = s[1].contiguous();
+            const OptTensor axis_of = s[2].defined() ? OptTensor(s[2].contiguous()) : OptTensor();
             at::Tensor dx;
-            const int rc = run_rotary(dx, aligned(grads[0]), call / 4, s[0].contiguous(), s[1].contiguous(), s[2].defined() ? OptTensor(s[2].contiguous()) : OptTensor(),
-                                      (call & 2) != 0, (call & 1) == 0, std::nullopt, std::nullopt);
-            if (rc != FWA_OK) raise_status(rc, "fwa_rotary");
+            if (at::GradMode::is_enabled() && dy.requires_grad()) {  // a gradient that is to be differentiated again
+                dx = Rotary::apply(dy, positions, frequencies, axis_of, call / 4, (call & 2) != 0, (call & 1) == 0);
+            } else {
+                const int rc = run_rotary(dx, dy, call / 4, positions, frequencies, axis_of, (call & 2) != 0, (call & 1) == 0, std::nullopt, std::nullopt);
+                if (rc != FWA_OK) raise_status(rc, "fwa_rotary");
+            }
             return {dx, at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()};
         });
     }

@@ -120,6 +120,22 @@ def test_gradient(native, dtype, interleaved):
     ref.check(odd, *ref.rotate(wide[1:].cpu().view(N, L, H * d), H, positions, f, axis, interleaved, True), "odd place")
 
 
+@pytest.mark.parametrize("native", [True, False])
+def test_gradient_of_a_gradient(native):
+    """f = |g|^2 / 2 with g = dx of sum(w y): of turns alone g has the length of w, so df/dw = w, up to the errors of two turns."""
+    from paper_2501_06480_amd import autograd
+    x, positions, f, axis, g = make(F32, 2, 9, 2, 32, (8, 8))
+    args = (positions.cuda(), f.cuda(), axis.cuda())
+    xd, w = x.cuda().requires_grad_(True), torch.randn(x.shape, generator=g).cuda().requires_grad_(True)
+    y = autograd.rotary(xd, 2, *args, True) if native else autograd._Rotary.apply(xd, *args, 2, True, False)
+    dx, = torch.autograd.grad((w * y).sum(), xd, create_graph=True)
+    assert dx.requires_grad
+    dw, = torch.autograd.grad((dx * dx).sum() / 2, w)
+    # a turn is off by 10 U32 of |a| + |b| at most; the first's error through the second, and the second's of a turned pair: sqrt 2 of that each
+    pair = w.detach().abs().view(2, 9, 2, 16, 2).sum(-1, keepdim=True).expand(2, 9, 2, 16, 2).reshape(w.shape)
+    assert bool(((dw - w.detach()).abs() <= 32 * ref.U32 * pair).all())
+
+
 def test_forward_mode_and_transforms_go_the_python_way():
     from paper_2501_06480_amd import autograd
     x, positions, f, axis, _ = make(F32, 2, 5, 1, 32, (16,))
