@@ -22,6 +22,7 @@ constexpr int kFewRows = 32;  // rows (new tokens times heads of a group) up to 
 // wave: 16.5 and 18.3), and sequences up to which it is: each lane adds up 16 of them at most.
 constexpr double kWorth = 8.0;
 constexpr int kMostShared = 1024;
+constexpr int kLengths = 16;  // lengths of parts that are tried at most
 
 // How a call is laid out on the device.
 struct PagePlan {
@@ -30,19 +31,19 @@ struct PagePlan {
     int group;        // heads of queries per head of keys
     int each;         // blocks of each sequence, 0: as many as it has, found by a search
     int blocks;
-    // The keys of a block may be shared out among workgroups: `splits` of them for each block, or `workers` for each head of the keys, evenly over all
-    // sequences.  1 and 0 otherwise.
-    int splits, workers;
+    // The keys of a block may be shared out among workgroups: `splits` of them for each block; parts of about one length of all blocks, `target` for each
+    // head of the keys; or `workers` for each, evenly over all sequences.  1, 0 and 0 otherwise.
+    int splits, target, workers;
     int alone, least; // tiles up to which a block is not shared out, and that a part has at least
     int lane_sequences;  // that a lane adds up for the workers
     unsigned grid;
     FastDiv by_kv, by_splits, by_each, by_group, by_sub;
-    size_t slots;     // rows of parts: [block][kv][split][rows] or [worker][kv][2][rows]
+    size_t slots;     // rows of parts: [block][kv][split][rows], [part][kv][rows] or [worker][kv][2][rows]
     float* part_o;    // [D] each, not divided by the sum
     float* part_ml;   // [2] each
-    int* joins;       // [block or worker][kv][8]: parts (0: nothing to join), first token, row of the block's first, rows of the sequence, rows of
+    int* joins;       // [block, part or worker][kv][8]: parts (0: nothing to join), first token, row of the block's first, rows of the sequence, rows of
                       // parts: the first part's, the second's, from one to the next
-    int joined;       // blocks or workers
+    int joined;       // blocks, parts or workers
 };
 
 // A block of a sequence's rows (token-major: row r is token r / group, head r % group of the group).
@@ -121,6 +122,37 @@ __device__ __forceinline__ int page_scan(int x) {
     x = page_scan_step<0x142, 0xa>(x);
     return page_scan_step<0x143, 0xc>(x);
 }
+// Parts of blocks of different sequences, of about one length: those of sequences of one block first, then those of the others, from a sequence's last
+// block on.  Each lane has a sequence.
+struct PageJob {
+    int split, parts, length;  // of the block; most parts of a block of the sequence; tiles of a part
+};
+template <int ROWS, int KT>
+__device__ __forceinline__ bool page_job(const PageArgs& a, const PagePlan& plan, int job, PageBlock& b, PageJob& j) {
+    const int lane = (int)(threadIdx.x & 63u), n = lane < a.N ? lane : a.N - 1;
+    const int offset = a.offsets[n], next_offset = a.offsets[n + 1], length = a.lengths[n];
+    const int from = page_offset(offset, a.rows), count = lane < a.N ? page_count(from, page_offset(next_offset, a.rows), a.most) : 0;
+    const int blocks = (int)(((uint32_t)count * (uint32_t)plan.group + ROWS - 1u) / ROWS);
+    const int tiles = (page_keys(page_length(length), count, a.width, a.page_size) + KT - 1) / KT;
+    j.length = page_length_first(__builtin_amdgcn_readlane(page_scan(blocks * tiles), 63), plan.target, plan.least);
+    int parts = page_parts(tiles, j.length, plan.alone);
+    for (int turn = 0; turn < kLengths && __builtin_amdgcn_readlane(page_scan(blocks * parts), 63) > plan.target; ++turn) {
+        j.length = page_length_next(j.length);
+        parts = page_parts(tiles, j.length, plan.alone);
+    }
+    const int one = blocks == 1 ? parts : 0, many = blocks > 1 ? blocks * parts : 0, ones = page_scan(one), all = page_scan(many);
+    const int first = blocks > 1 ? __builtin_amdgcn_readlane(ones, 63) + all - many : ones - one;
+    const unsigned long long mine = __ballot(first <= job && job < first + blocks * parts);
+    if (mine == 0) return false;
+    const int who = (int)__builtin_ctzll(mine), within = job - __builtin_amdgcn_readlane(first, who);
+    j.parts = __builtin_amdgcn_readlane(parts, who);
+    const int turn = (int)((uint32_t)within / (uint32_t)j.parts);
+    j.split = within - turn * j.parts;
+    page_sequence(a, plan, who, __builtin_amdgcn_readlane(offset, who), __builtin_amdgcn_readlane(next_offset, who), __builtin_amdgcn_readlane(length, who), b);
+    page_place_block(a, plan, __builtin_amdgcn_readlane(blocks, who) - 1 - turn, ROWS, b);
+    return true;
+}
+
 // A worker's way through its range of the keys of all sequences.
 template <int ROWS, int KT, int TURN>
 struct PageWalk {
@@ -236,11 +268,13 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     if (!KEYS && (round & 1u) && 256u * round + 256u <= gridDim.x) id = 512u * round + 248u - id + 2u * (id & 7u);
     const uint32_t rest = fastdiv(id, plan.by_kv), hk = id - rest * plan.by_kv.d;
     const uint32_t turn = fastdiv(rest, plan.by_splits), split = rest - turn * plan.by_splits.d;
-    const uint32_t block = WALKS ? turn : (uint32_t)plan.blocks - 1u - turn, unit = block * (uint32_t)a.KV + hk;
+    const uint32_t block = WALKS || plan.target > 0 ? turn : (uint32_t)plan.blocks - 1u - turn, unit = block * (uint32_t)a.KV + hk;
     PageBlock b;
     PageWalk<ROWS, KT, TURN> walk;
+    PageJob job = {};
     bool any;
     if constexpr (WALKS) any = walk.begin(a, plan, (int)block, b);
+    else if (!KEYS && plan.target > 0) any = page_job<ROWS, KT>(a, plan, (int)block, b, job);
     else any = page_block<ROWS>(a, plan, (int)block, b);
     if (!any) {
         if (plan.joined > 0 && split == 0 && threadIdx.x == 0) plan.joins[8 * (size_t)unit] = 0;
@@ -266,6 +300,18 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
         several = p.parts;
         slot0 = (2u * unit + (p.place > 0 ? 1u : 0u)) * ROWS;
         second = 2u * (unit + (uint32_t)a.KV) * ROWS;
+    } else if (!KEYS && plan.target > 0) {
+        const PageCut cut = page_cut(tiles, job.length, plan.alone, job.parts, job.split);
+        if (job.split >= cut.parts) {
+            if (threadIdx.x == 0) plan.joins[8 * (size_t)unit] = 0;
+            return;
+        }
+        t0 = cut.from;
+        t1 = cut.to;
+        whole = cut.parts == 1;
+        several = job.split == 0 && !whole ? cut.parts : 0;
+        slot0 = unit * ROWS;
+        second = slot0 + (uint32_t)a.KV * ROWS;
     } else if (plan.splits > 1) {
         int per = (int)fastdiv((uint32_t)(tiles + plan.splits - 1), plan.by_splits);
         if (per < plan.least) per = plan.least;
@@ -610,7 +656,7 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
         if (plan.joined > 0 && split == 0 && threadIdx.x == 0) {
             int* const to = plan.joins + 8 * (size_t)unit;
             *reinterpret_cast<i32x4*>(to) = i32x4{several, b.begin, b.row0, b.rows};
-            *reinterpret_cast<i32x4*>(to + 4) = i32x4{(int)slot0, (int)second, WALKS ? 2 * a.KV * ROWS : ROWS, 0};
+            *reinterpret_cast<i32x4*>(to + 4) = i32x4{(int)slot0, (int)second, WALKS ? 2 * a.KV * ROWS : !KEYS && plan.target > 0 ? a.KV * ROWS : ROWS, 0};
         }
         return;
     }
@@ -740,15 +786,18 @@ bool page_plan(const PageArgs& a, PagePlan& f) {
         if (f.keys && a.N <= kMostShared && base < 4.0 * cus && 2 * cus / a.KV >= 2 && base * (double)tiles >= kWorth * W * 2.0 * cus && (double)a.N * (double)tiles < 1.0e9) {
             f.workers = 2 * cus / a.KV;
             f.lane_sequences = (a.N + 63) / 64;
+        } else if (!f.keys && !same && a.N <= 64 && base < 2.0 * cus && base * (double)tiles > 2.0 * cus * f.least && (double)blocks * (double)tiles < 1.0e9) {
+            f.target = 2 * cus > a.KV ? 2 * cus / a.KV : 1;
+            f.blocks += f.target;
         } else {
             long long splits = (long long)((f.keys || !same ? 4.0 : 2.0) * cus / base);
             if (splits > tiles / f.least) splits = tiles / f.least;
             f.splits = splits < 1 ? 1 : splits > 64 ? 64 : (int)splits;
         }
     }
-    f.joined = f.workers > 0 ? f.workers : f.splits > 1 ? f.blocks : 0;
+    f.joined = f.workers > 0 ? f.workers : f.splits > 1 || f.target > 0 ? f.blocks : 0;
     f.grid = (unsigned)(f.workers > 0 ? f.workers : f.blocks * f.splits) * (unsigned)a.KV;
-    f.slots = f.workers > 0 ? (size_t)f.workers * a.KV * 2 * f.rows : f.splits > 1 ? (size_t)f.blocks * a.KV * f.splits * f.rows : 0;
+    f.slots = f.workers > 0 ? (size_t)f.workers * a.KV * 2 * f.rows : f.joined > 0 ? (size_t)f.blocks * a.KV * f.splits * f.rows : 0;
     f.by_kv = make_fastdiv((uint32_t)a.KV);
     f.by_splits = make_fastdiv((uint32_t)f.splits);
     f.by_each = make_fastdiv(f.each > 0 ? (uint32_t)f.each : 1u);

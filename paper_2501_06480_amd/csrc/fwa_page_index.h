@@ -62,4 +62,28 @@ FWA_PAGE_FN PagePart page_part(int at, int units, int lo, int per) {
     return p;
 }
 
+// Sharing out the keys of blocks whose sequences have different numbers of keys: parts of about one length, as many as a target.  A block of `tiles`
+// tiles of keys is this many parts of up to `length`, one if it has `alone` or fewer:
+FWA_PAGE_FN int page_parts(int tiles, int length, int alone) { return tiles <= alone ? 1 : (tiles + length - 1) / length; }
+// The length begins with what all blocks together have for each part, and grows while there are more parts than the target.  The first alone keeps
+// them below the target and the blocks together.
+FWA_PAGE_FN int page_length_first(int total, int target, int least) {
+    const int length = (int)(((uint32_t)total + (uint32_t)target - 1u) / (uint32_t)target);
+    return length > least ? length : least;
+}
+FWA_PAGE_FN int page_length_next(int length) { return length + 1 + length / 32; }
+// Tiles of part `split` of a block whose sequence has up to `most` parts a block; parts: how many this one has, all of them one behind the other.
+struct PageCut {
+    int from, to, parts;
+};
+FWA_PAGE_FN PageCut page_cut(int tiles, int length, int alone, int most, int split) {
+    const int wanted = page_parts(tiles, length, alone), parts = wanted < most ? wanted : most;
+    const int per = (int)((uint32_t)(tiles + parts - 1) / (uint32_t)parts);
+    PageCut c;
+    c.parts = tiles > 0 ? (int)((uint32_t)(tiles + per - 1) / (uint32_t)per) : 1;
+    c.from = split * per;
+    c.to = c.from + per < tiles ? c.from + per : tiles;
+    return c;
+}
+
 }  // namespace fwa

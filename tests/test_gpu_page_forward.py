@@ -90,6 +90,21 @@ def test_long_caches_are_shared_out(dtype, d, new, H, KV):
     compare(x, H, d ** -0.5, f"{dtype} d{d} {new} {H}/{KV}", most_new=new)
 
 
+@pytest.mark.parametrize("dtype,H,KV,d,size,causal", [(BF16, 4, 2, 64, 16, True), (F16, 4, 1, 128, 48, True), (F32, 2, 2, 32, 16, True), (F32, 2, 1, 128, 16, True),
+                                                      (BF16, 6, 3, 32, 32, False), (BF16, 8, 1, 128, 16, True)])
+@pytest.mark.parametrize("news,lengths", [([1, 150, 1, 40, 0, 260, 1], [900, 1500, 0, 2000, 700, 10, 3000]), ([300, 1], [2500, 100]), ([0, 0, 130], [50, 0, 4000]),
+                                          ([1] * 60 + [70, 0, 1, 33], [0, 1, 400, 90] * 15 + [1200, 10, 1600, 0])])
+def test_chunks_of_different_lengths(dtype, H, KV, d, size, causal, news, lengths):
+    """Up to 64 sequences of which each brings what it has, behind wide tables: blocks are cut into parts of about one length, some into one, some into many."""
+    x, _ = make(dtype, news, lengths, H, KV, d, size, spare=(2, 3), wider=3000 // size)
+    for n, column in ((len(news) - 1, 3), (1, 0)):
+        x["page_table"][n, column] = -1
+    got = compare(x, H, d ** -0.5, f"{dtype} {news[:7]} {H}/{KV} d{d}", size == 48, None, causal)
+    again = run(device(x), H, d ** -0.5, most_new=None, causal=causal, out=torch.full_like(x["q"], 7.0).cuda())
+    rows = slice(2, x["q"].shape[0] - 3)
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1][rows], again[1][rows])
+
+
 def test_mixed_batches_of_many_sequences():
     """More sequences than lanes: their blocks are found by a search of two steps."""
     g = torch.Generator().manual_seed(5)

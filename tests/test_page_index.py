@@ -141,3 +141,67 @@ def test_shares_cover_every_unit_once(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout + r.stderr
+
+
+CUTS = r'''
+#include "fwa_page_index.h"
+#include <cstdio>
+#include <cstdlib>
+#include <random>
+#include <vector>
+using namespace fwa;
+static void need(bool ok, const char* what) { if (!ok) { std::printf("FAILED %s\n", what); std::exit(1); } }
+int main() {
+    std::mt19937 g(3);
+    auto pick = [&](int lo, int hi) { return (int)(lo + (long long)(g() % (uint64_t)((long long)hi - lo + 1))); };
+    long long cuts = 0;
+    for (int round = 0; round < 20000; ++round) {
+        const int N = pick(1, 64), target = pick(1, 600), least = pick(1, 4), alone = pick(1, 8), turns = pick(0, 20), most = pick(0, 1) ? 30 : 4000;
+        std::vector<int> blocks, tiles;
+        int total = 0, all = 0;
+        for (int n = 0; n < N; ++n) {
+            blocks.push_back(pick(0, 2) ? pick(0, 2) : pick(0, 60));
+            tiles.push_back(pick(0, 5) ? pick(0, most) : 0);
+            total += blocks[n] * tiles[n];
+            all += blocks[n];
+        }
+        int length = page_length_first(total, target, least), jobs = 0;
+        need(length >= least && (long long)length * target >= total, "first length");
+        for (int turn = 0;; ++turn) {
+            jobs = 0;
+            for (int n = 0; n < N; ++n) jobs += blocks[n] * page_parts(tiles[n], length, alone);
+            need(jobs <= target + all, "parts that the grid has");
+            if (turn >= turns || jobs <= target) break;
+            need(page_length_next(length) > length, "a longer one");
+            length = page_length_next(length);
+        }
+        for (int n = 0; n < N; ++n) {
+            const int parts = page_parts(tiles[n], length, alone);
+            for (int block = 0; block < blocks[n]; ++block) {
+                const int mine = block + 1 == blocks[n] ? tiles[n] : pick(0, tiles[n]);  // causal blocks see fewer
+                int at = 0;
+                const int count = page_cut(mine, length, alone, parts, 0).parts;
+                need(count >= 1 && count <= parts, "places of the sequence's blocks");
+                for (int split = 0; split < count; ++split) {
+                    const PageCut c = page_cut(mine, length, alone, parts, split);
+                    need(c.parts == count && c.from == at && (c.to > c.from || mine == 0), "parts one behind the other");
+                    at = c.to;
+                    ++cuts;
+                }
+                need(at == mine, "all tiles");
+            }
+        }
+    }
+    std::printf("%lld cuts\n", cuts);
+    return cuts > 10000 ? 0 : 1;
+}
+'''
+
+
+def test_cuts_cover_every_tile_once(tmp_path):
+    """Parts of about one length of blocks of all kinds: no more than the grid has workgroups, every tile in one part, as many as the join reads."""
+    src, exe = tmp_path / "cuts.cpp", tmp_path / "cuts"
+    src.write_text(CUTS)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout + r.stderr
