@@ -235,7 +235,7 @@ int fwa_page_forward(const void* q, const void* k_pages, const void* v_pages, vo
     if (need > 0 && (!workspace || workspace_bytes < need)) return FWA_ERR_WORKSPACE;
     a.q = q; a.k = const_cast<void*>(k_pages); a.v = const_cast<void*>(v_pages); a.o = o; a.stats = stats;
     a.ldq = ld_q; a.ldo = ld_o; a.causal = causal != 0; a.scale = scale;
-    return fwa::launch_page_forward(a, workspace, static_cast<hipStream_t>(stream)) == hipSuccess ? FWA_OK : FWA_ERR_LAUNCH;
+    return fwa::launch_page_forward(a, workspace, workspace_bytes, static_cast<hipStream_t>(stream)) == hipSuccess ? FWA_OK : FWA_ERR_LAUNCH;
 }
 
 }  // extern "C"

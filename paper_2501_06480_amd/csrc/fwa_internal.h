@@ -208,6 +208,6 @@ bool page_append_fits(const PageArgs& a);
 hipError_t launch_page_append(const PageArgs& a, hipStream_t s);
 bool page_forward_fits(const PageArgs& a);
 size_t page_forward_workspace(const PageArgs& a);
-hipError_t launch_page_forward(const PageArgs& a, void* workspace, hipStream_t s);
+hipError_t launch_page_forward(const PageArgs& a, void* workspace, size_t workspace_bytes, hipStream_t s);
 
 }  // namespace fwa

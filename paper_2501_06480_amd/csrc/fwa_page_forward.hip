@@ -246,8 +246,8 @@ struct PageLoader {
 // Rows: bound by the power of the card and by what a tile takes of all units: 2048 tokens on 6001, 16 heads of 128 on 4, bf16: 122 us, 970 TFLOP/s,
 // matrix units 42 per cent busy at the 1.6 GHz that the clock falls to (a product of 8192^3 reaches 1260).  Leaving out the loads, or the
 // exponentials, gains a tenth each, and no order of instructions gains any (scores a tile ahead of the weights: the same; 64 rows a wave, 8 waves,
-// tiles of 32 keys: slower).  Of tokens beside chunks (16 sequences, two of them with 500 new tokens: 60 us): the ends of parts of different lengths,
-// 41 us if all were one. Keys: bound by the reads of the cache (814 MB in 140 to 148 us, 5.5 TB/s) or, for short ones, by a chain of loads, tables,
+// tiles of 32 keys: slower).  Of single tokens beside chunks (16 sequences, two of them with 500 new tokens: 54 us): one wave of four works for a
+// token's block, and parts are whole numbers of tiles in one round of workgroups.  Keys: bound by the reads of the cache (814 MB in 140 to 148 us, 5.5 TB/s) or, for short ones, by a chain of loads, tables,
 // pages, keys, of about 1 us each, behind the launch (4 tokens on 700, 12 heads of 64: 8.5 us).
 template <class T, int D, int W, int KT, int BUFS, bool KEYS, bool WALKS, int OCC>
 __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, PagePlan plan) {
@@ -760,8 +760,10 @@ hipError_t launch(const PageArgs& a, const PagePlan& plan, hipStream_t s) {
 // blocks for the device, its workgroups share out the keys besides, and a second launch joins the parts, but for caches that are too short to be
 // worth that: the join takes as long as about `alone` tiles (704 keys, 6 tiles a wave: 9.0 us whole, 10.4 in parts of two).  Parts are no shorter
 // than `least` tiles of a wave (8 sequences of up to 2000 keys: two tiles 16.5 us, four 18.1; fp32 rows, whose tiles take four times as long, one
-// tile 14.5 us, four 20.1), and as many as two workgroups for each CU where all sequences bring the same rows, four where not or where the keys are
-// all there is to do (2048 tokens: two 131 us, four 142; tokens beside chunks: 77 and 72).
+// tile 14.5 us, four 20.1).  How many: all blocks of sequences with the same number of new tokens have as many as make two workgroups for each CU (2048
+// tokens: 131 us, with four 142), four where the keys are all there is to do.  Blocks of sequences that bring different numbers, up to 64 of them, are cut
+// into parts of one length, no more than two for each CU, which the device finds from all lengths (two chunks of 500 beside 14 tokens: 63 us, 70
+// with as many parts for each block; 16 chunks of 61: 49 and 65; causal prompts of one length cut like that: 101 whole, 118 to 160 in parts).
 bool page_plan(const PageArgs& a, PagePlan& f) {
     const int size = a.dtype == 0 ? 4 : 2, RB = a.D * size, G = a.H / a.KV, cus = cu_count();
     const long long most_rows = (long long)a.most * G, capacity = (long long)a.width * a.page_size;
@@ -833,9 +835,10 @@ size_t page_forward_workspace(const PageArgs& a) {
     return page_plan(a, p) ? page_workspace(p, a) : 0;
 }
 
-hipError_t launch_page_forward(const PageArgs& a, void* workspace, hipStream_t s) {
+hipError_t launch_page_forward(const PageArgs& a, void* workspace, size_t workspace_bytes, hipStream_t s) {
     PagePlan p;
-    if (!page_plan(a, p)) return hipErrorInvalidValue;
+    // the layout goes by what the workspace's query knows too: not by pointers, strides of rows, scale or causality
+    if (!page_plan(a, p) || page_workspace(p, a) > (workspace ? workspace_bytes : 0)) return hipErrorInvalidValue;
     if (p.joined > 0) {
         p.part_o = static_cast<float*>(workspace);
         p.part_ml = p.part_o + p.slots * (size_t)a.D;

@@ -47,6 +47,26 @@ def test_more_sequences_than_lanes_shared_out():
     compare(x, 4, 0.1, "one sequence", most_new=1)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,H,KV,d,news,width,most", [(BF16, 4, 2, 64, [1, 1, 0, 1], 200, 1), (F16, 8, 1, 128, [3, 3, 3], 300, 3), (BF16, 4, 2, 64, [1, 2, 0, 1], 8192, 2),
+                                                          (F32, 2, 2, 32, [40, 40], 200, 40), (BF16, 4, 1, 128, [1, 150, 60, 0], 200, None)])
+def test_the_workspace_ends_where_the_query_says(dtype, H, KV, d, news, width, most, causal):
+    """Each way of sharing out keys, in a workspace of not a byte more than asked for, with a mark behind it."""
+    import paper_2501_06480_amd as fwa
+    T, N, code = sum(news), len(news), {F32: 0, BF16: 1, F16: 2}[dtype]
+    x, _ = shared_out(dtype, news, [700, 33, 5, 1500][:N], H, KV, d, 16, width)
+    need = fwa.fwa_page_forward_workspace_bytes(T, N, H, KV, d, 16, width, T if most is None else most, code)
+    assert need > 0
+    whole = torch.full((need + 4096,), 0xa5, dtype=torch.uint8, device="cuda")
+    y = device(x)
+    o, stats = run(y, H, 0.1, most_new=most, causal=causal, workspace=whole[:need])
+    assert bool((whole[need:] == 0xa5).all())
+    again, more = run(y, H, 0.1, most_new=most, causal=causal)
+    assert torch.equal(o, again) and torch.equal(stats, more)
+    with pytest.raises(fwa.FwaError):
+        run(y, H, 0.1, most_new=most, causal=causal, workspace=whole[:need - 1])
+
+
 def cache(pages, size, KV, d, dtype):
     return [torch.full((pages, size, KV, d), float("nan"), dtype=dtype, device="cuda") for _ in range(2)]
 
