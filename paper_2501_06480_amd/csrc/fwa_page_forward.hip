@@ -2,7 +2,7 @@
 // tokens of all sequences one behind the other.
 //
 // As fwa_sequence_forward.hip: one pass over the keys with a running reference and sum per row, S^T = K Q^T and O^T += V^T P^T, tiles of K and V
-// through LDS, two of each.  What differs: the rows of a workgroup are those of all heads that share the keys, token by token, so that a tile is
+// through LDS.  What differs: the rows of a workgroup are those of all heads that share the keys, token by token, so that a tile is
 // loaded once for all of them and single tokens fill a block as far as they can; the loads of 16 rows of a tile go to one page, whose number is
 // looked up by the scalar unit two tiles ahead; how many rows and keys a sequence has is known on the device alone.
 #include "fwa_internal.h"
@@ -175,7 +175,7 @@ struct PageWalk {
         units = 0;
         for (int n = owner * plan.lane_sequences;; ++n) {
             enter(a, plan, n, b);
-            if (at + units > lo) return true;
+            if (at + units > lo || n >= a.N - 1) return true;
         }
     }
     __device__ __forceinline__ void enter(const PageArgs& a, const PagePlan& plan, int n, PageBlock& b) {
@@ -189,7 +189,7 @@ struct PageWalk {
         if (at + units >= lo + per || at + units >= total) return false;
         int n = b.n;
         do enter(a, plan, ++n, b);
-        while (units == 0);
+        while (units == 0 && n < a.N - 1);
         return true;
     }
 };
@@ -213,6 +213,12 @@ __device__ __forceinline__ u32x4 page_weights(const f32x16& w, int h) {
     return u32x4{pack_e<F16>(w[8 * h], w[8 * h + 1]), pack_e<F16>(w[8 * h + 2], w[8 * h + 3]),
                  pack_e<F16>(w[8 * h + 4], w[8 * h + 5]), pack_e<F16>(w[8 * h + 6], w[8 * h + 7])};
 }
+
+// Waits until a wave has what it reads from LDS, so that loads may write there; until no more than N of its loads are on their way, which end in
+// their order.
+__device__ __forceinline__ void lds_reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void loads_left() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 // A wave's loads of a tile: its rows in groups of 16 (or 8) that lie in one page each.
 template <int RB, int KT, int WAVES>
@@ -241,25 +247,27 @@ struct PageLoader {
     }
 };
 
-// Two forms.  Rows: the W waves of a workgroup have 32 rows each and share the tiles.  KEYS: all have the same 32 rows and every W-th tile each, in
-// buffers of their own without a barrier, and join what they have at the end.  Workgroups share out the keys of a block besides where blocks are few.
+// Two forms.  Rows: the W waves of a workgroup have 32 rows each and share the tiles, two of K and of V, so that one is on its way while the other is
+// read.  KEYS: all have the same 32 rows and every W-th tile each, in one place for each wave without a barrier, and join what they have at the end; a
+// tile's loads follow its reads, beside softmax and products (two places each: 10.6 us for 300 sequences of 100 keys, 7.5 with one, which leaves a CU
+// room for more workgroups; 155 and 151 for 128 of up to 2000).  Workgroups share out the keys of a block besides where blocks are few.
 // Rows: bound by the power of the card and by what a tile takes of all units: 2048 tokens on 6001, 16 heads of 128 on 4, bf16: 122 us, 970 TFLOP/s,
 // matrix units 42 per cent busy at the 1.6 GHz that the clock falls to (a product of 8192^3 reaches 1260).  Leaving out the loads, or the
 // exponentials, gains a tenth each, and no order of instructions gains any (scores a tile ahead of the weights: the same; 64 rows a wave, 8 waves,
 // tiles of 32 keys: slower).  Of single tokens beside chunks (16 sequences, two of them with 500 new tokens: 54 us): one wave of four works for a
-// token's block, and parts are whole numbers of tiles in one round of workgroups.  Keys: bound by the reads of the cache (814 MB in 140 to 148 us, 5.5 TB/s) or, for short ones, by a chain of loads, tables,
-// pages, keys, of about 1 us each, behind the launch (4 tokens on 700, 12 heads of 64: 8.5 us).
-template <class T, int D, int W, int KT, int BUFS, bool KEYS, bool WALKS, int OCC>
+// token's block, and parts are whole numbers of tiles in one round of workgroups.  Keys: bound by the reads of the cache (814 MB in 137 to 148 us, 5.5
+// TB/s) or, for short ones, by a chain of loads, tables, pages, keys, of about 1 us each, behind the launch (4 tokens on 700, 12 heads of 64: 8.4 us).
+template <class T, int D, int W, int KT, bool KEYS, bool WALKS, int OCC>
 __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, PagePlan plan) {
     constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, KS = KT / 32, SUB = KT / kPageRows;
+    constexpr bool F32 = __is_same(T, SeqF32);
     constexpr int ROWS = KEYS ? 32 : 32 * W, TURN = KEYS ? W : 1;  // of a workgroup; from a wave's tile to its next one
     constexpr uint32_t kTile = KT * RB;
-    static_assert(KEYS || BUFS == 2, "a tile is on its way while the one in front of it is read");
     using Loader = PageLoader<RB, KT, KEYS ? 1 : W>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t lane = threadIdx.x & 63u, wave = W == 1 ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t hi = lane >> 5, c = lane & 31u;
-    const uint32_t base = lds_offset(lds) + (KEYS ? wave * 2u * BUFS * kTile : 0u);
+    const uint32_t base = lds_offset(lds) + (KEYS ? wave * 2u * kTile : 0u);
 
     // workgroup -> head of the keys (neighbours, so that each XCD has few of them), and a part of a block of rows, the last ones of which have most
     // keys, or a share of all sequences.  Rounds of as many workgroups as there are CUs go forwards and backwards in turn, so that a CU's come to one sum.
@@ -384,7 +392,7 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
             // Rows that no load fills hold zeros: their weights are zero, and zero times whatever else LDS may hold need not be.
             if (rows < Loader::kGroup) {
                 load.zero(to, g, lane);
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                lds_reads_done();  // or its writes
             }
             load.issue(lds_source(from + at, page_bytes_of(rows, token_bytes, RB)), to, g);
         }
@@ -431,7 +439,7 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
         for (int s = 0; s < NC; ++s) qf[s] = *reinterpret_cast<const u32x4*>(qp + 32 * s);
         // a negative scale goes into the queries, so that the largest product is the largest score
         if (a.scale < 0.f) {
-            constexpr uint32_t kSign = __is_same(T, SeqF32) ? 0x80000000u : 0x80008000u;
+            constexpr uint32_t kSign = F32 ? 0x80000000u : 0x80008000u;
 #pragma unroll
             for (int s = 0; s < NC; ++s) qf[s] ^= kSign;
         }
@@ -487,31 +495,40 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
         }
         return top_at == -__builtin_inff() ? 0.f : -top_at;
     };
+    constexpr int kTileLoads = Loader::kLoads * Loader::kGroups;
+    // Tile t, in the buffers of its parity.  Rows: the loads of the next one go to the other buffers in front of everything else.  Keys: they go to the
+    // same place as soon as a wave has read it, of 16-bit data all into registers in front of the softmax, of fp32 K in front of it and V behind.
     auto step = [&](auto parity, int t) {
         const uint32_t B = parity;
         const uint32_t kt = k_at + B * 2u * kTile, vt = v_at + B * 2u * kTile;
-        lds_loads_done();
-        if constexpr (!KEYS) __syncthreads();
-        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the reads of the tile in front, before the loads of the next one write there
-        if (BUFS == 2 && t + TURN < t1) {
-            issue(next, kp, left, k_at + (B ^ 1u) * 2u * kTile);
-            issue(next, vp, left, v_at + (B ^ 1u) * 2u * kTile);
-        }
-        if (BUFS == 2) left -= kStride;
-        if (!KEYS && t >= wave_end) {
-            next = look();
-            return;
+        if constexpr (KEYS && F32) loads_left<kTileLoads>();  // those of V may be on their way still
+        else lds_loads_done();
+        if constexpr (!KEYS) {
+            __syncthreads();
+            if (t + TURN < t1) {
+                issue(next, kp, left, k_at + (B ^ 1u) * 2u * kTile);
+                issue(next, vp, left, v_at + (B ^ 1u) * 2u * kTile);
+            }
+            left -= kStride;
+            if (t >= wave_end) {
+                next = look();
+                return;
+            }
         }
 
         f32x16 s[KS];
 #pragma unroll
         for (int k = 0; k < KS; ++k) seq_zero(s[k]);
         u32x4 v[2 * KS][NB];
-        if constexpr (__is_same(T, SeqF32)) {
+        if constexpr (F32) {
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
                 for (int x = 0; x < NC; ++x) s[k] = seq_dot<T>(row_reader.read(kt, x, k), qf[x], s[k]);
+            if constexpr (KEYS) {
+                lds_reads_done();
+                if (t + TURN < t1) issue(next, kp, left, k_at);
+            }
         } else {
             u32x4 f[KS][NC];
 #pragma unroll
@@ -525,6 +542,14 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
                 for (int k = 0; k < KS; ++k) s[k] = seq_dot<T>(f[k][x], qf[x], s[k]);
 #pragma unroll
             for (int h = 0; h < 2 * KS; ++h) page_values<T, D>(column_reader, v[h], vt, h);
+            if constexpr (KEYS) {
+                lds_reads_done();
+                if (t + TURN < t1) {
+                    issue(next, kp, left, k_at);
+                    issue(next, vp, left, v_at);
+                }
+                left -= kStride;
+            }
         }
         __builtin_amdgcn_sched_barrier(0);
         after = look();
@@ -536,7 +561,11 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
                 sum += s[k][r];
             }
         };
-        if constexpr (__is_same(T, SeqF32)) {
+        if constexpr (F32) {
+            if constexpr (KEYS) {
+                if (t + TURN < t1) loads_left<kTileLoads>();
+                else lds_loads_done();
+            }
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 weights(k);
@@ -556,19 +585,15 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
                 if (k + 1 < KS) weights(k + 1);
             }
         }
-        if constexpr (BUFS == 1) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (t + TURN < t1) {
-                issue(next, kp, left, k_at);
-                issue(next, vp, left, v_at);
-            }
+        if constexpr (KEYS && F32) {
+            lds_reads_done();
+            if (t + TURN < t1) issue(next, vp, left, v_at);
             left -= kStride;
         }
         next = after;
     };
     if constexpr (KEYS) {
-        uint32_t parity = 0;
-        for (int t = mine0; t < t1; t += TURN, parity ^= BUFS - 1u) step(parity, t);
+        for (int t = mine0; t < t1; t += TURN) step(std::integral_constant<uint32_t, 0>{}, t);
     } else {
         for (int t = mine0; t < t1; t += 2) {
             step(std::integral_constant<uint32_t, 0>{}, t);
@@ -737,16 +762,16 @@ __global__ void __launch_bounds__(256) page_join_kernel(PageArgs a, PagePlan pla
 // Tiles, waves, and waves of a SIMD that the registers are held to, as in the attention of whole sequences.
 constexpr int page_tile_keys(int row_bytes, bool keys) { return row_bytes >= 512 || keys ? 32 : 64; }
 constexpr int page_waves(int row_bytes, bool keys) { return keys ? seq_keys_waves(row_bytes) : 4; }
-// Tiles of K and of V that a wave (workgroup) has room for: two, so that one is on its way while the other is read, or one where two leave a CU no
-// more than two waves (fp32 heads of 128, 16 sequences of up to 4000 keys, 8 heads: 138 us with one, 172 with two).
-constexpr int page_bufs(int row_bytes, bool keys) { return keys && row_bytes >= 512 ? 1 : 2; }
+// Workgroups of a CU that share out all keys: as many as hide the loads of a wave's one tile (fp32 heads of 128, 16 sequences of up to 4000 keys, 8 heads:
+// two 124 us, four 112; bf16, 32 of up to 8192: 150 and 153).
+constexpr int page_walkers(int row_bytes) { return row_bytes >= 512 ? 4 : 2; }
 constexpr int page_occupancy(int row_bytes, bool keys) { return row_bytes == 128 && !keys ? 3 : 1; }
 
 template <class T, int D, bool KEYS, bool WALKS>
 hipError_t launch(const PageArgs& a, const PagePlan& plan, hipStream_t s) {
     constexpr int RB = D * SeqSize<T>::value, W = page_waves(RB, KEYS), KT = page_tile_keys(RB, KEYS), ROWS = KEYS ? 32 : 32 * W;
-    constexpr size_t tiles = 2 * (size_t)page_bufs(RB, KEYS) * KT * RB * (KEYS ? W : 1), sums = KEYS && W > 1 ? (size_t)W * 32 * (4 * (D + 4) + 8) : 0, lds = tiles > sums ? tiles : sums;
-    auto* const kernel = &page_forward_kernel<T, D, W, KT, page_bufs(RB, KEYS), KEYS, WALKS, page_occupancy(RB, KEYS)>;
+    constexpr size_t tiles = (size_t)KT * RB * (KEYS ? 2 * W : 4), sums = KEYS && W > 1 ? (size_t)W * 32 * (4 * (D + 4) + 8) : 0, lds = tiles > sums ? tiles : sums;
+    auto* const kernel = &page_forward_kernel<T, D, W, KT, KEYS, WALKS, page_occupancy(RB, KEYS)>;
     hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), lds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(plan.grid), dim3(64 * W), lds, s, a, plan);
@@ -785,8 +810,9 @@ bool page_plan(const PageArgs& a, PagePlan& f) {
     f.least = f.keys ? 2 * W : a.dtype == 0 ? 1 : 2;
     if (tiles > f.alone) {
         const bool same = (long long)a.N * a.most == a.rows;  // all sequences have the same number of new tokens
-        if (f.keys && a.N <= kMostShared && base < 4.0 * cus && 2 * cus / a.KV >= 2 && base * (double)tiles >= kWorth * W * 2.0 * cus && (double)a.N * (double)tiles < 1.0e9) {
-            f.workers = 2 * cus / a.KV;
+        const int fit = page_walkers(RB);
+        if (f.keys && a.N <= kMostShared && base < 2.0 * fit * cus && fit * cus / a.KV >= 2 && base * (double)tiles >= kWorth * W * fit * cus && (double)a.N * (double)tiles < 1.0e9) {
+            f.workers = fit * cus / a.KV;
             f.lane_sequences = (a.N + 63) / 64;
         } else if (!f.keys && !same && a.N <= 64 && base < 2.0 * cus && base * (double)tiles > 2.0 * cus * f.least && (double)blocks * (double)tiles < 1.0e9) {
             f.target = 2 * cus > a.KV ? 2 * cus / a.KV : 1;
