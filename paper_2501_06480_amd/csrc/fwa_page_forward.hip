@@ -23,6 +23,9 @@ constexpr int kFewRows = 32;  // rows (new tokens times heads of a group) up to 
 constexpr double kWorth = 8.0;
 constexpr int kMostShared = 1024;
 constexpr int kLengths = 16;  // lengths of parts that are tried at most
+// Tiles of a part up to which blocks of different sequences are cut for one workgroup on each CU and not two, if they are few enough to make four parts
+// each (4 sequences with up to 140 new tokens on 18000, one head: 35 us with two, 28 with one; 52 with up to 23 on 12000, 3 heads: 76 and 163).
+constexpr int kShort = 16;
 
 // How a call is laid out on the device.
 struct PagePlan {
@@ -44,6 +47,7 @@ struct PagePlan {
     int* joins;       // [block, part or worker][kv][8]: parts (0: nothing to join), first token, row of the block's first, rows of the sequence, rows of
                       // parts: the first part's, the second's, from one to the next
     int joined;       // blocks, parts or workers
+    bool many;        // blocks of rows may have many parts
 };
 
 // A block of a sequence's rows (token-major: row r is token r / group, head r % group of the group).
@@ -134,9 +138,11 @@ __device__ __forceinline__ bool page_job(const PageArgs& a, const PagePlan& plan
     const int from = page_offset(offset, a.rows), count = lane < a.N ? page_count(from, page_offset(next_offset, a.rows), a.most) : 0;
     const int blocks = (int)(((uint32_t)count * (uint32_t)plan.group + ROWS - 1u) / ROWS);
     const int tiles = (page_keys(page_length(length), count, a.width, a.page_size) + KT - 1) / KT;
-    j.length = page_length_first(__builtin_amdgcn_readlane(page_scan(blocks * tiles), 63), plan.target, plan.least);
+    const int work = __builtin_amdgcn_readlane(page_scan(blocks * tiles), 63), half = (plan.target + 1) / 2;
+    const int target = work <= kShort * half && 4 * __builtin_amdgcn_readlane(page_scan(blocks), 63) <= half ? half : plan.target;
+    j.length = page_length_first(work, target, plan.least);
     int parts = page_parts(tiles, j.length, plan.alone);
-    for (int turn = 0; turn < kLengths && __builtin_amdgcn_readlane(page_scan(blocks * parts), 63) > plan.target; ++turn) {
+    for (int turn = 0; turn < kLengths && __builtin_amdgcn_readlane(page_scan(blocks * parts), 63) > target; ++turn) {
         j.length = page_length_next(j.length);
         parts = page_parts(tiles, j.length, plan.alone);
     }
@@ -689,14 +695,14 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     }
 }
 
-// Joins the parts of blocks whose keys are shared out: a thread has four channels of a row, 16 parts at a time, of blocks of few rows (and as many as
-// 64 parts: one sequence of 32768 keys, 39 us in all, 58 with two at a time), or of some of a workgroup's 32 rows, with the loads of all on the way
-// together (512 blocks of 128 rows of 128 channels, 33 MB: 8.9 us, 10.4 with a row).  Few rows: 4 us, a launch and two loads one behind the other.
-template <class T, int D, int ROWS>
+// Joins the parts of blocks whose keys are shared out.  MANY: a thread has four channels of a row, 16 parts at a time, for blocks of few rows or of
+// many parts (one sequence of 32768 keys: 39 us in all, 58 with two at a time; 4 sequences with up to 140 new tokens on 18000, one head: 35 and 75);
+// otherwise of some of a workgroup's 32 rows, with the loads of all on the way together (512 blocks of 128 rows of 128 channels, 33 MB: 8.9 us, 10.4
+// with a row).  Few rows: 4 us, a launch and two loads one behind the other.
+template <class T, int D, int ROWS, bool MANY>
 __global__ void __launch_bounds__(256) page_join_kernel(PageArgs a, PagePlan plan) {
-    constexpr bool KEYS = ROWS == 32;
-    constexpr int E = SeqSize<T>::value, kThreads = D / 4, kRows = 256 / kThreads, kMine = KEYS ? 1 : 32 / kRows, kTurns = ROWS / (kRows * kMine);
-    constexpr int kAtOnce = KEYS ? 16 : 8 / kMine;  // parts of a row
+    constexpr int E = SeqSize<T>::value, kThreads = D / 4, kRows = 256 / kThreads, kMine = MANY ? 1 : 32 / kRows, kTurns = ROWS / (kRows * kMine);
+    constexpr int kAtOnce = MANY ? 16 : 8 / kMine;  // parts of a row
     const uint32_t unit = blockIdx.x / kTurns, turn = blockIdx.x - unit * kTurns, hk = unit - fastdiv(unit, plan.by_kv) * plan.by_kv.d;
     const i32x4 known = *reinterpret_cast<const i32x4*>(plan.joins + 8 * (size_t)unit), rows = *reinterpret_cast<const i32x4*>(plan.joins + 8 * (size_t)unit + 4);
     const int parts = known[0], channel = 4 * (int)(threadIdx.x % kThreads);
@@ -777,18 +783,30 @@ hipError_t launch(const PageArgs& a, const PagePlan& plan, hipStream_t s) {
     hipLaunchKernelGGL(kernel, dim3(plan.grid), dim3(64 * W), lds, s, a, plan);
     e = hipGetLastError();
     if (e != hipSuccess || plan.joined == 0) return e;
-    hipLaunchKernelGGL((page_join_kernel<T, D, ROWS>), dim3((unsigned)plan.joined * (unsigned)a.KV * (unsigned)(KEYS ? 32 / (256 / (D / 4)) : ROWS / 32)), dim3(256), 0, s, a, plan);
+    const unsigned units = (unsigned)plan.joined * (unsigned)a.KV;
+    if (KEYS || plan.many) hipLaunchKernelGGL((page_join_kernel<T, D, ROWS, true>), dim3(units * (unsigned)(ROWS / (256 / (D / 4)))), dim3(256), 0, s, a, plan);
+    else hipLaunchKernelGGL((page_join_kernel<T, D, ROWS, false>), dim3(units * (unsigned)(ROWS / 32)), dim3(256), 0, s, a, plan);
     return hipGetLastError();
+}
+
+// Microseconds that blocks of rows of up to `tiles` tiles take in `splits` parts each: tiles of one workgroup on a CU or of two, the join's launch, its
+// reads of the parts and their writes.  Measured over drawn calls; what counts is the difference between few splits and many.
+double page_rows_time(const PageArgs& a, int rows, double blocks, long long tiles, long long splits, int cus) {
+    const double one = a.dtype == 0 ? (a.D == 32 ? 2.3 : 4.0) : 0.8 + a.D / 256.0, two = a.dtype == 0 ? (a.D == 32 ? 3.6 : 7.0) : 0.9 + a.D / 98.0;
+    const double n = blocks * (double)splits, rounds = (double)(long long)((n + 2.0 * cus - 1.0) / (2.0 * cus));
+    return (double)((tiles + splits - 1) / splits) * (n <= cus ? one : two * rounds) + (splits > 1 ? 5.0 + n * rows * a.D * 8.0 / 7.0e6 + (double)splits / 16.0 : 0.0);
 }
 
 // How a call is laid out, from what the host knows: the waves share out the keys where no sequence has more than a few rows.  Where there are too few
 // blocks for the device, its workgroups share out the keys besides, and a second launch joins the parts, but for caches that are too short to be
 // worth that: the join takes as long as about `alone` tiles (704 keys, 6 tiles a wave: 9.0 us whole, 10.4 in parts of two).  Parts are no shorter
 // than `least` tiles of a wave (8 sequences of up to 2000 keys: two tiles 16.5 us, four 18.1; fp32 rows, whose tiles take four times as long, one
-// tile 14.5 us, four 20.1).  How many: all blocks of sequences with the same number of new tokens have as many as make two workgroups for each CU (2048
-// tokens: 131 us, with four 142), four where the keys are all there is to do.  Blocks of sequences that bring different numbers, up to 64 of them, are cut
-// into parts of one length, no more than two for each CU, which the device finds from all lengths (two chunks of 500 beside 14 tokens: 63 us, 70
-// with as many parts for each block; 16 chunks of 61: 49 and 65; causal prompts of one length cut like that: 101 whole, 118 to 160 in parts).
+// tile 14.5 us, four 20.1; 26 sequences of up to 370 fp32 keys, 3 heads of 64: two 24 us, one 14).  How many: of blocks of sequences with the same number
+// of new tokens as many as make one or two workgroups for each CU, whichever page_rows_time has as the shorter (2048 tokens on 6001: two 131 us, four 142;
+// 9 sequences of 612, one head: one 21, two 26), four where the keys are all there is to do.  Blocks of sequences that bring different numbers, up to
+// 64 of them, are cut into parts of one length, no more than one or two for each CU, which the device finds from all lengths (two chunks of 500 beside
+// 14 tokens: 63 us, 70 with as many parts for each block; 16 chunks of 61: 49 and 65; causal prompts of one length cut like that: 101 whole, 118 to
+// 160 in parts).
 bool page_plan(const PageArgs& a, PagePlan& f) {
     const int size = a.dtype == 0 ? 4 : 2, RB = a.D * size, G = a.H / a.KV, cus = cu_count();
     const long long most_rows = (long long)a.most * G, capacity = (long long)a.width * a.page_size;
@@ -806,23 +824,33 @@ bool page_plan(const PageArgs& a, PagePlan& f) {
     f.blocks = (int)blocks;
     f.splits = 1;
     const long long tiles = (capacity + KT - 1) / KT;
-    f.alone = f.keys ? 6 * W : a.dtype == 0 ? 1 : 4;
-    f.least = f.keys ? 2 * W : a.dtype == 0 ? 1 : 2;
+    const bool slow = a.dtype == 0 && RB >= 256;  // a wave's tile takes 2 us or more of fp32 products
+    f.alone = f.keys ? (slow ? 2 : 6) * W : a.dtype == 0 ? 1 : 4;
+    f.least = f.keys ? (slow ? 1 : 2) * W : a.dtype == 0 ? 1 : 2;
     if (tiles > f.alone) {
         const bool same = (long long)a.N * a.most == a.rows;  // all sequences have the same number of new tokens
         const int fit = page_walkers(RB);
         if (f.keys && a.N <= kMostShared && base < 2.0 * fit * cus && fit * cus / a.KV >= 2 && base * (double)tiles >= kWorth * W * fit * cus && (double)a.N * (double)tiles < 1.0e9) {
             f.workers = fit * cus / a.KV;
             f.lane_sequences = (a.N + 63) / 64;
-        } else if (!f.keys && !same && a.N <= 64 && base < 2.0 * cus && base * (double)tiles > 2.0 * cus * f.least && (double)blocks * (double)tiles < 1.0e9) {
+        } else if (!f.keys && !same && a.N <= 64 && base < 2.0 * cus && base * (double)tiles > 1.0 * cus * f.least && (double)blocks * (double)tiles < 1.0e9) {
             f.target = 2 * cus > a.KV ? 2 * cus / a.KV : 1;
             f.blocks += f.target;
         } else {
-            long long splits = (long long)((f.keys || !same ? 4.0 : 2.0) * cus / base);
-            if (splits > tiles / f.least) splits = tiles / f.least;
+            const long long most = tiles / f.least < 64 ? tiles / f.least : 64;
+            auto cut = [&](double wanted) { const long long x = (long long)(wanted * cus / base); return x < most ? x : most; };
+            long long splits = 1;
+            if (f.keys) {
+                splits = cut(4.0);
+            } else {
+                for (const double wanted : {1.0, 2.0, 4.0})
+                    if ((wanted < 4.0 || !same) && cut(wanted) > splits && page_rows_time(a, f.rows, base, tiles, cut(wanted), cus) < page_rows_time(a, f.rows, base, tiles, splits, cus))
+                        splits = cut(wanted);
+            }
             f.splits = splits < 1 ? 1 : splits > 64 ? 64 : (int)splits;
         }
     }
+    f.many = f.target > 0 ? f.target >= 4 * blocks : f.splits >= 4;
     f.joined = f.workers > 0 ? f.workers : f.splits > 1 || f.target > 0 ? f.blocks : 0;
     f.grid = (unsigned)(f.workers > 0 ? f.workers : f.blocks * f.splits) * (unsigned)a.KV;
     f.slots = f.workers > 0 ? (size_t)f.workers * a.KV * 2 * f.rows : f.joined > 0 ? (size_t)f.blocks * a.KV * f.splits * f.rows : 0;

@@ -105,6 +105,15 @@ def test_chunks_of_different_lengths(dtype, H, KV, d, size, causal, news, length
     assert torch.equal(got[0], again[0]) and torch.equal(got[1][rows], again[1][rows])
 
 
+@pytest.mark.parametrize("dtype,H,KV,d,new,length", [(BF16, 1, 1, 64, 40, 6000), (F16, 2, 1, 128, 70, 4000), (F32, 1, 1, 128, 35, 2500), (F32, 3, 1, 32, 20, 5000), (BF16, 1, 1, 32, 140, 3000)])
+def test_many_parts_of_few_blocks(dtype, H, KV, d, new, length):
+    """Few rows too many for the form for few, against a long cache: a block in dozens of parts, of one sequence and beside a short one."""
+    x, _ = make(dtype, [new], [length], H, KV, d, 16)
+    compare(x, H, d ** -0.5, f"{dtype} {new} on {length} d{d}", most_new=new)
+    x, _ = make(dtype, [new, 7], [length, 300], H, KV, d, 16)
+    compare(x, H, d ** -0.5, f"{dtype} {new} and 7 on {length} d{d}", most_new=new)
+
+
 def test_mixed_batches_of_many_sequences():
     """More sequences than lanes: their blocks are found by a search of two steps."""
     g = torch.Generator().manual_seed(5)
