@@ -16,7 +16,10 @@ namespace {
 
 // A row's reference moves when a score exceeds it by more than this, as in the attention of whole sequences.
 constexpr float kSlack = 6.f;
-constexpr int kFewRows = 32;  // rows (new tokens times heads of a group) up to which the waves of a workgroup share out the keys
+// Rows (new tokens times heads of a group) up to which the waves of a workgroup share out the keys: a block of 32, or of fp32 data, whose products take
+// longer than their tiles' way, two, since of 128 rows' waves half would have none (45 sequences of 5 tokens on up to 14834 keys, 3 heads of 32 with 8 of
+// queries each: 375 us in a block of 128 rows, 182 in two of 32; bf16, 8000 keys: 53 and 62).
+constexpr int few_rows(int dtype) { return dtype == 0 ? 64 : 32; }
 // Tiles of a wave from which an even share of all keys is worth finding, which takes a workgroup about 3 us (32 sequences of 4096 to 8192 keys, 8
 // heads of 128, bf16, 250 tiles a wave: 158 us in parts of each sequence, 150 in even shares; 8 sequences of 1000 to 2000, 2 heads of 64, 2 tiles a
 // wave: 16.5 and 18.3), and sequences up to which it is: each lane adds up 16 of them at most.
@@ -811,7 +814,7 @@ bool page_plan(const PageArgs& a, PagePlan& f) {
     const int size = a.dtype == 0 ? 4 : 2, RB = a.D * size, G = a.H / a.KV, cus = cu_count();
     const long long most_rows = (long long)a.most * G, capacity = (long long)a.width * a.page_size;
     f = PagePlan{};
-    f.keys = most_rows <= kFewRows;
+    f.keys = most_rows <= few_rows(a.dtype);
     const int KT = page_tile_keys(RB, f.keys), W = page_waves(RB, f.keys);
     f.rows = f.keys ? 32 : 32 * W;
     f.group = G;
@@ -830,7 +833,7 @@ bool page_plan(const PageArgs& a, PagePlan& f) {
     if (tiles > f.alone) {
         const bool same = (long long)a.N * a.most == a.rows;  // all sequences have the same number of new tokens
         const int fit = page_walkers(RB);
-        if (f.keys && a.N <= kMostShared && base < 2.0 * fit * cus && fit * cus / a.KV >= 2 && base * (double)tiles >= kWorth * W * fit * cus && (double)a.N * (double)tiles < 1.0e9) {
+        if (f.keys && f.each == 1 && a.N <= kMostShared && base < 2.0 * fit * cus && fit * cus / a.KV >= 2 && base * (double)tiles >= kWorth * W * fit * cus && (double)a.N * (double)tiles < 1.0e9) {
             f.workers = fit * cus / a.KV;
             f.lane_sequences = (a.N + 63) / 64;
         } else if (!f.keys && !same && a.N <= 64 && base < 2.0 * cus && base * (double)tiles > 1.0 * cus * f.least && (double)blocks * (double)tiles < 1.0e9) {

@@ -114,6 +114,15 @@ def test_many_parts_of_few_blocks(dtype, H, KV, d, new, length):
     compare(x, H, d ** -0.5, f"{dtype} {new} and 7 on {length} d{d}", most_new=new)
 
 
+@pytest.mark.parametrize("H,KV,d", [(2, 1, 32), (6, 3, 64), (2, 2, 128)])
+@pytest.mark.parametrize("news,lengths,wider", [([32, 32], [500, 20], 0), ([30, 1, 0, 20], [300, 1500, 9, 0], 0), ([17, 32, 5], [0, 900, 3000], 100), ([3] * 66 + [31], [0, 40, 100] * 22 + [200], 0)])
+def test_two_blocks_of_few_fp32_rows(H, KV, d, news, lengths, wider):
+    """32 to 64 rows of a sequence, in two blocks whose waves share out the keys: alone, beside others of one block, with and without parts, more sequences than lanes."""
+    x, _ = make(F32, news, lengths, H, KV, d, 16, spare=(1, 2), wider=wider)
+    compare(x, H, d ** -0.5, f"{news[:4]} {H}/{KV} d{d}", most_new=max(news))
+    compare(x, H, d ** -0.5, f"{news[:4]} {H}/{KV} d{d} all", most_new=max(news), causal=False)
+
+
 def test_mixed_batches_of_many_sequences():
     """More sequences than lanes: their blocks are found by a search of two steps."""
     g = torch.Generator().manual_seed(5)
