@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
         slot0 = (2u * unit + (p.place > 0 ? 1u : 0u)) * ROWS;
         second = 2u * (unit + (uint32_t)a.KV) * ROWS;
     } else if (!KEYS && plan.target > 0) {
-        const PageCut cut = page_cut(tiles, job.length, plan.alone, job.parts, job.split);
+        const PageCut cut = page_cut(tiles, job.length, plan.alone, page_parts_room(job.parts, (int)block, job.split, plan.blocks), job.split);
         if (job.split >= cut.parts) {
             if (threadIdx.x == 0) plan.joins[8 * (size_t)unit] = 0;
             return;

@@ -72,6 +72,13 @@ FWA_PAGE_FN int page_length_first(int total, int target, int least) {
     return length > least ? length : least;
 }
 FWA_PAGE_FN int page_length_next(int length) { return length + 1 + length / 32; }
+// Parts that a block has room for, of the `parts` that its sequence's tiles make: its jobs lie one behind the other, this one being the `split`-th, and there
+// are `jobs` in all.  Offsets that fall bring more than the launch has; a block that would reach beyond it is cut into fewer parts, so that each part that the
+// join reads is one that a workgroup leaves.
+FWA_PAGE_FN int page_parts_room(int parts, int job, int split, int jobs) {
+    const int room = jobs - (job - split);
+    return parts < room ? parts : room;
+}
 // Tiles of part `split` of a block whose sequence has up to `most` parts a block; parts: how many this one has, all of them one behind the other.
 struct PageCut {
     int from, to, parts;
