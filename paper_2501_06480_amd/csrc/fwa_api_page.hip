@@ -202,7 +202,8 @@ int fwa_page_append(const void* k, const void* v, void* k_pages, void* v_pages, 
 
 size_t fwa_page_forward_workspace_bytes(int64_t rows, int64_t N, int heads, int kv_heads, int d, int page_size, int width, int most_new, int dtype) {
     fwa::PageArgs a = {};
-    const int rc = check_attention(a, rows, N, heads, kv_heads, d, 1, page_size, (int64_t)kv_heads * page_size * d, d, (int64_t)page_size * d, width, most_new, dtype);
+    // The cache's strides are not known here and do not matter: heads one behind the other in one page, whose distance to the next is none.
+    const int rc = check_attention(a, rows, N, heads, kv_heads, d, 1, page_size, 0, d, (int64_t)page_size * d, width, most_new, dtype);
     if (rc != FWA_OK || rows == 0 || N == 0 || a.most == 0) return 0;
     return fwa::page_forward_workspace(a);
 }
