@@ -303,7 +303,7 @@ size_t fwa_sequence_backward_workspace_bytes(int64_t N, int Lq, int Lk, int head
  *   y           : out, like x, rows ld_y apart; may be x itself (the same address and stride), else no byte of it
  *   positions   : [position_rows, axes] int32; row r of x has row r mod position_rows of them (position_rows = L for all sequences of [N, L])
  *   frequencies : [pairs] fp32, radians a position
- *   axis_of     : [pairs] int32, or NULL: all pairs the first axis.  A pair with an axis outside [0, axes) is not turned.
+ *   axis_of     : [pairs] int32, or NULL: all pairs the first axis.  A pair with an axis outside [0, axes) stays as it is.
  *   inverse     : nonzero: by the negative angle, which is the inverse, and the gradient of x from that of y
  * d from 1 to 512, 0 <= pairs <= d / 2, axes <= 16, dtype FWA_F32, FWA_BF16 or FWA_F16, rows * heads * d / 2 below 2e9.  Angles are formed in 64 bits and
  * reduced to a turn there, so far positions lose nothing (2^20 of frequency 1: 1e-7 of the result, as near ones); the rotation is fp32, rounded once.
