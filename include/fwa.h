@@ -345,7 +345,8 @@ int fwa_page_append(const void* k, const void* v, void* k_pages, void* v_pages, 
  * Attention of the new tokens over the cache that already holds them: token i of sequence n sees the keys at places up to lengths[n] + i
  * (causal nonzero) or all lengths[n] + new ones, of those within width * page_size whose page exists.
  *   q, o      : [rows, heads * d], rows ld_q resp. ld_o apart; kv_heads divides heads
- *   most_new  : no sequence has more new tokens; what goes beyond is not computed and its rows left as they were.  The smaller this is, the
+ *   most_new  : no sequence has more new tokens.  Of one that has, the first most_new are all there are: the others are not computed, their
+ *               rows are left as they were, and (causal zero) nobody sees their keys, whatever the cache holds.  The smaller this is, the
  *               better the call can be laid out (1 for single tokens); rows is always enough.
  *   stats     : NULL, or out [rows, heads, 2] fp32, the row statistics as in fwa_sequence_forward
  *   workspace : device scratch of at least fwa_page_forward_workspace_bytes(...) bytes, 16-byte aligned.  It goes by the arguments on the host, the

@@ -191,7 +191,7 @@ struct PageArgs {
     long long ldq, ldo;
     // attention
     float* stats;        // [rows, H, 2] or nullptr
-    int most;            // new tokens of a sequence that count
+    int most;            // new tokens of a sequence that count, as rows and as keys
     int causal;
     float scale;
     // append: o is the rotated q

@@ -61,7 +61,7 @@ struct PageBlock {
     int kend;           // keys up to this one are seen by a row of the block
 };
 
-// What is known of a sequence from its entries in the tables, its blocks left open
+// What is known of a sequence from its entries in the tables, its blocks left open.  Of more new tokens than the caller told of, the first are all there are.
 __device__ __forceinline__ void page_sequence(const PageArgs& a, const PagePlan& plan, int n, int offset, int next_offset, int length, PageBlock& b) {
     b.n = n;
     b.begin = page_offset(offset, a.rows);
