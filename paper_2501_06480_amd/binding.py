@@ -510,6 +510,8 @@ def fwa_page_forward(q, k_pages, v_pages, page_table, offsets, lengths, heads: i
     and single tokens go in one call.  `most_new`: no sequence has more new tokens (default: T); tokens beyond are not computed, and not seen either where the
     call is not `causal`.  It is worth giving: 32 single tokens on up to 8192 keys, 32 heads of 128 on 8, bf16, take 149 us with 1 and 169 us without.  Returns o, or (o, stats)
     with the row statistics [T, heads, 2] as of ``fwa_sequence_forward``; rows outside the offsets are not written."""
+    if most_new is not None and most_new < 0:
+        raise ValueError("most_new must not be negative")
     args = (q, k_pages, v_pages, page_table, offsets, lengths, int(heads), float(scale), -1 if most_new is None else int(most_new), bool(causal),
             bool(want_stats), out, workspace)
     call = (_native_mod or _native()).page_forward
