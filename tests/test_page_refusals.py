@@ -14,3 +14,15 @@ def test_a_negative_number_of_new_tokens_is_refused():
     for most in (None, 3):
         with pytest.raises(TypeError):  # not on a GPU
             fwa.fwa_page_forward(*args, most_new=most)
+
+
+def test_frequencies_that_want_a_gradient_are_refused():
+    """They would be left without one in silence."""
+    from paper_2501_06480_amd import autograd
+    x, positions, f = torch.zeros(1, 4, 128), torch.zeros(4, 1, dtype=torch.int32), torch.nn.Parameter(torch.ones(32))
+    with pytest.raises(NotImplementedError, match="frequencies"):
+        autograd.rotary(x, 2, positions, f)
+    with torch.no_grad(), pytest.raises(TypeError):  # not on a GPU
+        autograd.rotary(x, 2, positions, f)
+    with pytest.raises(TypeError):
+        autograd.rotary(x, 2, positions, f.detach())
