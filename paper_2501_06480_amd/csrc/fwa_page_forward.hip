@@ -352,16 +352,13 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
 
     // Pages are looked up two tiles ahead of their use, so that nothing waits for the scalar loads, and in steps from group to group, without a
     // division: a group's place is an entry of the table and a row of that page.
-    struct Place {
-        int index, slot;
-    };
     const int page_size = a.page_size, last_index = klen > 0 ? (int)fastdiv((uint32_t)(klen - 1) / (uint32_t)kPageRows, plan.by_sub) : 0;
     auto place_of = [&](int key) {
         const int index = (int)fastdiv((uint32_t)key / (uint32_t)kPageRows, plan.by_sub);
-        return Place{index, key - index * page_size};
+        return PageSpot{index, key - index * page_size};
     };
     // (entries behind the sequence's last are read and not used)
-    auto find = [&](int index) { return seq_constant(page_row, index < a.width ? index : a.width - 1); };
+    auto find = [&](int index) { return seq_constant(page_row, page_entry(index, a.width)); };
     struct Group {
         int page, slot;
     };
@@ -370,26 +367,18 @@ __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, P
     };
     // what one wave's tiles are apart, and groups of a tile
     constexpr int kStride = TURN * KT;
-    const Place stride = place_of(kStride);
-    auto advance = [&](Place& p, int index, int slot) {
-        p.index += index;
-        p.slot += slot;
-        if (p.slot >= page_size) {
-            p.slot -= page_size;
-            ++p.index;
-        }
-    };
+    const PageSpot stride = place_of(kStride);
     const int mine0 = KEYS ? t0 + (int)wave : t0;
-    Place ahead = place_of(mine0 * KT + load.row);
+    PageSpot ahead = place_of(mine0 * KT + load.row);
     auto look = [&]() {
         Groups r;
-        Place p = ahead;
+        PageSpot p = ahead;
 #pragma unroll
         for (int g = 0; g < Loader::kGroups; ++g) {
             r.g[g] = Group{find(p.index), p.slot};
-            if (g + 1 < Loader::kGroups) advance(p, 0, Loader::kGroup);
+            if (g + 1 < Loader::kGroups) page_advance(p, 0, Loader::kGroup, page_size);
         }
-        advance(ahead, stride.index, stride.slot);
+        page_advance(ahead, stride.index, stride.slot, page_size);
         return r;
     };
     // rows of a tile of K or V from the first of this wave's on, of which there are `left`

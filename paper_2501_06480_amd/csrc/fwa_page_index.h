@@ -32,6 +32,20 @@ FWA_PAGE_FN int page_group(int key, int keys, int group, bool exists) {
     const int left = keys - key;
     return !exists || left <= 0 ? 0 : (left < group ? left : group);
 }
+// A way over the keys of a sequence in steps, without a division for each: an entry of its row of the table, and a row of that page.  A step is given as the
+// entries and rows that it is long, fewer rows than a page has.  What is looked up ahead of its use may lie behind the last entry, which stands for it then.
+struct PageSpot {
+    int index, slot;
+};
+FWA_PAGE_FN void page_advance(PageSpot& p, int index, int slot, int page_size) {
+    p.index += index;
+    p.slot += slot;
+    if (p.slot >= page_size) {
+        p.slot -= page_size;
+        ++p.index;
+    }
+}
+FWA_PAGE_FN int page_entry(int index, int width) { return index < width ? index : width - 1; }
 // Bytes from the base of a head to a row of a page.
 FWA_PAGE_FN uint64_t page_place(uint32_t page, uint32_t slot, uint32_t page_bytes, uint32_t token_bytes) { return (uint64_t)page * page_bytes + (uint64_t)slot * token_bytes; }
 // Bytes from there that the loads of `rows` rows may touch.
