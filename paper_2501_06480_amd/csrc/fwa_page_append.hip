@@ -23,8 +23,8 @@ constexpr uint32_t kNowhere = 0xffffffffu;
 
 // Units as in the rotary kernel, a token's heads of queries, keys and values one behind the other, with their vectors on the way while the places are
 // looked up: sequence and length in LDS (or, of more sequences than threads, from a sample of the offsets in LDS on), then the page, beside the
-// cosines. Bound by memory for long calls (4001 tokens of 24 heads of 128, half: 49 MB in 10.9 us, 4.5 TB/s; 6439 of 36 of 64: 59 MB in 12.3), by its
-// chain of loads for short ones (16 tokens: 4.0 us).
+// cosines. Bound by memory for long calls (4001 tokens of 24 heads of 128, half: kernel 11.8 us for 49 MB, 4.2 TB/s, fp32 19.7 for 98, 5.0 TB/s; 6439 of 36
+// of 64, bf16: 13.0 for 59), by its chain of loads for short ones (16 tokens: 3.9 us).
 template <class T, int V, int UNITS, int THREADS>
 __global__ void __launch_bounds__(THREADS) page_append_kernel(PageArgs a, AppendPlan plan) {
     constexpr int E = SeqSize<T>::value, U = UNITS / THREADS;
@@ -145,7 +145,7 @@ hipError_t launch(const PageArgs& a, AppendPlan plan, hipStream_t s) {
 template <class T, int V>
 hipError_t launch(const PageArgs& a, const AppendPlan& plan, hipStream_t s) {
     // Four units a thread where that leaves two workgroups for each CU: half as many searches (6439 tokens of 36 heads of 64, 0.9 million units,
-    // bf16: 15.0 us with two, 13.3 with four; a rotation of 0.2 million units, 7.6 and 8.1).
+    // bf16: calls one behind the other 15.0 us with two, 13.1 with four; a rotation of 0.2 million units, 7.6 and 8.1).
     if (rotary_small(plan.total)) return launch<T, V, RotaryShape::kSmall, RotaryShape::kSmall>(a, plan, s);
     return plan.total <= 512 * 1024 ? launch<T, V, RotaryShape::kLarge, 256>(a, plan, s) : launch<T, V, 2 * RotaryShape::kLarge, 256>(a, plan, s);
 }

@@ -215,7 +215,9 @@ __device__ __forceinline__ void page_values(const SeqColumnReader<T, D>& reader,
         v[b] = u32x4{p.x, p.y, q.x, q.y};
     }
 }
-// Half `h` of a tile of weights, rounded: the operand of a product over its 16 keys.
+// Half `h` of a tile of weights, rounded: the operand of a product over its 16 keys.  The matrix instruction has both operands in the data's
+// type, so a weight loses up to half a step of it, once; the sums are of the weights as they were.  Outputs are off by 2.3e-3 of their size in all (bf16; 1.7e-3 with
+// weights in 32 bits; half: 2.8e-4, 2.1e-4).  A second product, of what the rounding leaves, would be half as many matrix instructions again.
 template <class T>
 __device__ __forceinline__ u32x4 page_weights(const f32x16& w, int h) {
     constexpr bool F16 = __is_same(T, SeqF16);
@@ -260,12 +262,12 @@ struct PageLoader {
 // read.  KEYS: all have the same 32 rows and every W-th tile each, in one place for each wave without a barrier, and join what they have at the end; a
 // tile's loads follow its reads, beside softmax and products (two places each: 10.6 us for 300 sequences of 100 keys, 7.5 with one, which leaves a CU
 // room for more workgroups; 155 and 151 for 128 of up to 2000).  Workgroups share out the keys of a block besides where blocks are few.
-// Rows: bound by the power of the card and by what a tile takes of all units: 2048 tokens on 6001, 16 heads of 128 on 4, bf16: 122 us, 970 TFLOP/s,
-// matrix units 42 per cent busy at the 1.6 GHz that the clock falls to (a product of 8192^3 reaches 1260).  Leaving out the loads, or the
-// exponentials, gains a tenth each, and no order of instructions gains any (scores a tile ahead of the weights: the same; 64 rows a wave, 8 waves,
-// tiles of 32 keys: slower).  Of single tokens beside chunks (16 sequences, two of them with 500 new tokens: 54 us): one wave of four works for a
-// token's block, and parts are whole numbers of tiles in one round of workgroups.  Keys: bound by the reads of the cache (814 MB in 137 to 148 us, 5.5
-// TB/s) or, for short ones, by a chain of loads, tables, pages, keys, of about 1 us each, behind the launch (4 tokens on 700, 12 heads of 64: 8.4 us).
+// Rows: bound by what a tile takes of all units and by the clock: 2048 tokens on 6001, 16 heads of 128 on 4, bf16: 127 to 132 us, 890 to 930 TFLOP/s,
+// matrix units 42, vector units 38 and LDS 32 per cent busy at the 2.1 GHz that the clock falls to (2.4 where memory bounds; a product of 8192^3 reaches
+// 1260 TFLOP/s).  Leaving out the loads, or the exponentials, gains a tenth each, and no order of instructions gains any (scores a tile ahead of the
+// weights: the same; 64 rows a wave, 8 waves, tiles of 32 keys: slower).  Of single tokens beside chunks (16 sequences, two of them with 500 new tokens: 54 us): one wave of four works for a
+// token's block, and parts are whole numbers of tiles in one round of workgroups.  Keys: bound by the reads of the cache (814 MB in 133 to 147 us, 5.5
+// to 6.1 TB/s) or, for short ones, by a chain of loads, tables, pages, keys, of about 1 us each, behind the launch (4 tokens on 700, 12 heads of 64: 8.1 us).
 template <class T, int D, int W, int KT, bool KEYS, bool WALKS, int OCC>
 __global__ void __launch_bounds__(64 * W, OCC) page_forward_kernel(PageArgs a, PagePlan plan) {
     constexpr int E = SeqSize<T>::value, RB = D * E, NC = RB / 32, NB = D / 32, KS = KT / 32, SUB = KT / kPageRows;

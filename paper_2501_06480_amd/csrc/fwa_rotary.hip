@@ -12,7 +12,7 @@ struct RotaryPlan {
 
 // A workgroup has its units one behind the other, whatever rows they belong to: memory is read and written in order, and each thread has its four
 // vectors on the way while the workgroup forms the cosines and sines of the rows they touch, each once.  Bound by memory: 2 x 6272 rows of 16 heads
-// of 128, bf16, 103 MB in 20.5 us, 5.0 TB/s, as a copy; 64 windows of 49 rows of 3 heads of 32: 3.7 us, the launch and three loads one behind the
+// of 128, bf16, 103 MB in 20.6 us, 5.0 TB/s, as a copy; 64 windows of 49 rows of 3 heads of 32: 3.6 us, the launch and three loads one behind the
 // other (axis, position, LDS).
 template <class T, int V, int UNITS, int THREADS>
 __global__ void __launch_bounds__(THREADS) rotary_kernel(RotaryArgs a, RotaryPlan plan) {
