@@ -183,7 +183,7 @@ class _Rotary(torch.autograd.Function):
 def rotary(x, heads: int, positions, frequencies, axis_of=None, interleaved: bool = False, inverse: bool = False):
     """Rotary positions (``binding.fwa_rotary``), differentiable in x, any number of times: its gradient is the rotation back.  Frequencies that want a
     gradient are refused."""
-    if frequencies.requires_grad and torch.is_grad_enabled():
+    if getattr(frequencies, "requires_grad", False) and torch.is_grad_enabled():
         raise NotImplementedError("the gradient of the frequencies is not available")
     if _native_node(x, positions, frequencies, axis_of):
         return binding._native().rotary_node(x, int(heads), positions, frequencies, axis_of, bool(interleaved), bool(inverse))

@@ -26,3 +26,11 @@ def test_frequencies_that_want_a_gradient_are_refused():
         autograd.rotary(x, 2, positions, f)
     with pytest.raises(TypeError):
         autograd.rotary(x, 2, positions, f.detach())
+
+
+def test_frequencies_that_are_no_tensor_are_refused_as_such():
+    from paper_2501_06480_amd import autograd
+    x, positions = torch.zeros(1, 4, 128), torch.zeros(4, 1, dtype=torch.int32)
+    for f in (None, [1.0] * 32):
+        with pytest.raises(TypeError):
+            autograd.rotary(x, 2, positions, f)
